@@ -342,6 +342,159 @@ int sfc_gemm_model(int64_t M, int64_t N, int64_t K, int out_type, int ca_layers,
  */
 int sfc_probe_mfma(int random_operands, int iterations, double *tflops, double *mhz);
 
+/* ---- 4-bit operands ---------------------------------------------------------
+ * A microscaled (OCP MX) 4-bit matrix of `rows` x `cols` values is two arrays:
+ *   codes   E2M1 (1 sign, 2 exponent bits with bias 1, 1 mantissa bit: 0, 0.5, 1,
+ *           1.5, 2, 3, 4, 6 and their negatives), two to a byte, the even column
+ *           in the low bits; row i starts at byte i*ldq;
+ *   scales  E8M0, one byte s for each 32 columns, the power 2^(s - 127), 255 = NaN
+ *           (all 32 values are NaN); row i starts at byte i*lds.
+ * Rows whose length is no multiple of 32 end in a block that is filled up with
+ * zeros.  Rules for every call: codes 16-byte aligned, ldq a multiple of 16 and
+ * >= 16*ceil(cols/32); scales 4-byte aligned, lds a multiple of 4 and >=
+ * ceil(cols/32); both below 2^22.  The bytes of a row of scales up to the next
+ * multiple of 4 may be read (the last row's too) but are never used or written.
+ * Matrices that are not in 4 bits are row-major fp32 or bf16 (SFC_OUT_F32,
+ * SFC_OUT_BF16) at element alignment, leading dimensions in elements.
+ */
+
+/*
+ * sfc_mx4_quant -- a matrix to 4 bits, blocks along its rows (Q, S), along its
+ * columns and transposed (Qt, St), or both; an output pair that is NULL is left out.
+ *   X, ldx     rows x cols, in_type.
+ *   order      NULL, or `rows` sorted slots as sfc_moe_sort writes them: row p is
+ *              then X[order[p] / topk], X having x_rows rows, and a row of zeros
+ *              where order[p] < 0 or that row does not exist.  (NULL: x_rows and topk
+ *              are not used.)
+ *   Q, S       rows x cols.    Qt, St   cols x rows.
+ * Scale of a block: max(f - 2, 0), f the exponent field of the largest magnitude as
+ * fp32, i.e. 2^(floor(log2 max) - 2), at least 2^-127; 255 if the block holds an
+ * infinity or NaN.  Element: x over the scale rounded to the nearest E2M1 value,
+ * ties to the even code, at most 6 in magnitude.  The codes of a block with scale
+ * 255 are unspecified.
+ */
+int sfc_mx4_quant(int64_t rows, int64_t cols,
+                  const void *X, int64_t ldx, int in_type,
+                  const int32_t *order, int64_t x_rows, int topk,
+                  void *Q, int64_t ldq, void *S, int64_t lds,
+                  void *Qt, int64_t ldqt, void *St, int64_t ldst, void *stream);
+
+/* sfc_mx4_dequant -- the values of a 4-bit matrix, rows x cols, as fp32 or bf16 (exact
+ * but where a value exceeds the type: then infinity, rounded to nearest). */
+int sfc_mx4_dequant(int64_t rows, int64_t cols,
+                    const void *Q, int64_t ldq, const void *S, int64_t lds,
+                    void *Y, int64_t ldy, int out_type, void *stream);
+
+/*
+ * sfc_gemm_mx4_ex -- C = A * B^T, A (M x K) and B (N x K) in 4 bits, both with their
+ * blocks along K; C fp32 or bf16 (rounded to nearest even from the fp32 sums).
+ *   K          a multiple of 32 (SFC_ERR_INVALID_ARG otherwise); K == 0: C = 0.
+ * Products and block sums are exact, sums of blocks fp32.  Up to 64 rows run on a
+ * kernel that streams B once; the others on 256x256 or 128x128 blocks along the curve,
+ * K in up to 16 layers where that fills the chip (copies in library memory, as for
+ * sfc_gemm).  The choice depends on M, N and K alone, so equal calls give equal bits.
+ * The gradients of C = A * B^T are two such calls: dA = dC * B with dC's blocks along N
+ * and the transposed B (Qt of sfc_mx4_quant), dB = dC^T * A with both transposed.
+ */
+int sfc_gemm_mx4_ex(int64_t M, int64_t N, int64_t K,
+                    const void *A, int64_t lda, const void *As, int64_t ldas,
+                    const void *B, int64_t ldb, const void *Bs, int64_t ldbs,
+                    void *C, int64_t ldc, int out_type, void *stream);
+
+/*
+ * sfc_mx4_linear -- Y = X * W^T with X (M x K, fp32 or bf16) brought to 4 bits within the
+ * call and W (N x K) kept in 4 bits.  K is the row length of X, W's rows hold
+ * ceil(K/32) blocks; the result is that of sfc_mx4_quant and sfc_gemm_mx4_ex.  X's codes
+ * lie in library memory, one per stream, as layer copies do.
+ */
+int sfc_mx4_linear(int64_t M, int64_t N, int64_t K,
+                   const void *X, int64_t ldx, int in_type,
+                   const void *W, int64_t ldw, const void *Ws, int64_t ldws,
+                   void *Y, int64_t ldy, int out_type, void *stream);
+
+/* ---- mixture of experts -------------------------------------------------------
+ * A slot is one (token, choice) pair, slot = token*topk + choice.  Sorted rows belong to
+ * slots: order[p] is the slot of row p (-1: none), pos[slot] its row (-1: dropped), and
+ * rows offsets[e] .. offsets[e+1]-1 are expert e's.  All index arrays are int32 on
+ * the device.  Indices that point outside their array count as none.
+ */
+
+/*
+ * sfc_moe_sort -- slots sorted by expert, stable.
+ *   ids        `slots` expert ids; an id outside 0 .. experts-1 drops the slot.
+ *   align      every expert's rows start at a multiple of it (>= 1); the rows in between
+ *              belong to no slot.
+ *   rows       length of `order`, >= slots + experts*(align - 1).  offsets has
+ *              experts + 1 entries, offsets[experts] being the rows in use (the rest of
+ *              `order` is -1); pos has `slots`.
+ *   ws         NULL (library memory of the stream) or sfc_moe_sort_ws_size() bytes.
+ * At most 1024 experts.
+ */
+size_t sfc_moe_sort_ws_size(int64_t slots, int experts);
+int sfc_moe_sort(int64_t slots, int experts, int align, const int32_t *ids,
+                 int64_t rows, int32_t *offsets, int32_t *order, int32_t *pos,
+                 void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * sfc_moe_dispatch -- Xs[p] = w[order[p]] * X[order[p] / topk], a row of zeros where
+ * order[p] < 0; X tokens x cols, Xs rows x cols, both of `type`; weights fp32 per slot,
+ * or NULL: the rows as they are, bit for bit.
+ */
+int sfc_moe_dispatch(int64_t rows, int64_t cols, int64_t tokens, int topk,
+                     const void *X, int64_t ldx, int type,
+                     const int32_t *order, const float *weights,
+                     void *Xs, int64_t ldxs, void *stream);
+
+/*
+ * sfc_moe_combine -- Y[t] = sum over j ascending of w[t, j] * Ys[pos[t, j]], in fp32,
+ * dropped slots left out; Ys rows x cols, Y tokens x cols, both of `type`; weights
+ * (tokens x topk, fp32) or NULL: 1.  Without weights this is the gradient of
+ * sfc_moe_dispatch without weights.
+ */
+int sfc_moe_combine(int64_t tokens, int64_t cols, int64_t rows, int topk,
+                    const void *Ys, int64_t ldys, int type,
+                    const int32_t *pos, const float *weights,
+                    void *Y, int64_t ldy, void *stream);
+
+/*
+ * sfc_moe_combine_grad -- the gradient of sfc_moe_combine: dYs[pos[t, j]] = w[t, j] * dY[t],
+ * rows of no slot 0, and dW[t, j] = <dY[t], Ys[pos[t, j]]> (fp32, tokens x topk; 0 for a
+ * dropped slot).  order and pos are those of one sfc_moe_sort.
+ */
+int sfc_moe_combine_grad(int64_t tokens, int64_t cols, int64_t rows, int topk,
+                         const void *dY, int64_t lddy, const void *Ys, int64_t ldys, int type,
+                         const int32_t *order, const int32_t *pos, const float *weights,
+                         void *dYs, int64_t lddys, float *dW, void *stream);
+
+/*
+ * sfc_moe_gemm_mx4_ex -- C[p] = A[p] * B[e]^T for the rows p of every expert e; rows behind
+ * the last segment are set to 0.  A rows x K, B `experts` matrices of N x K that lie
+ * stride_b (codes) and stride_bs (scales) bytes apart, multiples of 16 and 4; K a multiple
+ * of 32.  The same call with the transposed weights gives the gradient of A.  The kernel
+ * and its block shape are chosen from rows, N, K and experts; segment lengths are read
+ * on the device.
+ */
+int sfc_moe_gemm_mx4_ex(int64_t rows, int64_t N, int64_t K, int experts,
+                        const void *A, int64_t lda, const void *As, int64_t ldas,
+                        const void *B, int64_t ldb, int64_t stride_b,
+                        const void *Bs, int64_t ldbs, int64_t stride_bs,
+                        const int32_t *offsets,
+                        void *C, int64_t ldc, int out_type, void *stream);
+
+/*
+ * sfc_moe_wgrad_mx4_ex -- C[e] = A[:, seg] * B[:, seg]^T with seg = offsets[e] ..
+ * offsets[e+1]-1, for every expert (zeros for one without rows): the weight gradient, A
+ * being the transposed dY (M x rows) and B the transposed X (N x rows), both with their
+ * blocks along the sorted rows.  Segments must start at multiples of 32
+ * (sfc_moe_sort's align); a start that does not is taken down to one.  C[e] lies
+ * stride_c elements after C[e-1], M x N, ldc.
+ */
+int sfc_moe_wgrad_mx4_ex(int64_t M, int64_t N, int64_t rows, int experts,
+                         const void *A, int64_t lda, const void *As, int64_t ldas,
+                         const void *B, int64_t ldb, const void *Bs, int64_t ldbs,
+                         const int32_t *offsets,
+                         void *C, int64_t ldc, int64_t stride_c, int out_type, void *stream);
+
 /* Static text of a return code. */
 const char *sfc_strerror(int code);
 

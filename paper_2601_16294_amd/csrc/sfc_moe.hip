@@ -1,0 +1,305 @@
+// Tokens sorted by expert and back.
+//
+// A slot is one (token, choice) pair, slot = token * topk + choice, with an expert id; ids
+// outside 0 .. experts-1 are dropped slots.  Sorting is stable: the rows of an expert
+// follow one another in slot order, from a start that is a multiple of `align`.
+//
+//   dispatch   Xs[p] = w[order[p]] * X[order[p] / topk]          (0 where order[p] < 0)
+//   combine    Y[t] = sum_j w[t, j] * Ys[pos[t, j]]              (pos < 0: no term)
+//   gradient   dYs[pos[t, j]] = w[t, j] * dY[t],  dw[t, j] = <dY[t], Ys[pos[t, j]]>
+//
+// The gradient of dispatch without weights is combine without weights.  Sums run in fp32
+// over j ascending, dot products in fp32 over a fixed split of the columns: no result
+// depends on the order in which workgroups run.
+//
+// Bound: memory, every row read and written once (a token's row once per choice).
+#include "sfc_ops_params.h"
+#include "sfc_row_io.h"
+
+namespace sfc {
+
+// ---- sort ----------------------------------------------------------------------------------
+// A workgroup of 16 waves ranks a chunk of kSortChunk slots, a wave 64 at a time in slot
+// order.  The lanes of a wave that hold the same expert find each other by one ballot per
+// bit of the id; a running count per wave and expert lies in LDS.  With several chunks a
+// first launch counts every chunk's slots per expert.
+constexpr int kSortWaves = 16;
+
+__global__ __launch_bounds__(1024) void moe_count_kernel(MoeSortParams p) {
+  extern __shared__ int32_t hist[];
+  for (int e = threadIdx.x; e < p.experts; e += 1024) hist[e] = 0;
+  __syncthreads();
+  const int64_t first = (int64_t)blockIdx.x * kSortChunk;
+  for (int i = threadIdx.x; i < kSortChunk; i += 1024) {
+    if (first + i < p.slots) {
+      const uint32_t e = (uint32_t)p.ids[first + i];
+      if (e < (uint32_t)p.experts) atomicAdd(&hist[e], 1);
+    }
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < p.experts; e += 1024) p.counts[(int64_t)blockIdx.x * p.experts + e] = hist[e];
+}
+
+// LDS: [kSortWaves][experts] running positions, then 16 + 1 scan words.
+__global__ __launch_bounds__(1024) void moe_sort_kernel(MoeSortParams p, int chunks, int bits) {
+  extern __shared__ int32_t hist[];
+  int32_t* wave_sum = hist + kSortWaves * p.experts;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int i = tid; i < kSortWaves * p.experts; i += 1024) hist[i] = 0;
+  __syncthreads();
+
+  constexpr int kRounds = kSortChunk / 1024;
+  const int64_t first = (int64_t)blockIdx.x * kSortChunk + wave * (64 * kRounds) + lane;
+  int32_t* mine = hist + wave * p.experts;
+  uint32_t id[kRounds];
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int64_t slot = first + 64 * r;
+    id[r] = slot < p.slots ? (uint32_t)p.ids[slot] : 0xFFFFFFFFu;
+    if (id[r] < (uint32_t)p.experts) atomicAdd(&mine[id[r]], 1);
+  }
+  __syncthreads();
+
+  // thread e: expert e's count in all chunks and in those before this one
+  int total = 0, before = 0;
+  if (tid < p.experts) {
+    if (chunks == 1) {
+#pragma unroll
+      for (int w = 0; w < kSortWaves; ++w) total += hist[w * p.experts + tid];
+    } else {
+      for (int ch = 0; ch < chunks; ++ch) {
+        const int n = p.counts[(int64_t)ch * p.experts + tid];
+        total += n;
+        before += ch < (int)blockIdx.x ? n : 0;
+      }
+    }
+  }
+  const int padded = (total + p.align - 1) / p.align * p.align;
+  // inclusive sum of the padded counts
+  int sum = padded;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int up = __shfl_up(sum, d);
+    sum += lane >= d ? up : 0;
+  }
+  if (lane == 63) wave_sum[wave] = sum;
+  __syncthreads();
+  if (wave == 0) {
+    int s = lane < kSortWaves ? wave_sum[lane] : 0;
+#pragma unroll
+    for (int d = 1; d < kSortWaves; d <<= 1) {
+      const int up = __shfl_up(s, d);
+      s += lane >= d ? up : 0;
+    }
+    if (lane < kSortWaves) wave_sum[lane] = s;
+  }
+  __syncthreads();
+  if (wave > 0) sum += wave_sum[wave - 1];
+  const int start = sum - padded;
+  const int end = wave_sum[kSortWaves - 1];
+  if (tid < p.experts) {
+    int run = start + before;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      const int n = hist[w * p.experts + tid];
+      hist[w * p.experts + tid] = run;
+      run += n;
+    }
+    if (blockIdx.x == 0) {
+      p.offsets[tid] = start;
+      if (tid == p.experts - 1) p.offsets[p.experts] = sum;
+      for (int i = start + total; i < sum; ++i) p.order[i] = -1;
+    }
+  }
+  for (int64_t i = end + (int64_t)blockIdx.x * 1024 + tid; i < p.rows; i += (int64_t)gridDim.x * 1024) p.order[i] = -1;
+  __syncthreads();
+
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int64_t slot = first + 64 * r;
+    const bool valid = id[r] < (uint32_t)p.experts;
+    uint64_t same = __ballot(valid);
+    for (int b = 0; b < bits; ++b) {
+      const uint64_t ones = __ballot((id[r] >> b) & 1);
+      same &= ((id[r] >> b) & 1) ? ones : ~ones;
+    }
+    int at = -1;
+    if (valid) at = mine[id[r]] + __popcll(same & ((1ull << lane) - 1));
+    // (the other lanes' stores are seen: LDS serves a wave's accesses in order)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    // the last lane of each expert carries the count on
+    if (valid && (same >> lane) == 1) mine[id[r]] = at + 1;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (slot < p.slots) p.pos[slot] = at;
+    if (valid) p.order[at] = (int32_t)slot;
+  }
+}
+
+hipError_t launch_moe_sort(const MoeSortParams& p, hipStream_t stream) {
+  const int chunks = p.slots > 0 ? (int)((p.slots + kSortChunk - 1) / kSortChunk) : 1;
+  if (chunks > 1) {
+    hipLaunchKernelGGL(moe_count_kernel, dim3(chunks), dim3(1024), p.experts * 4u, stream, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  int bits = 0;
+  while ((1 << bits) < p.experts) ++bits;
+  const unsigned lds = (unsigned)(kSortWaves * p.experts + kSortWaves) * 4u;
+  hipLaunchKernelGGL(moe_sort_kernel, dim3(chunks), dim3(1024), lds, stream, p, chunks, bits);
+  return hipGetLastError();
+}
+
+// ---- dispatch ------------------------------------------------------------------------------
+template <bool BF16>
+__global__ __launch_bounds__(256) void moe_dispatch_kernel(MoeRowsParams p, RowShape sh) {
+  const int tx = 1 << sh.tx_log2;
+  const int64_t rb = blockIdx.x / sh.splits;
+  const int split = (int)(blockIdx.x - rb * sh.splits);
+  const int64_t row = rb * (256 >> sh.tx_log2) + (threadIdx.x >> sh.tx_log2);
+  if (row >= p.rows) return;
+  const int64_t chunks = (p.cols + 7) >> 3, first = (int64_t)split * sh.per;
+  const int64_t last = first + sh.per < chunks ? first + sh.per : chunks;
+  const int32_t slot = p.order[row];
+  const int64_t token = slot < 0 ? -1 : (int64_t)((uint32_t)slot / (uint32_t)p.topk);
+  const bool valid = token >= 0 && token < p.tokens;
+  const float w = valid && p.weights ? p.weights[slot] : 1.0f;
+  const char* x = reinterpret_cast<const char*>(p.X) + (valid ? token : 0) * p.ldx * (BF16 ? 2 : 4);
+  char* y = reinterpret_cast<char*>(p.Y) + row * p.ldy * (BF16 ? 2 : 4);
+  for (int64_t c = first + (threadIdx.x & (tx - 1)); c < last; c += tx) {
+    Raw8<BF16> r = valid ? load8<BF16>(x, c * 8, p.cols) : zero8<BF16>();
+    if (p.weights) {
+      float f[8];
+      to_float<BF16>(r, f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] *= w;
+      r = from_float<BF16>(f);
+    }
+    store8<BF16>(y, c * 8, p.cols, r);
+  }
+}
+
+// ---- combine -------------------------------------------------------------------------------
+template <bool BF16>
+__global__ __launch_bounds__(256) void moe_combine_kernel(MoeRowsParams p, RowShape sh) {
+  const int tx = 1 << sh.tx_log2;
+  const int64_t rb = blockIdx.x / sh.splits;
+  const int split = (int)(blockIdx.x - rb * sh.splits);
+  const int64_t t = rb * (256 >> sh.tx_log2) + (threadIdx.x >> sh.tx_log2);
+  if (t >= p.tokens) return;
+  const int64_t chunks = (p.cols + 7) >> 3, first = (int64_t)split * sh.per;
+  const int64_t last = first + sh.per < chunks ? first + sh.per : chunks;
+  const char* ys = reinterpret_cast<const char*>(p.X);
+  char* y = reinterpret_cast<char*>(p.Y) + t * p.ldy * (BF16 ? 2 : 4);
+  const int32_t* pos = p.pos + t * p.topk;
+  for (int64_t c = first + (threadIdx.x & (tx - 1)); c < last; c += tx) {
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    // four rows in flight
+    for (int j = 0; j < p.topk; j += 4) {
+      Raw8<BF16> r[4];
+      float w[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t at = j + u < p.topk ? pos[j + u] : -1;
+        const bool valid = at >= 0 && at < p.rows;
+        r[u] = valid ? load8<BF16>(ys + at * p.ldx * (BF16 ? 2 : 4), c * 8, p.cols) : zero8<BF16>();
+        w[u] = valid && p.weights ? p.weights[t * p.topk + j + u] : valid ? 1.0f : 0.0f;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float f[8];
+        to_float<BF16>(r[u], f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += f[i] * w[u];
+      }
+    }
+    store8<BF16>(y, c * 8, p.cols, from_float<BF16>(sum));
+  }
+}
+
+// ---- gradient of combine -------------------------------------------------------------------
+// W waves per token; behind the tokens' workgroups, others clear the rows that no slot has.
+template <bool BF16, int W>
+__global__ __launch_bounds__(256) void moe_combine_grad_kernel(MoeRowsParams p, int64_t token_groups) {
+  __shared__ float part[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t chunks = (p.cols + 7) >> 3;
+  constexpr int ES = BF16 ? 2 : 4;
+  if ((int64_t)blockIdx.x >= token_groups) {
+    const int64_t r0 = ((int64_t)blockIdx.x - token_groups) * 256 + 64 * wave;
+    const int32_t slot = r0 + lane < p.rows ? p.order[r0 + lane] : 0;
+    uint64_t none = __ballot(slot < 0 || (int64_t)slot >= p.tokens * p.topk);
+    while (none) {
+      const int i = __ffsll((unsigned long long)none) - 1;
+      none &= none - 1;
+      char* y = reinterpret_cast<char*>(p.Y) + (r0 + i) * p.ldy * ES;
+      for (int64_t c = lane; c < chunks; c += 64) store8<BF16>(y, c * 8, p.cols, zero8<BF16>());
+    }
+    return;
+  }
+  const int64_t t = (int64_t)blockIdx.x * (4 / W) + wave / W;
+  const int part_of = W == 4 ? wave : 0;       // this wave's share of the token's chunks
+  const bool in = t < p.tokens;
+  const char* dy = reinterpret_cast<const char*>(p.X) + (in ? t : 0) * p.ldx * ES;
+  for (int j = 0; j < p.topk; ++j) {
+    const int64_t at = in ? p.pos[t * p.topk + j] : -1;
+    const bool valid = at >= 0 && at < p.rows;
+    float dot = 0.f;
+    if (valid) {
+      const float w = p.weights ? p.weights[t * p.topk + j] : 1.0f;
+      const char* ys = reinterpret_cast<const char*>(p.Ys) + at * p.ldys * ES;
+      char* y = reinterpret_cast<char*>(p.Y) + at * p.ldy * ES;
+#pragma unroll 2
+      for (int64_t c = part_of * 64 + lane; c < chunks; c += 64 * W) {
+        const Raw8<BF16> a = load8<BF16>(dy, c * 8, p.cols), b = load8<BF16>(ys, c * 8, p.cols);
+        float f[8], g[8];
+        to_float<BF16>(a, f);
+        to_float<BF16>(b, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          dot += f[i] * g[i];
+          f[i] *= w;
+        }
+        store8<BF16>(y, c * 8, p.cols, from_float<BF16>(f));
+      }
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) dot += __shfl_xor(dot, d);
+    if constexpr (W == 4) {
+      if (lane == 0) part[wave] = dot;
+      __syncthreads();
+      dot = (part[0] + part[1]) + (part[2] + part[3]);
+      __syncthreads();
+    }
+    if (in && lane == 0 && part_of == 0) p.dW[t * p.topk + j] = dot;
+  }
+}
+
+hipError_t launch_moe_dispatch(const MoeRowsParams& p, bool bf16, int num_cus, hipStream_t stream) {
+  const RowShape sh = row_shape(p.rows, (p.cols + 7) / 8, num_cus);
+  const dim3 g((unsigned)(sh.row_blocks * sh.splits)), b(256);
+  if (bf16) hipLaunchKernelGGL((moe_dispatch_kernel<true>), g, b, 0, stream, p, sh);
+  else hipLaunchKernelGGL((moe_dispatch_kernel<false>), g, b, 0, stream, p, sh);
+  return hipGetLastError();
+}
+
+hipError_t launch_moe_combine(const MoeRowsParams& p, bool bf16, int num_cus, hipStream_t stream) {
+  const RowShape sh = row_shape(p.tokens, (p.cols + 7) / 8, num_cus);
+  const dim3 g((unsigned)(sh.row_blocks * sh.splits)), b(256);
+  if (bf16) hipLaunchKernelGGL((moe_combine_kernel<true>), g, b, 0, stream, p, sh);
+  else hipLaunchKernelGGL((moe_combine_kernel<false>), g, b, 0, stream, p, sh);
+  return hipGetLastError();
+}
+
+hipError_t launch_moe_combine_grad(const MoeRowsParams& p, bool bf16, int num_cus, hipStream_t stream) {
+  // a whole workgroup for a token's row where a wave would loop over it more than 4 times
+  const bool wide = p.cols > 4 * 512;
+  const int64_t groups = wide ? p.tokens : (p.tokens + 3) / 4;
+  const dim3 g((unsigned)(groups + (p.rows + 255) / 256)), b(256);
+  if (bf16 && wide) hipLaunchKernelGGL((moe_combine_grad_kernel<true, 4>), g, b, 0, stream, p, groups);
+  else if (bf16) hipLaunchKernelGGL((moe_combine_grad_kernel<true, 1>), g, b, 0, stream, p, groups);
+  else if (wide) hipLaunchKernelGGL((moe_combine_grad_kernel<false, 4>), g, b, 0, stream, p, groups);
+  else hipLaunchKernelGGL((moe_combine_grad_kernel<false, 1>), g, b, 0, stream, p, groups);
+  return hipGetLastError();
+}
+
+}  // namespace sfc

@@ -14,6 +14,7 @@
 #include <string>
 #include <tuple>
 
+#include "sfc_host.h"
 #include "sfc_model.h"
 #include "sfc_params.h"
 #include "sfc_validate.h"
@@ -680,6 +681,33 @@ int gemm_noalloc_impl(int64_t M, int64_t N, int64_t K, const void* A, int64_t ld
 }
 
 }  // namespace
+
+namespace sfc {
+
+int host_error(int code, const char* what) { return set_error(code, what); }
+int host_hip_error(hipError_t e, const char* where) { return hip_fail(e, where); }
+std::mutex& host_mutex() { return g_mu; }
+
+int host_num_cus(int* num_cus) {
+  DeviceState* st = nullptr;
+  const int rc = device_state(&st);
+  if (rc == SFC_OK) *num_cus = st->num_cus;
+  return rc;
+}
+
+int host_table(int gm, int gn, hipStream_t stream, const int32_t** table) {
+  DeviceState* st = nullptr;
+  const int rc = device_state(&st);
+  return rc != SFC_OK ? rc : get_table(*st, gm, gn, SFC_ORDER_HILBERT, stream, table);
+}
+
+int host_workspace(hipStream_t stream, size_t bytes, void** ws) {
+  DeviceState* st = nullptr;
+  const int rc = device_state(&st);
+  return rc != SFC_OK ? rc : stream_workspace(*st, stream, bytes, ws);
+}
+
+}  // namespace sfc
 
 extern "C" {
 

@@ -35,7 +35,11 @@ SCHEDS = {"interleaved": 0, "block": 1, "interleaved_plain": 2}
 # Every symbol include/sfcgemm.h declares.
 EXPORTS = ["sfc_tile_order", "sfc_tile_order_ex", "sfc_gemm", "sfc_gemm_bf16out", "sfc_gemm_ws_size",
            "sfc_gemm_ex", "sfc_gemm_fused_ex", "sfc_gemm_noalloc_ex", "sfc_gemm_f8_ex", "sfc_gemm_f8_fmt_ex", "sfc_gemm_plan", "sfc_gemm_f8_plan", "sfc_gemm_model", "sfc_probe_mfma", "sfc_strerror",
-           "sfc_last_error", "sfc_version"]
+           "sfc_last_error", "sfc_version",
+           # the operators of sfcops.py
+           "sfc_mx4_quant", "sfc_mx4_dequant", "sfc_gemm_mx4_ex", "sfc_mx4_linear", "sfc_moe_sort_ws_size",
+           "sfc_moe_sort", "sfc_moe_dispatch", "sfc_moe_combine", "sfc_moe_combine_grad", "sfc_moe_gemm_mx4_ex",
+           "sfc_moe_wgrad_mx4_ex"]
 
 
 class SfcError(RuntimeError):

@@ -1,0 +1,332 @@
+"""Python binding of the 4-bit (MX) and mixture-of-experts operators of libsfcgemm.so.
+
+Argument marshalling and checks only, as in ``sfcgemm``; names follow the C ABI
+(include/sfcgemm.h, where each operator's definition stands).  Outputs are tensors
+that the caller passes.
+
+A 4-bit matrix of rows x cols values is a pair of uint8 tensors: codes (rows,
+16 * ceil(cols/32)), two E2M1 codes to a byte, and scales (rows, ceil(cols/32)), E8M0;
+rows of codes lie a multiple of 16 bytes apart, rows of scales a multiple of 4.
+``mx4_empty`` allocates such a pair.
+
+    xq = mx4_empty(M, K)
+    sfc_mx4_quant(x, *xq)
+    sfc_gemm_mx4_ex(*xq, *wq, y)            # y = x w^T
+"""
+from __future__ import annotations
+
+import ctypes
+
+from paper_2601_16294_amd.sfcgemm import SFC_OUT_BF16, SFC_OUT_F32, SfcError, _cached, _check, _stream_handle, lib
+
+__all__ = ["SfcError", "mx4_empty", "sfc_mx4_quant", "sfc_mx4_dequant", "sfc_gemm_mx4_ex", "sfc_mx4_linear",
+           "sfc_moe_sort", "sfc_moe_sort_rows", "sfc_moe_dispatch", "sfc_moe_combine", "sfc_moe_combine_grad",
+           "sfc_moe_gemm_mx4_ex", "sfc_moe_wgrad_mx4_ex"]
+
+
+def _declare() -> None:
+    i64, i32, p, sz = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
+    mx = [p, i64, p, i64]                        # codes, row bytes, scales, row bytes
+    rows = [p, i64]                              # matrix, leading dimension
+    lib.sfc_mx4_quant.argtypes = [i64, i64] + rows + [i32, p, i64, i32] + mx + mx + [p]
+    lib.sfc_mx4_dequant.argtypes = [i64, i64] + mx + rows + [i32, p]
+    lib.sfc_gemm_mx4_ex.argtypes = [i64, i64, i64] + mx + mx + rows + [i32, p]
+    lib.sfc_mx4_linear.argtypes = [i64, i64, i64] + rows + [i32] + mx + rows + [i32, p]
+    lib.sfc_moe_sort_ws_size.argtypes = [i64, i32]
+    lib.sfc_moe_sort.argtypes = [i64, i32, i32, p, i64, p, p, p, p, sz, p]
+    lib.sfc_moe_dispatch.argtypes = [i64, i64, i64, i32] + rows + [i32, p, p] + rows + [p]
+    lib.sfc_moe_combine.argtypes = [i64, i64, i64, i32] + rows + [i32, p, p] + rows + [p]
+    lib.sfc_moe_combine_grad.argtypes = [i64, i64, i64, i32] + rows + rows + [i32, p, p, p] + rows + [p, p]
+    lib.sfc_moe_gemm_mx4_ex.argtypes = [i64, i64, i64, i32] + mx + [p, i64, i64, p, i64, i64, p] + rows + [i32, p]
+    lib.sfc_moe_wgrad_mx4_ex.argtypes = [i64, i64, i64, i32] + mx + mx + [p] + rows + [i64, i32, p]
+    for name in __all__:
+        if name.startswith("sfc_") and name != "sfc_moe_sort_rows":
+            getattr(lib, name).restype = i32
+    lib.sfc_moe_sort_ws_size.restype = sz
+
+
+_declare()
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _types():
+    torch = _torch()
+    return {torch.float32: SFC_OUT_F32, torch.bfloat16: SFC_OUT_BF16}
+
+
+def _current_device():
+    return _torch().cuda.current_device
+
+
+def _tensor(t, name, what):
+    if not isinstance(t, _cached(_torch).Tensor):
+        raise TypeError(f"{what}: {name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{what}: {name} must be a CUDA tensor (got {t.device})")
+    if t.get_device() != _cached(_current_device)():
+        raise ValueError(f"{what}: {name} is on {t.device}, the current device is "
+                         f"cuda:{_cached(_current_device)()}")
+
+
+def _rows(t, name, what, shape=None):
+    """(pointer, leading dimension, type code) of a 2-D fp32 or bf16 tensor with unit column stride."""
+    _tensor(t, name, what)
+    code = _cached(_types).get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what}: {name} must be float32 or bfloat16 (got {t.dtype})")
+    if t.dim() != 2:
+        raise ValueError(f"{what}: {name} must be 2-D")
+    r, c = t.shape
+    if shape is not None and (r != shape[0] or c != shape[1]):
+        raise ValueError(f"{what}: shape mismatch: {name} is {tuple(t.shape)}, expected {tuple(shape)}")
+    s0, s1 = t.stride()
+    if s1 != 1 and c > 1:
+        raise ValueError(f"{what}: {name} must have unit column stride")
+    return t.data_ptr(), s0 if r > 1 else max(c, 1), code
+
+
+def _blocks(cols: int) -> int:
+    return (cols + 31) // 32
+
+
+def _mx4(q, s, name, what, rows=None, cols=None, lead=0):
+    """(codes, row bytes, scales, row bytes) of a 4-bit matrix, `lead` dimensions before it.
+    Checks the shape against rows x cols where they are given."""
+    for t, n in ((q, name), (s, f"the scales of {name}")):
+        _tensor(t, n, what)
+        if t.dtype != _cached(_torch).uint8:
+            raise TypeError(f"{what}: {n} must be uint8 (got {t.dtype})")
+        if t.dim() != 2 + lead:
+            raise ValueError(f"{what}: {n} must be {2 + lead}-D")
+        if t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError(f"{what}: {n} must have unit column stride")
+    r, half = q.shape[-2:]
+    blocks = s.shape[-1]
+    if half != 16 * blocks or s.shape[:-1] != q.shape[:-1]:
+        raise ValueError(f"{what}: shape mismatch: {name} {tuple(q.shape)} and its scales {tuple(s.shape)} "
+                         "(16 bytes of codes to a scale)")
+    if rows is not None and (r != rows or blocks != _blocks(cols)):
+        raise ValueError(f"{what}: shape mismatch: {name} is {tuple(q.shape)}, expected "
+                         f"{(rows, 16 * _blocks(cols))}")
+    padded = (blocks + 3) // 4 * 4
+    ldq, lds = (q.stride(-2), s.stride(-2)) if r > 1 else (max(half, 16), max(padded, 4))
+    if padded != blocks and q.numel():
+        # the last row of scales, too, is read in whole groups of 4
+        last = s.storage_offset() + sum((n - 1) * st for n, st in zip(s.shape[:-1], s.stride()[:-1]))
+        if last + padded > s.untyped_storage().nbytes():
+            raise ValueError(f"{what}: the scales of {name} end inside a group of 4 bytes: allocate rows of "
+                             f"{padded} (mx4_empty does)")
+    return q.data_ptr(), ldq, s.data_ptr(), lds
+
+
+def _ints(t, name, what, count):
+    """Pointer of a contiguous int32 tensor of `count` elements."""
+    _tensor(t, name, what)
+    if t.dtype != _cached(_torch).int32:
+        raise TypeError(f"{what}: {name} must be int32 (got {t.dtype})")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: {name} must be contiguous")
+    if count is not None and t.numel() != count:
+        raise ValueError(f"{what}: {name} has {t.numel()} elements, expected {count}")
+    return t.data_ptr()
+
+
+def _weights(t, what, count, name="weights"):
+    if t is None:
+        return None
+    _tensor(t, name, what)
+    if t.dtype != _cached(_torch).float32:
+        raise TypeError(f"{what}: {name} must be float32 (got {t.dtype})")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: {name} must be contiguous")
+    if count is not None and t.numel() != count:
+        raise ValueError(f"{what}: {name} has {t.numel()} elements, expected {count}")
+    return t.data_ptr()
+
+
+def _topk(topk, what):
+    if topk < 1:
+        raise ValueError(f"{what}: topk must be >= 1")
+    return topk
+
+
+def mx4_empty(rows: int, cols: int, lead=(), device=None):
+    """Uninitialised (codes, scales) of a rows x cols 4-bit matrix (or of `lead` such matrices)."""
+    torch = _cached(_torch)
+    device = "cuda" if device is None else device
+    b = _blocks(cols)
+    codes = torch.empty((*lead, rows, 16 * b), dtype=torch.uint8, device=device)
+    scales = torch.empty((*lead, rows, (b + 3) // 4 * 4), dtype=torch.uint8, device=device)
+    return codes, scales[..., :b]
+
+
+def sfc_mx4_quant(X, Q=None, S=None, Qt=None, St=None, order=None, topk: int = 1, stream=None) -> None:
+    """X (rows, cols) to 4 bits: Q, S with blocks along the rows, and / or Qt, St (cols, rows),
+    transposed with blocks along the columns.  With `order` (sfc_moe_sort's) the rows are
+    X[order // topk], zeros where order is negative."""
+    what = "sfc_mx4_quant"
+    px, ldx, kind = _rows(X, "X", what)
+    x_rows, cols = X.shape
+    rows, po = x_rows, None
+    if order is not None:
+        po, rows = _ints(order, "order", what, None), order.numel()
+        _topk(topk, what)
+    if (Q is None) != (S is None) or (Qt is None) != (St is None):
+        raise ValueError(f"{what}: codes and scales go together")
+    if Q is None and Qt is None:
+        raise ValueError(f"{what}: no output")
+    a = _mx4(Q, S, "Q", what, rows, cols) if Q is not None else (None, 0, None, 0)
+    b = _mx4(Qt, St, "Qt", what, cols, rows) if Qt is not None else (None, 0, None, 0)
+    _check(lib.sfc_mx4_quant(rows, cols, px, ldx, kind, po, x_rows, topk, *a, *b, _stream_handle(stream)), what)
+
+
+def sfc_mx4_dequant(Q, S, Y, stream=None) -> None:
+    """Y (rows, cols), float32 or bfloat16, = the values of the 4-bit matrix (Q, S)."""
+    what = "sfc_mx4_dequant"
+    py, ldy, kind = _rows(Y, "Y", what)
+    rows, cols = Y.shape
+    _check(lib.sfc_mx4_dequant(rows, cols, *_mx4(Q, S, "Q", what, rows, cols), py, ldy, kind, _stream_handle(stream)),
+           what)
+
+
+def sfc_gemm_mx4_ex(A, As, B, Bs, C, stream=None) -> None:
+    """C (M, N), float32 or bfloat16, = A B^T with A (M, K) and B (N, K) in 4 bits."""
+    what = "sfc_gemm_mx4_ex"
+    a, b = _mx4(A, As, "A", what), _mx4(B, Bs, "B", what)
+    M, K, N = A.shape[0], 32 * As.shape[1], B.shape[0]
+    if Bs.shape[1] != As.shape[1]:
+        raise ValueError(f"{what}: shape mismatch: A {tuple(A.shape)} B {tuple(B.shape)}")
+    pc, ldc, kind = _rows(C, "C", what, (M, N))
+    _check(lib.sfc_gemm_mx4_ex(M, N, K, *a, *b, pc, ldc, kind, _stream_handle(stream)), what)
+
+
+def sfc_mx4_linear(X, W, Ws, Y, stream=None) -> None:
+    """Y (M, N) = X W^T with X (M, K), float32 or bfloat16, brought to 4 bits in the call and
+    W (N, K) in 4 bits."""
+    what = "sfc_mx4_linear"
+    px, ldx, kind = _rows(X, "X", what)
+    M, K = X.shape
+    N = W.shape[0]
+    w = _mx4(W, Ws, "W", what, N, K)
+    py, ldy, out = _rows(Y, "Y", what, (M, N))
+    _check(lib.sfc_mx4_linear(M, N, K, px, ldx, kind, *w, py, ldy, out, _stream_handle(stream)), what)
+
+
+def sfc_moe_sort_rows(slots: int, experts: int, align: int = 1) -> int:
+    """Rows that sorted arrays need: every slot, and the padding of each expert's rows."""
+    return slots + experts * (align - 1)
+
+
+def sfc_moe_sort(ids, offsets, order, pos, align: int = 1, workspace=None, stream=None) -> None:
+    """Slots sorted by expert.  ids (int32, any shape; slot = flat index), offsets
+    (experts + 1,), order (at least sfc_moe_sort_rows(...),), pos (as many as ids): int32."""
+    what = "sfc_moe_sort"
+    slots = ids.numel()
+    pi, pp = _ints(ids, "ids", what, None), _ints(pos, "pos", what, slots)
+    po, pr = _ints(offsets, "offsets", what, None), _ints(order, "order", what, None)
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        _tensor(workspace, "workspace", what)
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(lib.sfc_moe_sort(slots, offsets.numel() - 1, align, pi, order.numel(), po, pr, pp, ws, ws_bytes,
+                            _stream_handle(stream)), what)
+
+
+def sfc_moe_dispatch(X, order, Xs, topk: int = 1, weights=None, stream=None) -> None:
+    """Xs (rows, cols) = the tokens' rows in sorted order, X (tokens, cols); times weights
+    (float32, tokens * topk) if given."""
+    what = "sfc_moe_dispatch"
+    px, ldx, kind = _rows(X, "X", what)
+    tokens, cols = X.shape
+    rows = order.numel()
+    ps, lds, out = _rows(Xs, "Xs", what, (rows, cols))
+    if out != kind:
+        raise TypeError(f"{what}: Xs must hold X's type")
+    _check(lib.sfc_moe_dispatch(rows, cols, tokens, _topk(topk, what), px, ldx, kind, _ints(order, "order", what, rows),
+                                _weights(weights, what, tokens * topk), ps, lds, _stream_handle(stream)), what)
+
+
+def sfc_moe_combine(Ys, pos, Y, weights=None, stream=None) -> None:
+    """Y (tokens, cols) = sum over a token's slots of weights * Ys[pos]; Ys (rows, cols), pos
+    and weights of tokens * topk elements, the topk slots of a token side by side."""
+    what = "sfc_moe_combine"
+    pr, ldr, kind = _rows(Ys, "Ys", what)
+    rows, cols = Ys.shape
+    py, ldy, out = _rows(Y, "Y", what)
+    tokens = Y.shape[0]
+    if Y.shape[1] != cols:
+        raise ValueError(f"{what}: shape mismatch: Ys {tuple(Ys.shape)} Y {tuple(Y.shape)}")
+    if out != kind:
+        raise TypeError(f"{what}: Y must hold Ys's type")
+    slots = pos.numel()
+    topk = _slots_per_token(slots, tokens, what)
+    _check(lib.sfc_moe_combine(tokens, cols, rows, topk, pr, ldr, kind, _ints(pos, "pos", what, slots),
+                               _weights(weights, what, slots), py, ldy, _stream_handle(stream)), what)
+
+
+def _slots_per_token(slots, tokens, what):
+    if tokens == 0:
+        if slots:
+            raise ValueError(f"{what}: pos has {slots} elements, expected 0")
+        return 1
+    if slots == 0 or slots % tokens:
+        raise ValueError(f"{what}: pos has {slots} elements, expected a multiple of {tokens} tokens")
+    return slots // tokens
+
+
+def sfc_moe_combine_grad(dY, Ys, order, pos, weights, dYs, dW, stream=None) -> None:
+    """Gradient of sfc_moe_combine: dYs (rows, cols) and dW (float32, tokens * topk) from dY
+    (tokens, cols), Ys (rows, cols) and weights (or None: 1)."""
+    what = "sfc_moe_combine_grad"
+    pd, ldd, kind = _rows(dY, "dY", what)
+    tokens, cols = dY.shape
+    pr, ldr, kr = _rows(Ys, "Ys", what)
+    rows = Ys.shape[0]
+    if Ys.shape[1] != cols:
+        raise ValueError(f"{what}: shape mismatch: dY {tuple(dY.shape)} Ys {tuple(Ys.shape)}")
+    ps, lds, ks = _rows(dYs, "dYs", what, (rows, cols))
+    if kr != kind or ks != kind:
+        raise TypeError(f"{what}: Ys and dYs must hold dY's type")
+    slots = pos.numel()
+    topk = _slots_per_token(slots, tokens, what)
+    if dW is None:
+        raise TypeError(f"{what}: dW must be a torch.Tensor")
+    _check(lib.sfc_moe_combine_grad(tokens, cols, rows, topk, pd, ldd, pr, ldr, kind, _ints(order, "order", what, rows),
+                                    _ints(pos, "pos", what, slots), _weights(weights, what, slots), ps, lds,
+                                    _weights(dW, what, slots, "dW"), _stream_handle(stream)), what)
+
+
+def sfc_moe_gemm_mx4_ex(A, As, B, Bs, offsets, C, stream=None) -> None:
+    """C (rows, N) = A (rows, K) times, row by row, the transposed B (experts, N, K) of the row's
+    expert; rows offsets[e] .. offsets[e+1]-1 are expert e's.  4-bit operands."""
+    what = "sfc_moe_gemm_mx4_ex"
+    a, b = _mx4(A, As, "A", what), _mx4(B, Bs, "B", what, lead=1)
+    rows, K, E, N = A.shape[0], 32 * As.shape[1], B.shape[0], B.shape[1]
+    if Bs.shape[2] != As.shape[1]:
+        raise ValueError(f"{what}: shape mismatch: A {tuple(A.shape)} B {tuple(B.shape)}")
+    pc, ldc, kind = _rows(C, "C", what, (rows, N))
+    _check(lib.sfc_moe_gemm_mx4_ex(rows, N, K, E, *a, b[0], b[1], B.stride(0), b[2], b[3], Bs.stride(0),
+                                   _ints(offsets, "offsets", what, E + 1), pc, ldc, kind, _stream_handle(stream)), what)
+
+
+def sfc_moe_wgrad_mx4_ex(A, As, B, Bs, offsets, C, stream=None) -> None:
+    """C (experts, M, N), C[e] = A[:, seg] B[:, seg]^T over the sorted rows seg of expert e (starts
+    multiples of 32); A (M, rows) and B (N, rows) in 4 bits, blocks along the rows."""
+    what = "sfc_moe_wgrad_mx4_ex"
+    a, b = _mx4(A, As, "A", what), _mx4(B, Bs, "B", what)
+    M, N, rows = A.shape[0], B.shape[0], 32 * As.shape[1]
+    if Bs.shape[1] != As.shape[1]:
+        raise ValueError(f"{what}: shape mismatch: A {tuple(A.shape)} B {tuple(B.shape)}")
+    if not isinstance(C, _cached(_torch).Tensor) or C.dim() != 3:
+        raise ValueError(f"{what}: C must be a 3-D tensor")
+    E = C.shape[0]
+    po = _ints(offsets, "offsets", what, None)
+    if E < 1 or offsets.numel() != E + 1 or C.shape[1] != M or C.shape[2] != N:
+        raise ValueError(f"{what}: shape mismatch: A {tuple(A.shape)} B {tuple(B.shape)} offsets "
+                         f"{tuple(offsets.shape)} C {tuple(C.shape)}")
+    pc, ldc, kind = _rows(C[0], "C", what, (M, N))
+    _check(lib.sfc_moe_wgrad_mx4_ex(M, N, rows, E, *a, *b, po, pc, ldc, C.stride(0), kind, _stream_handle(stream)), what)

@@ -1,0 +1,276 @@
+"""Sorting by expert, dispatch, combine, their gradients and the experts' 4-bit products on the GPU.
+
+Integers are compared exactly.  A weighted sum of k rows in fp32 is within (k + 1) * 2^-23 of
+the sum of magnitudes, a dot product over D terms within (D + 1) * 2^-23; bf16 output adds 2^-8 of
+the result.  Products: as in test_gpu_mx4."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx4
+from test_gpu_mx4 import BF16, F32, check, host, inputs, operand
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def so():
+    from paper_2601_16294_amd import sfcops
+    return sfcops
+
+
+def routing(T, k, E, seed, skew=0.0, dropped=0.0):
+    rng = np.random.default_rng(seed)
+    p = np.exp(skew * rng.standard_normal(E))
+    ids = np.stack([rng.choice(E, k, replace=False, p=p / p.sum()) for _ in range(T)]) if T else np.zeros((0, k))
+    ids = ids.astype(np.int32)
+    ids[rng.random(ids.shape) < dropped] = rng.choice([-1, E, 1 << 30])
+    return ids
+
+
+def sort(so, ids, E, align, extra=0, **kw):
+    rows = so.sfc_moe_sort_rows(ids.size, E, align) + extra
+    offsets = torch.full((E + 1,), 7, dtype=torch.int32, device="cuda")
+    order = torch.full((rows,), 7, dtype=torch.int32, device="cuda")
+    pos = torch.full((ids.size,), 7, dtype=torch.int32, device="cuda")
+    so.sfc_moe_sort(torch.from_numpy(ids).cuda(), offsets, order, pos, align=align, **kw)
+    return offsets, order, pos
+
+
+@pytest.mark.parametrize("T,k,E,align,dropped", [
+    (0, 2, 8, 1, 0), (0, 1, 3, 16, 0), (1, 1, 1, 1, 0), (5, 2, 2, 1, 0), (16, 2, 8, 1, 0), (16, 4, 60, 32, 0.3),
+    (2048, 2, 8, 1, 0), (2049, 2, 8, 1, 0), (4097, 1, 64, 16, 0.1), (3000, 8, 128, 32, 0), (999, 5, 1024, 3, 0.2),
+    (5000, 1, 1, 64, 0)])
+def test_sort(so, T, k, E, align, dropped):
+    ids = routing(T, k, E, T + E, 1.0, dropped)
+    got = sort(so, ids, E, align, extra=3)
+    want = mx4.sort_slots(ids, E, align, got[1].numel())
+    for g, w in zip(got, want):
+        assert (g.cpu().numpy() == w).all()
+    ws = torch.empty(max(so.lib.sfc_moe_sort_ws_size(ids.size, E), 4), dtype=torch.uint8, device="cuda")
+    again = sort(so, ids, E, align, extra=3, workspace=ws)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+def test_sort_of_dropped_slots_only(so):
+    ids = np.full((10, 2), -1, dtype=np.int32)
+    offsets, order, pos = sort(so, ids, 4, 8)
+    assert (offsets == 0).all() and (order == -1).all() and (pos == -1).all()
+
+
+CASES = [(1, 1, 1, 1), (3, 2, 4, 7), (16, 2, 8, 4096), (100, 4, 8, 129), (333, 1, 60, 64), (257, 5, 16, 2056), (50, 8, 64, 1000)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,k,E,D", CASES)
+@pytest.mark.parametrize("align,dropped", [(1, 0.0), (32, 0.2)])
+def test_dispatch_and_combine(so, dtype, T, k, E, D, align, dropped):
+    ids = routing(T, k, E, D, 0.5, dropped)
+    offsets, order, pos = sort(so, ids, E, align)
+    rows = order.numel()
+    x = inputs(T, D, dtype, 1, D + 3, 1)
+    w = torch.rand((T, k), device="cuda")
+    ys = inputs(rows, D, dtype, 2, D + 1)
+    o, p, wn = order.cpu().numpy(), pos.cpu().numpy().reshape(T, k), host(w)
+    # dispatch
+    xs = torch.full((rows, D + 2), 9.0, dtype=dtype, device="cuda")
+    so.sfc_moe_dispatch(x, order, xs[:, 1:1 + D], topk=k)
+    want = np.where((o >= 0)[:, None], host(x)[np.maximum(o, 0) // k], 0.0)
+    assert (host(xs)[:, 1:1 + D] == want).all() and (xs[:, 0] == 9).all() and (xs[:, 1 + D:] == 9).all()
+    xw = torch.empty((rows, D), dtype=dtype, device="cuda")
+    so.sfc_moe_dispatch(x, order, xw, topk=k, weights=w)
+    ref = want * np.where(o >= 0, wn.reshape(-1)[np.maximum(o, 0)], 0.0)[:, None]
+    assert (np.abs(host(xw) - ref) <= (2.0 ** -8 if dtype == BF16 else 2.0 ** -24) * np.abs(ref)).all()
+    # combine
+    for weights in (w, None):
+        y = torch.full((T, D + 2), 9.0, dtype=dtype, device="cuda")
+        so.sfc_moe_combine(ys, pos, y[:, 1:1 + D], weights=weights)
+        ww = wn if weights is not None else np.ones_like(wn)
+        terms = np.where((p >= 0)[..., None], host(ys)[np.maximum(p, 0)], 0.0) * np.where(p >= 0, ww, 0.0)[..., None]
+        ref, size = terms.sum(1), np.abs(terms).sum(1)
+        bound = (k + 1) * 2.0 ** -23 * size
+        if dtype == BF16:
+            bound = bound + 2.0 ** -8 * (np.abs(ref) + bound)
+        assert (np.abs(host(y)[:, 1:1 + D] - ref) <= bound).all()
+        assert (y[:, 0] == 9).all() and (y[:, 1 + D:] == 9).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,k,E,D", CASES)
+@pytest.mark.parametrize("align,dropped", [(1, 0.0), (32, 0.2)])
+def test_combine_gradient(so, dtype, T, k, E, D, align, dropped):
+    ids = routing(T, k, E, D + 1, 0.5, dropped)
+    offsets, order, pos = sort(so, ids, E, align)
+    rows = order.numel()
+    dy = inputs(T, D, dtype, 1, D + 3, 1)
+    ys = inputs(rows, D, dtype, 2, D + 1)
+    w = torch.rand((T, k), device="cuda")
+    o, p = order.cpu().numpy(), pos.cpu().numpy().reshape(T, k)
+    for weights in (w, None):
+        dys = torch.full((rows, D + 1), 9.0, dtype=dtype, device="cuda")
+        dw = torch.full((T, k), 9.0, device="cuda")
+        so.sfc_moe_combine_grad(dy, ys, order, pos, weights, dys[:, :D], dw)
+        wn = host(w) if weights is not None else np.ones((T, k))
+        ref = np.where((o >= 0)[:, None], host(dy)[np.maximum(o, 0) // k] * wn.reshape(-1)[np.maximum(o, 0)][:, None], 0.0)
+        assert (np.abs(host(dys)[:, :D] - ref) <= (2.0 ** -8 if dtype == BF16 else 2.0 ** -24) * np.abs(ref)).all()
+        assert (dys[:, D:] == 9).all()
+        terms = host(dy)[:, None] * host(ys)[np.maximum(p, 0)] * (p >= 0)[..., None]
+        assert (np.abs(host(dw) - terms.sum(2)) <= (D + 1) * 2.0 ** -23 * np.abs(terms).sum(2)).all()
+
+
+def test_gradients_against_differences(so):
+    """L = sum(G * combine(Ys, w)) and sum(H * dispatch(x)): central differences in fp64 of the
+    formulas agree with the kernels' gradients (both are linear in each argument)."""
+    T, k, E, D = 9, 2, 4, 24
+    ids = routing(T, k, E, 3, 0.0, 0.1)
+    offsets, order, pos = sort(so, ids, E, 4)
+    rows = order.numel()
+    p, o = pos.view(T, k).long(), order.long()
+    ys, G, x, H = (inputs(r, D, F32, i) for i, r in enumerate((rows, T, T, rows)))
+    w = torch.rand((T, k), device="cuda")
+
+    def combine(ysv, wv):
+        return (torch.where((p >= 0)[..., None], ysv[p.clamp(min=0)], 0.0) * wv[..., None]).sum(1)
+
+    def dispatch(xv):
+        return torch.where((o >= 0)[:, None], xv[o.clamp(min=0) // k], 0.0)
+
+    dys, dw, dx = torch.empty_like(ys), torch.empty((T, k), device="cuda"), torch.empty_like(x)
+    so.sfc_moe_combine_grad(G, ys, order, pos, w, dys, dw)
+    so.sfc_moe_combine(H, pos, dx)
+
+    def differences(f, at, got):
+        for i in torch.randperm(at.numel(), generator=torch.Generator().manual_seed(5))[:24].tolist():
+            step = torch.zeros(at.numel(), dtype=torch.float64, device="cuda")
+            step[i] = 1.0
+            d = (f(at + step.view(at.shape)) - f(at - step.view(at.shape))) / 2
+            assert abs(got.double().view(-1)[i] - d) <= 1e-6 * (f(at.abs() + 1).abs() + abs(d) + 1)
+
+    Gd, Hd = G.double(), H.double()
+    differences(lambda v: (Gd.abs() * 0 + Gd).mul(combine(v, w.double())).sum(), ys.double(), dys)
+    differences(lambda v: Gd.mul(combine(ys.double(), v)).sum(), w.double(), dw)
+    differences(lambda v: Hd.mul(dispatch(v)).sum(), x.double(), dx)
+
+
+def test_a_wide_array_passes_32_bit_offsets(so):
+    T, k, D = 80000, 1, 32768                   # 5.2 GB of bf16
+    perm = torch.randperm(T, device="cuda", dtype=torch.int32)
+    x = torch.zeros((T, D), dtype=BF16, device="cuda")
+    mark = torch.arange(T, device="cuda") % 251 + 1
+    x[:, 0] = mark.to(BF16)
+    x[:, D - 1] = mark.to(BF16)
+    xs = torch.empty((T, D), dtype=BF16, device="cuda")
+    so.sfc_moe_dispatch(x, perm, xs, topk=k)
+    want = x[:, 0][perm.long()]
+    assert torch.equal(xs[:, 0], want) and torch.equal(xs[:, D - 1], want)
+    pos = torch.empty_like(perm)
+    pos[perm.long()] = torch.arange(T, dtype=torch.int32, device="cuda")
+    y = torch.empty((T, D), dtype=BF16, device="cuda")
+    so.sfc_moe_combine(xs, pos, y)
+    assert torch.equal(y[:, 0], x[:, 0]) and torch.equal(y[:, D - 1], x[:, D - 1])
+
+
+# ---- experts' products ---------------------------------------------------------------------------
+
+
+def weights(E, N, K, seed):
+    parts = [operand(N, K, seed + e) for e in range(E)]
+    b = -(-K // 32)
+    q = torch.stack([x[0] for x in parts])
+    s = torch.full((E, N, (b + 3) // 4 * 4), 255, dtype=torch.uint8, device="cuda")[..., :b]
+    s.copy_(torch.stack([x[1] for x in parts]))
+    return q, s, [x[2] for x in parts]
+
+
+PRODUCTS = [
+    # rows of every expert (0: none), N, K
+    ([1], 16, 32), ([0, 0, 3], 100, 96), ([2, 1, 0, 5, 16, 17, 0, 1], 333, 544), ([40, 0, 1, 90], 64, 1024),
+    ([70, 200, 0, 129], 200, 160), ([128, 128, 256], 257, 512), ([0, 0, 0], 70, 64), ([1000, 3, 0, 1500], 4100, 288),
+    ([300] * 8, 4096, 160), ([0, 2000, 1], 4096, 1056)]
+
+
+@pytest.mark.parametrize("out", [F32, BF16])
+@pytest.mark.parametrize("counts,N,K", PRODUCTS)
+@pytest.mark.parametrize("spare", [0, 37])
+def test_experts_product(so, counts, N, K, spare, out):
+    E, rows = len(counts), sum(counts) + spare
+    if rows == 0:
+        spare = rows = 5
+    A, As, a = operand(rows, K, 3)
+    B, Bs, b = weights(E, N, K, 50)
+    offsets = torch.tensor(np.cumsum([0] + counts), dtype=torch.int32, device="cuda")
+    C = torch.full((rows, N + 2), 99.0, dtype=out, device="cuda")
+    so.sfc_moe_gemm_mx4_ex(A, As, B, Bs, offsets, C[:, 1:1 + N])
+    assert (C[:, 0] == 99).all() and (C[:, 1 + N:] == 99).all()
+    at = 0
+    for e, n in enumerate(counts):
+        check(C[at:at + n, 1:1 + N], a[at:at + n], b[e], K, True)
+        at += n
+    assert (C[at:, 1:1 + N] == 0).all()
+
+
+@pytest.mark.parametrize("out", [F32, BF16])
+@pytest.mark.parametrize("starts,M,N", [
+    ([0, 32], 16, 16), ([0, 0, 64, 64, 96], 130, 70), ([0, 32, 160, 2048], 200, 300), ([0, 96, 96, 800, 1000], 129, 257),
+    ([0, 4096], 100, 60), ([0, 512, 1024, 3136, 4000], 1030, 2050)])
+def test_weight_gradient(so, starts, M, N, out):
+    rows = starts[-1] + 31
+    Kp = -(-rows // 32) * 32
+    A, As, a = operand(M, Kp, 3)
+    B, Bs, b = operand(N, Kp, 4)
+    E = len(starts) - 1
+    C = torch.full((E, M + 1, N + 2), 99.0, dtype=out, device="cuda")
+    offsets = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    so.sfc_moe_wgrad_mx4_ex(A, As, B, Bs, offsets, C[:, :M, 1:1 + N])
+    assert (C[:, M:] == 99).all() and (C[:, :, 0] == 99).all() and (C[:, :, 1 + N:] == 99).all()
+    for e in range(E):
+        # a segment that ends inside a block takes the whole block
+        lo, hi = starts[e], -(-starts[e + 1] // 32) * 32 if starts[e + 1] > starts[e] else starts[e]
+        check(C[e, :M, 1:1 + N], a[:, lo:hi], b[:, lo:hi], max(hi - lo, 1), True)
+
+
+def test_offsets_outside_the_rows_are_cut(so):
+    A, As, a = operand(100, 64, 1)
+    B, Bs, b = weights(3, 40, 64, 2)
+    C = torch.full((100, 40), 9.0, device="cuda")
+    so.sfc_moe_gemm_mx4_ex(A, As, B, Bs, torch.tensor([0, 60, 1 << 30, 5], dtype=torch.int32, device="cuda"), C)
+    check(C[60:], a[60:], b[1], 64, True)
+
+
+def test_layer_forward_and_gradient(so):
+    """Sorted, cast, multiplied and summed back: a layer of experts against 64 bits, and its
+    gradients against the formulas on the same 4-bit values."""
+    T, k, E, K, N = 200, 2, 6, 160, 224
+    ids = routing(T, k, E, 1, 0.7, 0.05)
+    offsets, order, pos = sort(so, ids, E, 32)
+    rows = order.numel()
+    x, w = inputs(T, K, BF16, 1), torch.rand((T, k), device="cuda")
+    B, Bs, b = weights(E, N, K, 9)
+    xq = so.mx4_empty(rows, K)
+    so.sfc_mx4_quant(x, *xq, order=order, topk=k)
+    ys = torch.empty((rows, N), device="cuda")
+    so.sfc_moe_gemm_mx4_ex(*xq, B, Bs, offsets, ys)
+    y = torch.empty((T, N), device="cuda")
+    so.sfc_moe_combine(ys, pos, y, weights=w)
+    xv = torch.from_numpy(mx4.values(*mx4.quantise(host(x)))).cuda()
+    want, size = torch.zeros((T, N), dtype=torch.float64, device="cuda"), torch.zeros((T, N), dtype=torch.float64, device="cuda")
+    for t in range(T):
+        for j in range(k):
+            if 0 <= ids[t, j] < E:
+                want[t] += w[t, j].double() * (b[ids[t, j]] @ xv[t])
+                size[t] += w[t, j].double() * (b[ids[t, j]].abs() @ xv[t].abs())
+    assert ((y.double() - want).abs() <= (K + k + 2) * 2.0 ** -23 * size).all()
+    dy = inputs(T, N, F32, 7)
+    dys, dw = torch.empty_like(ys), torch.empty((T, k), device="cuda")
+    so.sfc_moe_combine_grad(dy, ys, order, pos, w, dys, dw)
+    dq, dt, xt = so.mx4_empty(rows, N), so.mx4_empty(N, rows), so.mx4_empty(K, rows)
+    so.sfc_mx4_quant(dys, *dq, *dt)
+    so.sfc_mx4_quant(x, None, None, *xt, order=order, topk=k)
+    dwe = torch.empty((E, N, K), device="cuda")
+    so.sfc_moe_wgrad_mx4_ex(*dt, *xt, offsets, dwe)
+    at = offsets.tolist()
+    xs = np.where((order.cpu().numpy() >= 0)[:, None], host(x)[np.maximum(order.cpu().numpy(), 0) // k], 0.0)
+    dv = torch.from_numpy(mx4.values(*mx4.quantise(host(dys).T))).cuda()
+    xvt = torch.from_numpy(mx4.values(*mx4.quantise(xs.T))).cuda()
+    for e in range(E):
+        check(dwe[e], dv[:, at[e]:at[e + 1]], xvt[:, at[e]:at[e + 1]], rows, False)
