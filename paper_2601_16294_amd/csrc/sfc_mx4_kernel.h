@@ -7,15 +7,19 @@
 // 32 rows with one scale byte per row and block, and accumulates in fp32.
 //
 // Mapping.  A workgroup of 4 waves (2 x 2) computes a BM x BN block.  K runs in stages of
-// 128 values: 64 bytes of codes per row, in a ring of four LDS slots that buffer loads
-// fill straight from memory, and 16 bytes of scales per row for four stages, in a ring of
-// two.  During stage t the loads of stage t+4 go out; one barrier per stage, between its
-// two MFMA steps, where all waves have read stage t and the loads of stage t+1 have
-// landed: behind it slot t is free and slot t+1 may be read.
-//   * lane l of a fragment holds row l%32 and, in step s, block 2*(l/32) + s of the stage:
-//     its two scale bytes lie side by side, and the MFMA selects one by an immediate;
-//   * 16-byte chunk c of row r is stored at chunk c ^ ((r >> 2) & 3): 16 consecutive rows
-//     read at one logical chunk touch the 16 16-byte bank groups;
+// 256 values: 128 bytes of codes per row, one cache line (a load of half a line brings the
+// whole line out of L2: with stages of 128 values the kernel drew twice its bytes and took
+// 0.69 us a 128 values and CU against 0.54 with the loads left out).  LDS holds two stages.
+// During stage t the rows of stage t+1 go from registers, loaded a stage ago, into the
+// slot that stage t-1 left, and the same registers receive stage t+2.  A stage is four MFMA
+// steps of 64 values; one barrier per stage, before its last step: by then every wave has
+// read stage t and written its part of t+1.
+//   * lane l of a fragment holds row l%32 and, in step s, block 4*(l/32) + s of the stage:
+//     its four scale bytes are one dword, and the MFMA selects the byte by an immediate;
+//   * 16-byte chunk c of row r is stored at chunk c ^ ((r >> 1) & 7): the 16 rows that a part
+//     of a wave reads at one logical chunk touch the 16 16-byte bank groups;
+//   * scales come straight from memory into LDS, 32 bytes of a row at a time (four stages),
+//     into a ring of two slots, four stages ahead;
 //   * rows past M or N and blocks outside the range of K are loaded as zeros (lanes past
 //     the descriptor's range); scale bytes outside the range are masked to code 0, because
 //     a NaN scale makes even zeros NaN;
@@ -28,40 +32,43 @@
 namespace sfc {
 
 typedef __attribute__((address_space(3))) const i32x4 lds_ci32x4;
-typedef __attribute__((address_space(3))) const uint16_t lds_cu16;
-
-constexpr int kMxStage = 128;                   // values of K in a stage
-constexpr int kMxRing = 4;                      // stages in LDS
-constexpr int kMxScaleStages = 4;               // stages that one load of scales covers
+typedef __attribute__((address_space(3))) i32x4 lds_i32x4;
+typedef __attribute__((address_space(3))) const int lds_cint;
 
 template <int BM, int BN>
 struct MxTile {
   static constexpr int THREADS = 256;
   static constexpr int WTM = BM / 2, WTN = BN / 2;            // a wave's part
   static constexpr int FM = WTM / 32, FN = WTN / 32;          // fragments of 32 rows
-  static constexpr int A_BYTES = BM * 64, B_BYTES = BN * 64, SLOT = A_BYTES + B_BYTES;
-  static constexpr int AL = A_BYTES / 1024 / 4, BL = B_BYTES / 1024 / 4;   // loads per wave and stage
-  static constexpr int SA_OFF = kMxRing * SLOT;               // scale ring
-  static constexpr int S_SLOT = (BM + BN) * 16;
+  static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, SLOT = A_BYTES + B_BYTES;
+  static constexpr int L = BM / 32;                           // loads of 8 rows per wave, operand and stage
+  // scales: two slots of four stages, for every 32 rows [two stages][row][16 bytes]
+  static constexpr int SA_OFF = 2 * SLOT;
+  static constexpr int S_SLOT = (BM + BN) * 32;
+  static constexpr int SC = (BM + BN) / 128;                  // loads of scales per wave (32 rows each)
   static constexpr int LDS = SA_OFF + 2 * S_SLOT;
-  static constexpr int LOADS = AL + BL;
   static constexpr int PER_CU = BM == 256 ? 1 : 2;            // workgroups
   // epilogue: a wave's strip of 32 rows, fp32, rows 16 bytes apart from a multiple of 256
   static constexpr int RS = WTN * 4 + 16;
+  static_assert(BM == BN, "square blocks");
   static_assert(4 * 32 * RS <= SA_OFF, "strips fit the ring");
-  static_assert(PER_CU * (LDS + 4 * (kMaxExperts + 2)) <= 160 * 1024, "LDS of one CU");
+  static_assert(PER_CU * LDS <= 160 * 1024, "LDS of one CU");
 };
 
-__device__ __forceinline__ void mx_dma16(const i32x4& rsrc, uint32_t lds, int voffset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :: "s"(lds), "v"(voffset), "s"(rsrc) : "memory");
+// 16 bytes per lane from descriptor base + voffset + koffset to LDS lds + 16 * lane, behind the
+// compiler's back: whoever reads them waits for them (it counts the other loads, which
+// return in order).
+__device__ __forceinline__ void mx_dma16(const i32x4& rsrc, uint32_t lds, int voffset, int koffset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :: "s"(lds), "v"(voffset), "s"(rsrc), "s"(koffset) : "memory");
 }
-
-// One operand's rows of a block: where its loads start.
-struct MxSide {
-  uint64_t codes, scales;      // first byte of the stage / of the scale chunk to load next
-  uint32_t scale_range;        // bytes from `scales` to the end of the last row's scales
-};
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_rsrc(const uint8_t* base, uint32_t range) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, (int)range, 0x00020000);
+}
+// 16 bytes at base + voffset + koffset; zeros past the descriptor's range.
+__device__ __forceinline__ i32x4 mx_load16(__amdgpu_buffer_rsrc_t rsrc, int voffset, int koffset) {
+  return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, voffset, koffset, 0));
+}
 
 __device__ __forceinline__ i32x8 mx_wide(const i32x4& v) {
   return __builtin_shufflevector(v, v, 0, 1, 2, 3, -1, -1, -1, -1);
@@ -147,166 +154,181 @@ __device__ __forceinline__ void mx_block(const Mx4GemmParams& p, const MxTask& t
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  const int stages = (t.hi + 3) >> 2;
-  // loads: lane i of a load takes row i/4 of 16 rows, and the logical chunk that lies at i%4
-  const int chunk = (lane & 3) ^ ((lane >> 4) & 3);
-  int av[T::AL], bv[T::BL], sav, sbv;
+  constexpr int L = T::L, NF = T::FM + T::FN, NM = T::FM * T::FN;
+  const int stages = (t.hi + 7) >> 3;
+  // Loads: lane i of a load takes row i/8 of 8 rows, chunk i%8; wave w the rows w*BM/4 ..
+  const int chunk = lane & 7;
+  int av[L], bv[L];
 #pragma unroll
-  for (int i = 0; i < T::AL; ++i) {
-    const int r = (wave * T::AL + i) * 16 + (lane >> 2);
+  for (int i = 0; i < L; ++i) {
+    const int r = (wave * L + i) * 8 + (lane >> 3);
     av[i] = r < t.m_valid ? (int)(r * p.lda) + 16 * chunk : kOobOffset;
-  }
-#pragma unroll
-  for (int i = 0; i < T::BL; ++i) {
-    const int r = (wave * T::BL + i) * 16 + (lane >> 2);
     bv[i] = r < t.n_valid ? (int)(r * p.ldb) + 16 * chunk : kOobOffset;
   }
-  // scales: 64 rows a load; blocks of fewer than 256 rows are loaded by two waves, alike
-  const int sa_seg = wave & (BM / 64 - 1), sb_seg = wave & (BN / 64 - 1);
-  {
-    const int ra = sa_seg * 64 + lane, rb = sb_seg * 64 + lane;
-    sav = ra < t.m_valid ? (int)(ra * p.ldas) : kOobOffset;
-    sbv = rb < t.n_valid ? (int)(rb * p.ldbs) : kOobOffset;
-  }
-  uint64_t a_at = reinterpret_cast<uint64_t>(p.A) + (uint64_t)(t.a_row * p.lda + t.block0 * 16);
-  uint64_t b_at = reinterpret_cast<uint64_t>(t.B) + (uint64_t)(t.b_row * p.ldb + t.block0 * 16);
-  uint64_t sa_at = reinterpret_cast<uint64_t>(p.As) + (uint64_t)(t.a_row * p.ldas + t.block0);
-  uint64_t sb_at = reinterpret_cast<uint64_t>(t.Bs) + (uint64_t)(t.b_row * p.ldbs + t.block0);
-  // bytes to the end of the last row's scales (whole dwords): nothing past it is read
+  const __amdgpu_buffer_rsrc_t qa = mx_rsrc(p.A + t.a_row * p.lda + t.block0 * 16, kOobOffset);
+  const __amdgpu_buffer_rsrc_t qb = mx_rsrc(t.B + t.b_row * p.ldb + t.block0 * 16, kOobOffset);
+  // stages from here on hold blocks past the range: the lanes that would load them turn into
+  // lanes that read zeros, for good
+  const int full_stages = t.hi >> 3;
+  auto cut_lanes = [&](int stage) {
+    const bool out = 8 * stage + chunk >= t.hi;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      av[i] = out ? kOobOffset : av[i];
+      bv[i] = out ? kOobOffset : bv[i];
+    }
+  };
+  // Scales: a load takes 32 bytes of 32 rows (of A's, then B's).  They end with the last
+  // row's (whole dwords): nothing past it is read.
   const int s_row_end = (t.hi + 3) & ~3;
-  int sa_range = t.hi > 0 ? (int)((t.m_valid - 1) * p.ldas) + s_row_end : 0;
-  int sb_range = t.hi > 0 ? (int)((t.n_valid - 1) * p.ldbs) + s_row_end : 0;
-  int load_stage = 0;
-
-  // codes of the next stage into slot `slot`, one of LOADS pieces at a time
-  i32x4 ra, rb;
-  int lane_in = 0;
-  auto stage_begin = [&]() {
-    ra = make_rsrc_addr(a_at, (uint32_t)kOobOffset);
-    rb = make_rsrc_addr(b_at, (uint32_t)kOobOffset);
-    const int blk = 4 * load_stage + chunk;
-    lane_in = blk >= t.lo && blk < t.hi;
-  };
-  auto stage_piece = [&](uint32_t slot_at, int k) {
-    const uint32_t at = lds0 + slot_at;
-    if (k < T::AL) mx_dma16(ra, at + (uint32_t)((wave * T::AL + k) * 1024), lane_in ? av[k] : kOobOffset);
-    else mx_dma16(rb, at + (uint32_t)(T::A_BYTES + (wave * T::BL + k - T::AL) * 1024),
-                  lane_in ? bv[k - T::AL] : kOobOffset);
-  };
-  auto stage_end = [&]() {
-    a_at += 64;
-    b_at += 64;
-    ++load_stage;
-  };
-  // scales of four stages into scale slot `slot`
-  auto scales_load = [&](int slot) {
-    const i32x4 qa = make_rsrc_addr(sa_at, sa_range > 0 ? (uint32_t)sa_range : 0u);
-    const i32x4 qb = make_rsrc_addr(sb_at, sb_range > 0 ? (uint32_t)sb_range : 0u);
-    const uint32_t at = lds0 + (uint32_t)(T::SA_OFF + slot * T::S_SLOT);
-    mx_dma16(qa, at + (uint32_t)(sa_seg * 1024), sav);
-    mx_dma16(qb, at + (uint32_t)(BM * 16 + sb_seg * 1024), sbv);
-    sa_at += 16;
-    sb_at += 16;
-    sa_range -= 16;
-    sb_range -= 16;
+  const i32x4 qas = make_rsrc_addr(reinterpret_cast<uint64_t>(p.As) + (uint64_t)(t.a_row * p.ldas + t.block0),
+                                   t.hi > 0 ? (uint32_t)((t.m_valid - 1) * p.ldas + s_row_end) : 0u);
+  const i32x4 qbs = make_rsrc_addr(reinterpret_cast<uint64_t>(t.Bs) + (uint64_t)(t.b_row * p.ldbs + t.block0),
+                                   t.hi > 0 ? (uint32_t)((t.n_valid - 1) * p.ldbs + s_row_end) : 0u);
+  int sv[T::SC];
+#pragma unroll
+  for (int k = 0; k < T::SC; ++k) {
+    const bool of_a = (wave * T::SC + k) * 32 < BM;
+    const int r = (wave * T::SC + k) * 32 - (of_a ? 0 : BM) + (lane & 31);
+    sv[k] = r < (of_a ? t.m_valid : t.n_valid) ? (int)(r * (of_a ? p.ldas : p.ldbs)) + 16 * (lane >> 5) : kOobOffset;
+  }
+  auto load_scales = [&](int group) {        // four stages of scales, number `group`, into their slot
+    const uint32_t at = lds0 + (uint32_t)(T::SA_OFF + (group & 1) * T::S_SLOT + wave * T::SC * 1024);
+#pragma unroll
+    for (int k = 0; k < T::SC; ++k) {
+      const bool of_a = (wave * T::SC + k) * 32 < BM;
+      mx_dma16(of_a ? qas : qbs, at + (uint32_t)(k * 1024), sv[k], 32 * group);
+    }
   };
 
-  // fragment reads
+  // LDS addresses: writes of even loads (odd ones: ^ 64) and fragment reads of step 0 (step s: ^ 16 s)
+  const uint32_t w0 = lds0 + (uint32_t)(wave * L * 1024 + (lane >> 3) * 128 + ((chunk ^ (lane >> 4)) << 4));
   const int h = lane >> 5, r32 = lane & 31;
-  const uint32_t frag = (uint32_t)(r32 * 64 + (((2 * h) ^ ((r32 >> 2) & 3)) << 4));
-  const uint32_t a_frag = lds0 + (uint32_t)(wm * T::WTM * 64) + frag;
-  const uint32_t b_frag = lds0 + (uint32_t)(T::A_BYTES + wn * T::WTN * 64) + frag;
-  const uint32_t a_sc = lds0 + (uint32_t)(T::SA_OFF + (wm * T::WTM + r32) * 16 + 2 * h);
-  const uint32_t b_sc = lds0 + (uint32_t)(T::SA_OFF + BM * 16 + (wn * T::WTN + r32) * 16 + 2 * h);
+  const uint32_t frag = (uint32_t)(r32 * 128 + (((4 * h) ^ ((r32 >> 1) & 7)) << 4));
+  const uint32_t a_frag = lds0 + (uint32_t)(wm * T::WTM * 128) + frag, b_frag = lds0 + (uint32_t)(wn * T::WTN * 128) + frag;
+  const uint32_t a_sc = lds0 + (uint32_t)(T::SA_OFF + wm * T::WTM * 32 + r32 * 16 + 4 * h);
+  const uint32_t b_sc = lds0 + (uint32_t)(T::SA_OFF + (BM + wn * T::WTN) * 32 + r32 * 16 + 4 * h);
+  i32x4 ga[L], gb[L];
   i32x4 fa[2][T::FM], fb[2][T::FN];
-  int sa[2][T::FM], sb[2][T::FN];
-  // (step 1's chunk is step 0's ^ 1)
-  auto read_frag = [&](uint32_t slot_at, int step, int k) {
-    const uint32_t flip = step ? 16u : 0u;
-    if (k < T::FM) fa[step][k] = *(lds_ci32x4*)(uintptr_t)((a_frag ^ flip) + slot_at + (uint32_t)(k * 2048));
-    else fb[step][k - T::FM] = *(lds_ci32x4*)(uintptr_t)((b_frag ^ flip) + slot_at + (uint32_t)((k - T::FM) * 2048));
+  int sa[2][T::FM], sb[2][T::FN];              // the stage's scales, and the next one's
+  auto write_rows = [&](uint32_t slot, int k) {      // load k of 2 L: A's, then B's
+    const uint32_t at = ((k & 1) ? w0 ^ 64u : w0) + slot + (uint32_t)((k < L ? k : k - L) * 1024);
+    if (k < L) *(lds_i32x4*)(uintptr_t)at = ga[k];
+    else *(lds_i32x4*)(uintptr_t)(at + T::A_BYTES) = gb[k - L];
   };
-  auto read_scale = [&](uint32_t off, int mask, int k) {
-    if (k < T::FM) sa[1][k] = *(lds_cu16*)(uintptr_t)(a_sc + off + (uint32_t)(k * 512)) & mask;
-    else sb[1][k - T::FM] = *(lds_cu16*)(uintptr_t)(b_sc + off + (uint32_t)((k - T::FM) * 512)) & mask;
+  auto load_rows = [&](int koff, int k) {
+    if (k < L) ga[k] = mx_load16(qa, av[k], koff);
+    else gb[k - L] = mx_load16(qb, bv[k - L], koff);
   };
-  // which of this lane's two scale bytes of stage st count
-  auto scale_mask = [&](int st) {
-    const int b0 = 4 * st + 2 * h;
-    return (b0 >= t.lo && b0 < t.hi ? 0xFF : 0) | (b0 + 1 >= t.lo && b0 + 1 < t.hi ? 0xFF00 : 0);
+  auto read_frag = [&](uint32_t slot, int step, int set, int k) {
+    if (k < T::FM) fa[set][k] = *(lds_ci32x4*)(uintptr_t)((a_frag ^ (uint32_t)(16 * step)) + slot + (uint32_t)(k * 4096));
+    else fb[set][k - T::FM] = *(lds_ci32x4*)(uintptr_t)((b_frag ^ (uint32_t)(16 * step)) + slot +
+                                                        (uint32_t)(T::A_BYTES + (k - T::FM) * 4096));
   };
-  constexpr int NF = T::FM + T::FN, NM = T::FM * T::FN;
+  auto read_scale = [&](uint32_t off, int k) {
+    if (k < T::FM) sa[1][k] = *(lds_cint*)(uintptr_t)(a_sc + off + (uint32_t)(k * 1024));
+    else sb[1][k - T::FM] = *(lds_cint*)(uintptr_t)(b_sc + off + (uint32_t)((k - T::FM) * 1024));
+  };
+  // stages that hold blocks outside the range: their scale bytes there become 0
+  const int first_cut = t.lo > 0 ? 0 : -1, last_cut = (t.hi & 7) ? stages - 1 : -1;
+  auto cut_scales = [&](int st) {
+    int mask = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int b = 8 * st + 4 * h + k;
+      mask |= b >= t.lo && b < t.hi ? 0xFF << (8 * k) : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < T::FM; ++k) sa[1][k] &= mask;
+#pragma unroll
+    for (int k = 0; k < T::FN; ++k) sb[1][k] &= mask;
+  };
 
-  // prologue: stages 0 .. 3
-  scales_load(0);
-#pragma unroll
-  for (int s = 0; s < kMxRing; ++s) {
-    stage_begin();
-#pragma unroll
-    for (int k = 0; k < T::LOADS; ++k) stage_piece((uint32_t)(s * T::SLOT), k);
-    stage_end();
-  }
-  wait_vmem_at_most<3 * T::LOADS>();
-  __builtin_amdgcn_s_barrier();
+  // prologue: stage 0 and its scales into LDS, stage 1 into registers
+  load_scales(0);
+  if (0 >= full_stages) cut_lanes(0);
   {
-    const int mask = scale_mask(0);
+    const bool in = chunk >= t.lo;
 #pragma unroll
-    for (int k = 0; k < NF; ++k) {
-      read_frag(0, 0, k);
-      read_scale(0, mask, k);
-    }
+    for (int k = 0; k < L; ++k) ga[k] = mx_load16(qa, in ? av[k] : kOobOffset, 0);
+#pragma unroll
+    for (int k = 0; k < L; ++k) gb[k] = mx_load16(qb, in ? bv[k] : kOobOffset, 0);
+  }
+  if (1 >= full_stages) cut_lanes(1);
+#pragma unroll
+  for (int k = 0; k < 2 * L; ++k) {
+    write_rows(0, k);
+    load_rows(128, k);
+  }
+  wait_vmem_at_most<2 * L>();                  // the scales
+  wait_lds_all();
+  __builtin_amdgcn_s_barrier();
+#pragma unroll
+  for (int k = 0; k < NF; ++k) {
+    read_frag(0, 0, 0, k);
+    read_scale(0, k);
   }
 
+  // What goes beside which MFMA: fragment reads on the first MFMAs of a step, the 2 L moves of rows
+  // (into LDS, and the next load into the same registers) evenly over steps 0 .. 2.
+  constexpr auto read_at = [](int k) { return NM >= 16 ? k + k / 2 : k * NM / NF; };
+  constexpr auto move_at = [](int k) { return (k * 3 * NM) / (2 * L) + (NM >= 16 ? 2 : 0); };
+  uint32_t slot = 0;                           // LDS offset of the stage's slot
   for (int st = 0; st < stages; ++st) {
-    const uint32_t slot_at = (uint32_t)((st & 3) * T::SLOT), next_at = (uint32_t)(((st + 1) & 3) * T::SLOT);
-    const uint32_t scale_at = (uint32_t)((((st + 1) >> 2) & 1) * T::S_SLOT + 4 * ((st + 1) & 3));
+    uint32_t next = (uint32_t)T::SLOT - slot;
+    pin_scalar(next);                          // (one value: the LDS offsets stay in the instructions)
+    const int koff = 128 * (st + 2);
+    const uint32_t scale_at = (uint32_t)((((st + 1) >> 2) & 1) * T::S_SLOT + (((st + 1) >> 1) & 1) * 512 + 8 * ((st + 1) & 1));
+    // (no branch between the steps: the compiler would move MFMAs down past it)
+    if (st == first_cut || st == last_cut) cut_scales(st);
+    if (st + 2 >= full_stages) cut_lanes(st + 2);
+    // (their slot's last reader was stage st - 2)
+    if ((st & 3) == 0) load_scales((st >> 2) + 1);
+    sb[0][0] = sb[1][0];
+    sa[0][0] = sa[1][0];
 #pragma unroll
-    for (int k = 0; k < T::FM; ++k) sa[0][k] = sa[1][k];
+    for (int s = 0; s < 4; ++s) {
 #pragma unroll
-    for (int k = 0; k < T::FN; ++k) sb[0][k] = sb[1][k];
-    // step 0, beside it the fragments of step 1
-#pragma unroll
-    for (int m = 0; m < NM; ++m) {
-      const int i = m / T::FN, j = m % T::FN;
-      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx_wide(fb[0][j]), mx_wide(fa[0][i]), acc[i][j], 4, 4, 0,
-                                                                  sb[0][j], 0, sa[0][i]);
-      constexpr int RP = (NF + NM - 1) / NM;           // reads beside one MFMA
-#pragma unroll
-      for (int k = m * RP; k < (m + 1) * RP; ++k)
-        if (k < NF) read_frag(slot_at, 1, k);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    wait_lds_all();
-    // younger loads: stages st+2 and st+3 (and, at times, the scales that came with one)
-    wait_vmem_at_most<2 * T::LOADS>();
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-    const int mask = scale_mask(st + 1);
-    if ((st & 3) == 0) scales_load(((st >> 2) & 1) ^ 1);
-    stage_begin();
-    // step 1, beside it the next stage's first fragments and scales, and the loads of stage st + 4
-#pragma unroll
-    for (int m = 0; m < NM; ++m) {
-      const int i = m / T::FN, j = m % T::FN;
-      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx_wide(fb[1][j]), mx_wide(fa[1][i]), acc[i][j], 4, 4, 1,
-                                                                  sb[0][j], 1, sa[0][i]);
-      constexpr int RP = (NF + NM - 1) / NM;
-#pragma unroll
-      for (int k = m * RP; k < (m + 1) * RP; ++k)
-        if (k < NF) {
-          read_frag(next_at, 0, k);
-          read_scale(scale_at, mask, k);
+      for (int m = 0; m < NM; ++m) {
+        const int i = m / T::FN, j = m % T::FN;
+        const i32x8 xb = mx_wide(fb[s & 1][j]), xa = mx_wide(fa[s & 1][i]);
+        if (s == 0) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xb, xa, acc[i][j], 4, 4, 0, sb[0][j], 0, sa[0][i]);
+        if (s == 1) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xb, xa, acc[i][j], 4, 4, 1, sb[0][j], 1, sa[0][i]);
+        if (s == 2) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xb, xa, acc[i][j], 4, 4, 2, sb[0][j], 2, sa[0][i]);
+        if (s == 3) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xb, xa, acc[i][j], 4, 4, 3, sb[0][j], 3, sa[0][i]);
+        if (s == 0) {
+          if (m + 1 < T::FN) sb[0][m + 1] = sb[1][m + 1];
+          if ((m + 1) % T::FN == 0 && m + 1 < NM) sa[0][(m + 1) / T::FN] = sa[1][(m + 1) / T::FN];
         }
-      constexpr int LP = (T::LOADS + NM - 1) / NM;
 #pragma unroll
-      for (int k = m * LP; k < (m + 1) * LP; ++k)
-        if (k < T::LOADS) stage_piece(slot_at, k);
-      __builtin_amdgcn_sched_barrier(0);
+        for (int k = 0; k < NF; ++k)
+          if (read_at(k) == m) {
+            if (s < 3) {
+              read_frag(slot, s + 1, (s + 1) & 1, k);
+            } else {
+              read_frag(next, 0, 0, k);
+              read_scale(scale_at, k);
+            }
+          }
+#pragma unroll
+        for (int k = 0; k < 2 * L; ++k)
+          if (move_at(k) == s * NM + m) {
+            write_rows(next, k);
+            load_rows(koff, k);
+          }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (s == 2) {
+        // this stage's 2 L loads are younger than all scales
+        wait_vmem_at_most<2 * L>();
+        wait_lds_all();
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
-    stage_end();
+    slot = next;
   }
-  wait_vmem_at_most<0>();
-  __syncthreads();                // every wave is done with the ring, and no load is in flight
+  __syncthreads();                // every wave is done with the ring
   const bool full = t.m_valid == BM && t.n_valid == BN;
   if (full) mx_store<BM, BN, OB, true>(p, t, acc, lds0, wave, lane);
   else mx_store<BM, BN, OB, false>(p, t, acc, lds0, wave, lane);
@@ -330,20 +352,23 @@ __global__ __launch_bounds__(256, (MxTile<BM, BN>::PER_CU)) void mx4_gemm_kernel
   t.C = reinterpret_cast<char*>(p.C);
 
   if constexpr (MODE == kMxRows) {
-    // blocks of rows before each expert
-    __shared__ int before[kMaxExperts + 1];
-    __shared__ int used;             // rows up to the end of the last segment
-    if (wave == 0) {
-      int carry = 0, end = 0;
+    // rows lo .. hi-1 of expert e
+    auto segment = [&](int e, int64_t& lo, int64_t& hi) {
+      lo = p.offsets[e];
+      hi = p.offsets[e + 1];
+      lo = lo < 0 ? 0 : lo > p.M ? p.M : lo;
+      hi = hi < lo ? lo : hi > p.M ? p.M : hi;
+    };
+    // the expert that holds block of rows `mt` (counted over all experts): -1 if there are
+    // fewer; the blocks before it and its own
+    auto find = [&](int mt, int& first, int& gm) {
+      int carry = 0;
       for (int e0 = 0; e0 < p.experts; e0 += 64) {
-        const int e = e0 + lane;
         int n = 0;
-        if (e < p.experts) {
-          int64_t lo = p.offsets[e], hi = p.offsets[e + 1];
-          lo = lo < 0 ? 0 : lo > p.M ? p.M : lo;
-          hi = hi < lo ? lo : hi > p.M ? p.M : hi;
+        if (e0 + lane < p.experts) {
+          int64_t lo, hi;
+          segment(e0 + lane, lo, hi);
           n = (int)((hi - lo + BM - 1) / BM);
-          end = hi > end ? (int)hi : end;
         }
         int sum = n;
 #pragma unroll
@@ -351,38 +376,24 @@ __global__ __launch_bounds__(256, (MxTile<BM, BN>::PER_CU)) void mx4_gemm_kernel
           const int up = __shfl_up(sum, d);
           sum += lane >= d ? up : 0;
         }
-        if (e < p.experts) before[e] = carry + sum - n;
-        carry += __shfl(sum, 63);
+        const uint64_t past = __ballot(carry + sum > mt);
+        if (past) {
+          const int l = __ffsll((unsigned long long)past) - 1;
+          gm = __builtin_amdgcn_readfirstlane(__shfl(n, l));
+          first = __builtin_amdgcn_readfirstlane(carry + __shfl(sum, l)) - gm;
+          return e0 + l;
+        }
+        carry += __builtin_amdgcn_readfirstlane(__shfl(sum, 63));
       }
-#pragma unroll
-      for (int d = 32; d >= 1; d >>= 1) {
-        const int other = __shfl_xor(end, d);
-        end = other > end ? other : end;
-      }
-      if (lane == 0) {
-        before[p.experts] = carry;
-        used = end;
-      }
-    }
-    __syncthreads();
-    const int64_t total = (int64_t)before[p.experts] * p.gn;
+      return -1;
+    };
     const int blocks = (int)(p.K >> 5);
-    for (int64_t task = rank; task < total; task += P) {
-      // the expert whose blocks hold this one: the last whose start is not past it
-      const int mt = (int)(task / p.gn);
-      int e = 0;
-      for (int e0 = 0; e0 < p.experts; e0 += 64) {
-        const bool le = e0 + lane < p.experts && before[e0 + lane] <= mt;
-        const uint64_t m = __ballot(le);
-        if (m == 0) break;
-        e = e0 + 63 - __clzll((long long)m);
-      }
-      e = __builtin_amdgcn_readfirstlane(e);
-      const int first = __builtin_amdgcn_readfirstlane(before[e]);
-      const int gm = __builtin_amdgcn_readfirstlane(before[e + 1]) - first;
-      int64_t lo = p.offsets[e], hi = p.offsets[e + 1];
-      lo = lo < 0 ? 0 : lo > p.M ? p.M : lo;
-      hi = hi < lo ? lo : hi > p.M ? p.M : hi;
+    for (int64_t task = rank;; task += P) {
+      int first = 0, gm = 0;
+      const int e = __builtin_amdgcn_readfirstlane(find((int)(task / p.gn), first, gm));
+      if (e < 0) break;
+      int64_t lo, hi;
+      segment(e, lo, hi);
       const int64_t local = task - (int64_t)first * p.gn;
       const int super = (int)(local / (8 * (int64_t)p.gn));
       const int height = gm - 8 * super < 8 ? gm - 8 * super : 8;
@@ -400,7 +411,18 @@ __global__ __launch_bounds__(256, (MxTile<BM, BN>::PER_CU)) void mx4_gemm_kernel
       t.Bs = p.Bs + (int64_t)e * p.stride_bs;
       mx_block<BM, BN, OB>(p, t, lds0, wave, lane);
     }
-    // rows of no expert
+    // rows of no expert: behind the last segment
+    int used = 0;
+    for (int e = lane; e < p.experts; e += 64) {
+      int64_t lo, hi;
+      segment(e, lo, hi);
+      used = hi > used ? (int)hi : used;
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) {
+      const int other = __shfl_xor(used, d);
+      used = other > used ? other : used;
+    }
     for (int64_t r = (int64_t)used + blockIdx.x; r < p.M; r += P)
       for (int64_t c = tid; c < p.N; c += 256) {
         if constexpr (OB) reinterpret_cast<uint16_t*>(p.C)[r * p.ldc + c] = 0;
