@@ -150,78 +150,82 @@ hipError_t launch_moe_sort(const MoeSortParams& p, hipStream_t stream) {
 }
 
 // ---- dispatch ------------------------------------------------------------------------------
-template <bool BF16>
+template <bool BF16, bool PAST>
 __global__ __launch_bounds__(256) void moe_dispatch_kernel(MoeRowsParams p, RowShape sh) {
-  const int tx = 1 << sh.tx_log2;
-  const int64_t rb = blockIdx.x / sh.splits;
-  const int split = (int)(blockIdx.x - rb * sh.splits);
-  const int64_t row = rb * (256 >> sh.tx_log2) + (threadIdx.x >> sh.tx_log2);
-  if (row >= p.rows) return;
-  const int64_t chunks = (p.cols + 7) >> 3, first = (int64_t)split * sh.per;
-  const int64_t last = first + sh.per < chunks ? first + sh.per : chunks;
-  const int32_t slot = p.order[row];
+  const RowPlace at = row_place(sh, (p.cols + 7) >> 3);
+  if (at.row >= p.rows) return;
+  const int32_t slot = p.order[at.row];
   const int64_t token = slot < 0 ? -1 : (int64_t)((uint32_t)slot / (uint32_t)p.topk);
   const bool valid = token >= 0 && token < p.tokens;
   const float w = valid && p.weights ? p.weights[slot] : 1.0f;
   const char* x = reinterpret_cast<const char*>(p.X) + (valid ? token : 0) * p.ldx * (BF16 ? 2 : 4);
-  char* y = reinterpret_cast<char*>(p.Y) + row * p.ldy * (BF16 ? 2 : 4);
-  for (int64_t c = first + (threadIdx.x & (tx - 1)); c < last; c += tx) {
-    Raw8<BF16> r = valid ? load8<BF16>(x, c * 8, p.cols) : zero8<BF16>();
-    if (p.weights) {
-      float f[8];
-      to_float<BF16>(r, f);
+  char* y = reinterpret_cast<char*>(p.Y) + at.row * p.ldy * (BF16 ? 2 : 4);
+  constexpr int U = 4;
+  Raw8<BF16> r[U];
+  row_loop<U>(
+      at, [&](int u, int64_t c) { r[u] = valid ? load8<BF16>(x, c * 8, p.cols) : zero8<BF16>(); },
+      [&](int u, int64_t c) {
+        if (p.weights) {
+          float f[8];
+          to_float<BF16>(r[u], f);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] *= w;
-      r = from_float<BF16>(f);
-    }
-    store8<BF16>(y, c * 8, p.cols, r);
-  }
+          for (int i = 0; i < 8; ++i) f[i] *= w;
+          r[u] = from_float<BF16>(f);
+        }
+        store8<BF16, PAST>(y, c * 8, p.cols, r[u]);
+      });
 }
 
 // ---- combine -------------------------------------------------------------------------------
-template <bool BF16>
+// Two choices at a time, two chunks of each: four loads in flight.
+template <bool BF16, bool PAST>
 __global__ __launch_bounds__(256) void moe_combine_kernel(MoeRowsParams p, RowShape sh) {
-  const int tx = 1 << sh.tx_log2;
-  const int64_t rb = blockIdx.x / sh.splits;
-  const int split = (int)(blockIdx.x - rb * sh.splits);
-  const int64_t t = rb * (256 >> sh.tx_log2) + (threadIdx.x >> sh.tx_log2);
-  if (t >= p.tokens) return;
-  const int64_t chunks = (p.cols + 7) >> 3, first = (int64_t)split * sh.per;
-  const int64_t last = first + sh.per < chunks ? first + sh.per : chunks;
+  const RowPlace at = row_place(sh, (p.cols + 7) >> 3);
+  if (at.row >= p.tokens) return;
   const char* ys = reinterpret_cast<const char*>(p.X);
-  char* y = reinterpret_cast<char*>(p.Y) + t * p.ldy * (BF16 ? 2 : 4);
-  const int32_t* pos = p.pos + t * p.topk;
-  for (int64_t c = first + (threadIdx.x & (tx - 1)); c < last; c += tx) {
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    // four rows in flight
-    for (int j = 0; j < p.topk; j += 4) {
-      Raw8<BF16> r[4];
-      float w[4];
+  char* y = reinterpret_cast<char*>(p.Y) + at.row * p.ldy * (BF16 ? 2 : 4);
+  const int32_t* pos = p.pos + at.row * p.topk;
+  const float* weights = p.weights ? p.weights + at.row * p.topk : nullptr;
+  for (int64_t c = at.first + at.lane_tx; c < at.last; c += 2 * at.tx) {
+    const bool two = c + at.tx < at.last;
+    float sum[2][8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int64_t at = j + u < p.topk ? pos[j + u] : -1;
-        const bool valid = at >= 0 && at < p.rows;
-        r[u] = valid ? load8<BF16>(ys + at * p.ldx * (BF16 ? 2 : 4), c * 8, p.cols) : zero8<BF16>();
-        w[u] = valid && p.weights ? p.weights[t * p.topk + j + u] : valid ? 1.0f : 0.0f;
+    for (int i = 0; i < 8; ++i) sum[0][i] = sum[1][i] = 0.f;
+    for (int j = 0; j < p.topk; j += 2) {
+      Raw8<BF16> r[2][2];
+      float w[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int64_t row = j + u < p.topk ? pos[j + u] : -1;
+        const bool valid = row >= 0 && row < p.rows;
+        const char* src = ys + row * p.ldx * (BF16 ? 2 : 4);
+        r[u][0] = valid ? load8<BF16>(src, c * 8, p.cols) : zero8<BF16>();
+        r[u][1] = valid && two ? load8<BF16>(src, (c + at.tx) * 8, p.cols) : zero8<BF16>();
+        w[u] = valid ? (weights ? weights[j + u] : 1.0f) : 0.0f;
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        float f[8];
-        to_float<BF16>(r[u], f);
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += f[i] * w[u];
-      }
+        for (int k = 0; k < 2; ++k) {
+          float f[8];
+          to_float<BF16>(r[u][k], f);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sum[k][i] += f[i] * w[u];
+        }
     }
-    store8<BF16>(y, c * 8, p.cols, from_float<BF16>(sum));
+    store8<BF16, PAST>(y, c * 8, p.cols, from_float<BF16>(sum[0]));
+    if (two) store8<BF16, PAST>(y, (c + at.tx) * 8, p.cols, from_float<BF16>(sum[1]));
   }
 }
 
 // ---- gradient of combine -------------------------------------------------------------------
-// W waves per token; behind the tokens' workgroups, others clear the rows that no slot has.
-template <bool BF16, int W>
+// W waves per token, two choices at a time (dy is read once for both); behind the tokens'
+// workgroups, others clear the rows that no slot has.
+template <bool BF16, bool PAST, int W>
 __global__ __launch_bounds__(256) void moe_combine_grad_kernel(MoeRowsParams p, int64_t token_groups) {
-  __shared__ float part[4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ float part[2][4];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t chunks = (p.cols + 7) >> 3;
   constexpr int ES = BF16 ? 2 : 4;
   if ((int64_t)blockIdx.x >= token_groups) {
@@ -232,7 +236,7 @@ __global__ __launch_bounds__(256) void moe_combine_grad_kernel(MoeRowsParams p, 
       const int i = __ffsll((unsigned long long)none) - 1;
       none &= none - 1;
       char* y = reinterpret_cast<char*>(p.Y) + (r0 + i) * p.ldy * ES;
-      for (int64_t c = lane; c < chunks; c += 64) store8<BF16>(y, c * 8, p.cols, zero8<BF16>());
+      for (int64_t c = lane; c < chunks; c += 64) store8<BF16, PAST>(y, c * 8, p.cols, zero8<BF16>());
     }
     return;
   }
@@ -240,66 +244,117 @@ __global__ __launch_bounds__(256) void moe_combine_grad_kernel(MoeRowsParams p, 
   const int part_of = W == 4 ? wave : 0;       // this wave's share of the token's chunks
   const bool in = t < p.tokens;
   const char* dy = reinterpret_cast<const char*>(p.X) + (in ? t : 0) * p.ldx * ES;
-  for (int j = 0; j < p.topk; ++j) {
-    const int64_t at = in ? p.pos[t * p.topk + j] : -1;
-    const bool valid = at >= 0 && at < p.rows;
-    float dot = 0.f;
-    if (valid) {
-      const float w = p.weights ? p.weights[t * p.topk + j] : 1.0f;
-      const char* ys = reinterpret_cast<const char*>(p.Ys) + at * p.ldys * ES;
-      char* y = reinterpret_cast<char*>(p.Y) + at * p.ldy * ES;
-#pragma unroll 2
-      for (int64_t c = part_of * 64 + lane; c < chunks; c += 64 * W) {
-        const Raw8<BF16> a = load8<BF16>(dy, c * 8, p.cols), b = load8<BF16>(ys, c * 8, p.cols);
-        float f[8], g[8];
-        to_float<BF16>(a, f);
-        to_float<BF16>(b, g);
+  for (int j = 0; j < p.topk; j += 2) {
+    bool valid[2];
+    float w[2], dot[2] = {0.f, 0.f};
+    const char* ys[2];
+    char* y[2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          dot += f[i] * g[i];
-          f[i] *= w;
+    for (int u = 0; u < 2; ++u) {
+      const int64_t at = in && j + u < p.topk ? p.pos[t * p.topk + j + u] : -1;
+      valid[u] = at >= 0 && at < p.rows;
+      w[u] = valid[u] && p.weights ? p.weights[t * p.topk + j + u] : 1.0f;
+      ys[u] = reinterpret_cast<const char*>(p.Ys) + (valid[u] ? at : 0) * p.ldys * ES;
+      y[u] = reinterpret_cast<char*>(p.Y) + (valid[u] ? at : 0) * p.ldy * ES;
+    }
+    if (valid[0] || valid[1]) {
+      constexpr int U = 2;
+      for (int64_t c = part_of * 64 + lane; c < chunks; c += U * 64 * W) {
+        Raw8<BF16> a[U], b[U][2];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          const int64_t ck = c + k * 64 * W;
+          if (ck < chunks) {
+            a[k] = load8<BF16>(dy, ck * 8, p.cols);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+              if (valid[u]) b[k][u] = load8<BF16>(ys[u], ck * 8, p.cols);
+          }
         }
-        store8<BF16>(y, c * 8, p.cols, from_float<BF16>(f));
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          const int64_t ck = c + k * 64 * W;
+          if (ck < chunks) {
+            float f[8];
+            to_float<BF16>(a[k], f);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+              if (valid[u]) {
+                float g[8], o[8];
+                to_float<BF16>(b[k][u], g);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                  dot[u] += f[i] * g[i];
+                  o[i] = f[i] * w[u];
+                }
+                store8<BF16, PAST>(y[u], ck * 8, p.cols, from_float<BF16>(o));
+              }
+          }
+        }
       }
     }
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) dot += __shfl_xor(dot, d);
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int d = 32; d >= 1; d >>= 1) dot[u] += __shfl_xor(dot[u], d);
     if constexpr (W == 4) {
-      if (lane == 0) part[wave] = dot;
+      if (lane == 0) {
+        part[0][wave] = dot[0];
+        part[1][wave] = dot[1];
+      }
       __syncthreads();
-      dot = (part[0] + part[1]) + (part[2] + part[3]);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) dot[u] = (part[u][0] + part[u][1]) + (part[u][2] + part[u][3]);
       __syncthreads();
     }
-    if (in && lane == 0 && part_of == 0) p.dW[t * p.topk + j] = dot;
+    if (in && lane == 0 && part_of == 0) {
+      p.dW[t * p.topk + j] = dot[0];
+      if (j + 1 < p.topk) p.dW[t * p.topk + j + 1] = dot[1];
+    }
   }
 }
 
 hipError_t launch_moe_dispatch(const MoeRowsParams& p, bool bf16, int num_cus, hipStream_t stream) {
+  const bool past = streams_past_caches(p.rows * p.cols * (bf16 ? 2 : 4));
   const RowShape sh = row_shape(p.rows, (p.cols + 7) / 8, num_cus);
   const dim3 g((unsigned)(sh.row_blocks * sh.splits)), b(256);
-  if (bf16) hipLaunchKernelGGL((moe_dispatch_kernel<true>), g, b, 0, stream, p, sh);
-  else hipLaunchKernelGGL((moe_dispatch_kernel<false>), g, b, 0, stream, p, sh);
+  if (bf16 && past) hipLaunchKernelGGL((moe_dispatch_kernel<true, true>), g, b, 0, stream, p, sh);
+  else if (bf16) hipLaunchKernelGGL((moe_dispatch_kernel<true, false>), g, b, 0, stream, p, sh);
+  else if (past) hipLaunchKernelGGL((moe_dispatch_kernel<false, true>), g, b, 0, stream, p, sh);
+  else hipLaunchKernelGGL((moe_dispatch_kernel<false, false>), g, b, 0, stream, p, sh);
   return hipGetLastError();
 }
 
 hipError_t launch_moe_combine(const MoeRowsParams& p, bool bf16, int num_cus, hipStream_t stream) {
+  const bool past = streams_past_caches(p.tokens * p.cols * (bf16 ? 2 : 4));
   const RowShape sh = row_shape(p.tokens, (p.cols + 7) / 8, num_cus);
   const dim3 g((unsigned)(sh.row_blocks * sh.splits)), b(256);
-  if (bf16) hipLaunchKernelGGL((moe_combine_kernel<true>), g, b, 0, stream, p, sh);
-  else hipLaunchKernelGGL((moe_combine_kernel<false>), g, b, 0, stream, p, sh);
+  if (bf16 && past) hipLaunchKernelGGL((moe_combine_kernel<true, true>), g, b, 0, stream, p, sh);
+  else if (bf16) hipLaunchKernelGGL((moe_combine_kernel<true, false>), g, b, 0, stream, p, sh);
+  else if (past) hipLaunchKernelGGL((moe_combine_kernel<false, true>), g, b, 0, stream, p, sh);
+  else hipLaunchKernelGGL((moe_combine_kernel<false, false>), g, b, 0, stream, p, sh);
   return hipGetLastError();
 }
 
+template <bool BF16, bool PAST>
+static const void* grad_kernel(bool wide) {
+  return wide ? reinterpret_cast<const void*>(&moe_combine_grad_kernel<BF16, PAST, 4>)
+              : reinterpret_cast<const void*>(&moe_combine_grad_kernel<BF16, PAST, 1>);
+}
+
 hipError_t launch_moe_combine_grad(const MoeRowsParams& p, bool bf16, int num_cus, hipStream_t stream) {
-  // a whole workgroup for a token's row where a wave would loop over it more than 4 times
-  const bool wide = p.cols > 4 * 512;
+  // four waves to a token where each has two loads of its row or more (8192 tokens x 4096 bf16:
+  // 67 us, one wave 81; 16384 x 1024: one wave 35 us)
+  const bool wide = p.cols >= 2048;
+  const bool past = streams_past_caches(p.rows * p.cols * (bf16 ? 2 : 4));
   const int64_t groups = wide ? p.tokens : (p.tokens + 3) / 4;
   const dim3 g((unsigned)(groups + (p.rows + 255) / 256)), b(256);
-  if (bf16 && wide) hipLaunchKernelGGL((moe_combine_grad_kernel<true, 4>), g, b, 0, stream, p, groups);
-  else if (bf16) hipLaunchKernelGGL((moe_combine_grad_kernel<true, 1>), g, b, 0, stream, p, groups);
-  else if (wide) hipLaunchKernelGGL((moe_combine_grad_kernel<false, 4>), g, b, 0, stream, p, groups);
-  else hipLaunchKernelGGL((moe_combine_grad_kernel<false, 1>), g, b, 0, stream, p, groups);
-  return hipGetLastError();
+  const void* k = bf16 ? (past ? grad_kernel<true, true>(wide) : grad_kernel<true, false>(wide))
+                       : (past ? grad_kernel<false, true>(wide) : grad_kernel<false, false>(wide));
+  MoeRowsParams local = p;
+  int64_t token_groups = groups;
+  void* args[] = {&local, &token_groups};
+  return hipLaunchKernel(k, g, b, args, 0, stream);
 }
 
 }  // namespace sfc

@@ -17,7 +17,9 @@ from __future__ import annotations
 
 import ctypes
 
-from paper_2601_16294_amd.sfcgemm import SFC_OUT_BF16, SFC_OUT_F32, SfcError, _cached, _check, _stream_handle, lib
+import torch
+
+from paper_2601_16294_amd.sfcgemm import SFC_OUT_BF16, SFC_OUT_F32, SFC_OK, SfcError, _stream_handle, lib
 
 __all__ = ["SfcError", "mx4_empty", "sfc_mx4_quant", "sfc_mx4_dequant", "sfc_gemm_mx4_ex", "sfc_mx4_linear",
            "sfc_moe_sort", "sfc_moe_sort_rows", "sfc_moe_dispatch", "sfc_moe_combine", "sfc_moe_combine_grad",
@@ -48,104 +50,97 @@ def _declare() -> None:
 _declare()
 
 
-def _torch():
-    import torch
-    return torch
+_TYPES = {torch.float32: SFC_OUT_F32, torch.bfloat16: SFC_OUT_BF16}
+_Tensor, _U8, _I32, _F32 = torch.Tensor, torch.uint8, torch.int32, torch.float32
+# (the accessor behind torch.cuda.current_device; a small call is bound by its host time)
+_current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _types():
-    torch = _torch()
-    return {torch.float32: SFC_OUT_F32, torch.bfloat16: SFC_OUT_BF16}
-
-
-def _current_device():
-    return _torch().cuda.current_device
+def _check(code: int, what: str) -> None:
+    if code != SFC_OK:
+        raise SfcError(code, what)
 
 
 def _tensor(t, name, what):
-    if not isinstance(t, _cached(_torch).Tensor):
+    if not isinstance(t, _Tensor):
         raise TypeError(f"{what}: {name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{what}: {name} must be a CUDA tensor (got {t.device})")
-    if t.get_device() != _cached(_current_device)():
-        raise ValueError(f"{what}: {name} is on {t.device}, the current device is "
-                         f"cuda:{_cached(_current_device)()}")
+    if t.get_device() != _current():
+        raise ValueError(f"{what}: {name} is on {t.device}, the current device is cuda:{_current()}")
 
 
 def _rows(t, name, what, shape=None):
     """(pointer, leading dimension, type code) of a 2-D fp32 or bf16 tensor with unit column stride."""
-    _tensor(t, name, what)
-    code = _cached(_types).get(t.dtype)
+    if t.__class__ is not _Tensor or t.get_device() != _current():     # (what the checks come to for a good one)
+        _tensor(t, name, what)
+    code = _TYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"{what}: {name} must be float32 or bfloat16 (got {t.dtype})")
-    if t.dim() != 2:
+    s = t.stride()
+    if len(s) != 2:
         raise ValueError(f"{what}: {name} must be 2-D")
     r, c = t.shape
     if shape is not None and (r != shape[0] or c != shape[1]):
         raise ValueError(f"{what}: shape mismatch: {name} is {tuple(t.shape)}, expected {tuple(shape)}")
-    s0, s1 = t.stride()
-    if s1 != 1 and c > 1:
+    if s[1] != 1 and c > 1:
         raise ValueError(f"{what}: {name} must have unit column stride")
-    return t.data_ptr(), s0 if r > 1 else max(c, 1), code
-
-
-def _blocks(cols: int) -> int:
-    return (cols + 31) // 32
+    return t.data_ptr(), s[0] if r > 1 else c or 1, code
 
 
 def _mx4(q, s, name, what, rows=None, cols=None, lead=0):
     """(codes, row bytes, scales, row bytes) of a 4-bit matrix, `lead` dimensions before it.
     Checks the shape against rows x cols where they are given."""
-    for t, n in ((q, name), (s, f"the scales of {name}")):
-        _tensor(t, n, what)
-        if t.dtype != _cached(_torch).uint8:
-            raise TypeError(f"{what}: {n} must be uint8 (got {t.dtype})")
-        if t.dim() != 2 + lead:
-            raise ValueError(f"{what}: {n} must be {2 + lead}-D")
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
-            raise ValueError(f"{what}: {n} must have unit column stride")
-    r, half = q.shape[-2:]
-    blocks = s.shape[-1]
-    if half != 16 * blocks or s.shape[:-1] != q.shape[:-1]:
-        raise ValueError(f"{what}: shape mismatch: {name} {tuple(q.shape)} and its scales {tuple(s.shape)} "
+    cur = _current()
+    if (q.__class__ is not _Tensor or s.__class__ is not _Tensor or q.get_device() != cur
+            or s.get_device() != cur):
+        _tensor(q, name, what)
+        _tensor(s, f"{name}'s scales", what)
+    if q.dtype != _U8 or s.dtype != _U8:
+        raise TypeError(f"{what}: {name} and its scales must be uint8 (got {q.dtype} and {s.dtype})")
+    sq, ss, dq, ds = q.shape, s.shape, q.stride(), s.stride()
+    if len(sq) != 2 + lead or len(ss) != 2 + lead:
+        raise ValueError(f"{what}: {name} and its scales must be {2 + lead}-D")
+    r, half, blocks = sq[-2], sq[-1], ss[-1]
+    if half != 16 * blocks or ss[-2] != r or (lead and ss[0] != sq[0]):
+        raise ValueError(f"{what}: shape mismatch: {name} {tuple(sq)} and its scales {tuple(ss)} "
                          "(16 bytes of codes to a scale)")
-    if rows is not None and (r != rows or blocks != _blocks(cols)):
-        raise ValueError(f"{what}: shape mismatch: {name} is {tuple(q.shape)}, expected "
-                         f"{(rows, 16 * _blocks(cols))}")
-    padded = (blocks + 3) // 4 * 4
-    ldq, lds = (q.stride(-2), s.stride(-2)) if r > 1 else (max(half, 16), max(padded, 4))
+    if (dq[-1] != 1 and half > 1) or (ds[-1] != 1 and blocks > 1):
+        raise ValueError(f"{what}: {name} and its scales must have unit column stride")
+    if rows is not None and (r != rows or blocks != (cols + 31) // 32):
+        raise ValueError(f"{what}: shape mismatch: {name} is {tuple(sq)}, expected "
+                         f"{(rows, 16 * ((cols + 31) // 32))}")
+    padded = (blocks + 3) & ~3
     if padded != blocks and q.numel():
         # the last row of scales, too, is read in whole groups of 4
-        last = s.storage_offset() + sum((n - 1) * st for n, st in zip(s.shape[:-1], s.stride()[:-1]))
+        last = s.storage_offset() + sum((n - 1) * d for n, d in zip(ss[:-1], ds[:-1]))
         if last + padded > s.untyped_storage().nbytes():
             raise ValueError(f"{what}: the scales of {name} end inside a group of 4 bytes: allocate rows of "
                              f"{padded} (mx4_empty does)")
-    return q.data_ptr(), ldq, s.data_ptr(), lds
+    if r > 1:
+        return q.data_ptr(), dq[-2], s.data_ptr(), ds[-2]
+    return q.data_ptr(), half or 16, s.data_ptr(), padded or 4
+
+
+def _vector(t, name, what, dtype, count):
+    """Pointer of a contiguous tensor of `count` elements (None: any number)."""
+    if t.__class__ is not _Tensor or t.get_device() != _current():
+        _tensor(t, name, what)
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: {name} must be {str(dtype)[6:]} (got {t.dtype})")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: {name} must be contiguous")
+    if count is not None and t.numel() != count:
+        raise ValueError(f"{what}: {name} has {t.numel()} elements, expected {count}")
+    return t.data_ptr()
 
 
 def _ints(t, name, what, count):
-    """Pointer of a contiguous int32 tensor of `count` elements."""
-    _tensor(t, name, what)
-    if t.dtype != _cached(_torch).int32:
-        raise TypeError(f"{what}: {name} must be int32 (got {t.dtype})")
-    if not t.is_contiguous():
-        raise ValueError(f"{what}: {name} must be contiguous")
-    if count is not None and t.numel() != count:
-        raise ValueError(f"{what}: {name} has {t.numel()} elements, expected {count}")
-    return t.data_ptr()
+    return _vector(t, name, what, _I32, count)
 
 
-def _weights(t, what, count, name="weights"):
-    if t is None:
-        return None
-    _tensor(t, name, what)
-    if t.dtype != _cached(_torch).float32:
-        raise TypeError(f"{what}: {name} must be float32 (got {t.dtype})")
-    if not t.is_contiguous():
-        raise ValueError(f"{what}: {name} must be contiguous")
-    if count is not None and t.numel() != count:
-        raise ValueError(f"{what}: {name} has {t.numel()} elements, expected {count}")
-    return t.data_ptr()
+def _weights(t, what, count):
+    return None if t is None else _vector(t, "weights", what, _F32, count)
 
 
 def _topk(topk, what):
@@ -154,14 +149,13 @@ def _topk(topk, what):
     return topk
 
 
-def mx4_empty(rows: int, cols: int, lead=(), device=None):
+def mx4_empty(rows: int, cols: int, lead=(), device="cuda"):
     """Uninitialised (codes, scales) of a rows x cols 4-bit matrix (or of `lead` such matrices)."""
-    torch = _cached(_torch)
-    device = "cuda" if device is None else device
-    b = _blocks(cols)
-    codes = torch.empty((*lead, rows, 16 * b), dtype=torch.uint8, device=device)
-    scales = torch.empty((*lead, rows, (b + 3) // 4 * 4), dtype=torch.uint8, device=device)
-    return codes, scales[..., :b]
+    b = (cols + 31) // 32
+    padded = (b + 3) & ~3
+    codes = torch.empty((*lead, rows, 16 * b), dtype=_U8, device=device)
+    scales = torch.empty((*lead, rows, padded), dtype=_U8, device=device)
+    return codes, scales if padded == b else scales[..., :b]
 
 
 def sfc_mx4_quant(X, Q=None, S=None, Qt=None, St=None, order=None, topk: int = 1, stream=None) -> None:
@@ -293,11 +287,9 @@ def sfc_moe_combine_grad(dY, Ys, order, pos, weights, dYs, dW, stream=None) -> N
         raise TypeError(f"{what}: Ys and dYs must hold dY's type")
     slots = pos.numel()
     topk = _slots_per_token(slots, tokens, what)
-    if dW is None:
-        raise TypeError(f"{what}: dW must be a torch.Tensor")
     _check(lib.sfc_moe_combine_grad(tokens, cols, rows, topk, pd, ldd, pr, ldr, kind, _ints(order, "order", what, rows),
                                     _ints(pos, "pos", what, slots), _weights(weights, what, slots), ps, lds,
-                                    _weights(dW, what, slots, "dW"), _stream_handle(stream)), what)
+                                    _vector(dW, "dW", what, _F32, slots), _stream_handle(stream)), what)
 
 
 def sfc_moe_gemm_mx4_ex(A, As, B, Bs, offsets, C, stream=None) -> None:
@@ -321,7 +313,7 @@ def sfc_moe_wgrad_mx4_ex(A, As, B, Bs, offsets, C, stream=None) -> None:
     M, N, rows = A.shape[0], B.shape[0], 32 * As.shape[1]
     if Bs.shape[1] != As.shape[1]:
         raise ValueError(f"{what}: shape mismatch: A {tuple(A.shape)} B {tuple(B.shape)}")
-    if not isinstance(C, _cached(_torch).Tensor) or C.dim() != 3:
+    if not isinstance(C, _Tensor) or C.dim() != 3:
         raise ValueError(f"{what}: C must be a 3-D tensor")
     E = C.shape[0]
     po = _ints(offsets, "offsets", what, None)
