@@ -22,25 +22,61 @@ int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
 // How a dense product runs.
 struct Mx4Plan {
-  int fm = 0, fn = 0, waves = 0;       // fm > 0: the kernel for few rows
+  bool few = false;                    // up to 16 rows: A stays in registers
+  int fm = 0;                          // > 0: the streaming kernel, 16 * fm rows at a time
   bool large = false;                  // 256x256 blocks, else 128x128
   int layers = 1;
 };
 
+// Microseconds of `tasks` blocks over `stages` 256-deep stages on the tile kernels, fitted to
+// timings of random operands (M, N from 100 to 14336, K from 1024 to 16384; within 10 %):
+// 256x256 blocks take 1.9 us a stage on a full chip (1.5 on few CUs: the clock), 128x128
+// blocks 0.6 alone on a CU and 1.15 for the two that share one.
+double mx4_tile_us(bool large, int64_t tasks, double stages, int num_cus) {
+  const int64_t slots = large ? num_cus : 2 * (int64_t)num_cus;
+  const double part = (double)(tasks % slots) / (double)slots;
+  double us = (double)(tasks / slots) * (large ? 1.9 * stages + 5.5 : 1.15 * stages + 2.5);
+  if (part > 0) {
+    if (large) us += (1.5 + 0.4 * part) * stages + 2.0 + 3.5 * part;
+    else if (part <= 0.5) us += (0.55 + 0.2 * part) * stages + 0.4 + 2.2 * part;
+    else us += (0.3 + 0.85 * part) * stages + 2.5;
+  }
+  return us;
+}
+
 Mx4Plan mx4_plan(int64_t M, int64_t N, int64_t K, int num_cus) {
   Mx4Plan pl;
-  const int64_t turns = sfc::ceil_div(K, 512);
-  if (M <= 64) {
-    pl.fm = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    pl.fn = pl.fm == 1 && sfc::ceil_div(N, 32) < num_cus ? 1 : 2;
-    pl.waves = turns >= 8 ? 8 : 4;
+  if (M <= 16) {
+    // (one block of columns to a workgroup and several turns to a wave: no loads ahead to gain.
+    // 1x4096x14336: 10.2 us, streaming 8.4; 1x16384x16384: 26.8, streaming 30.7)
+    pl.few = K <= 16 * 512 || (K <= sfc::kFewDepth && N > 16 * (int64_t)num_cus);
+    pl.fm = pl.few ? 0 : 1;
     return pl;
   }
-  const int64_t large = sfc::ceil_div(M, 256) * sfc::ceil_div(N, 256);
-  pl.large = 2 * large >= num_cus;
-  const int64_t tasks = pl.large ? large : sfc::ceil_div(M, 128) * sfc::ceil_div(N, 128);
-  const int64_t slots = pl.large ? num_cus : 2 * num_cus;
-  while (pl.layers < sfc::kAutoLayers && 2 * tasks * pl.layers <= slots && turns >= 4 * pl.layers) pl.layers *= 2;
+  // Up to 64 rows: the streaming kernel reads A once for every 32 columns, which pays while a
+  // wave has one turn of K (us, streaming against 128x128 blocks with their best layers:
+  // 32x4096x4096 7.6 / 10.6, 32x14336x4096 13.7 / 14.5, 32x4096x14336 20.5 / 16.0; 64x4096x4096
+  // 10.3 / 11.7, 64x1024x1024 4.4 / 6.2, 64x14336x4096 21.0 / 15.5).
+  if (M <= 64 && K <= 8 * 512 && (M <= 32 || N <= 4096)) {
+    pl.fm = M <= 32 ? 2 : 4;
+    return pl;
+  }
+  // block shape and layers of the least estimated time; copies are written and read back
+  // (6 bytes a ns) by a second launch (2.5 us)
+  double best = 0;
+  for (int large = 1; large >= 0; --large) {
+    const int64_t b = large ? 256 : 128, blocks = sfc::ceil_div(M, b) * sfc::ceil_div(N, b);
+    const int64_t stages = K > 0 ? sfc::ceil_div(K, 256) : 1;
+    for (int c = 1; c <= sfc::kAutoLayers && (c == 1 || 2 * c <= stages); c *= 2) {
+      double us = mx4_tile_us(large, blocks * c, (double)sfc::ceil_div(stages, c), num_cus);
+      if (c > 1) us += 2.5 + 8.0 * (double)c * (double)M * (double)N / 6.0e6;
+      if (best == 0 || us < best) {
+        best = us;
+        pl.large = large != 0;
+        pl.layers = c;
+      }
+    }
+  }
   return pl;
 }
 
@@ -51,8 +87,9 @@ size_t mx4_copies(const Mx4Plan& pl, int64_t M, int64_t N) {
 
 // Launches a dense product; `copies` holds its layer copies.  With the lock held.
 int mx4_dense(const Mx4Plan& pl, sfc::Mx4GemmParams& p, bool ob, int num_cus, float* copies, hipStream_t stream) {
-  if (pl.fm) {
-    const hipError_t e = sfc::launch_mx4_rows(p, sfc::kMxDense, pl.fm, pl.fn, pl.waves, ob, stream);
+  if (pl.few || pl.fm) {
+    const hipError_t e = pl.few ? sfc::launch_mx4_few(p, sfc::kRowsCodes, num_cus, ob, stream)
+                                : sfc::launch_mx4_rows(p, sfc::kMxDense, pl.fm, sfc::ceil_div(p.N, 32) < num_cus, ob, stream);
     return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "4-bit product of few rows");
   }
   const int b = pl.large ? 256 : 128;
@@ -152,7 +189,7 @@ int sfc_gemm_mx4_ex(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda,
   if (need) rc = sfc::host_workspace(st, need, &ws);
   if (rc != SFC_OK) return rc;
   sfc::Mx4GemmParams p = {M, N, K, bytes(A), bytes(As), bytes(B), bytes(Bs), lda, ldas, ldb, ldbs, 0, 0, C, ldc, 0,
-                          nullptr, 0, 0, 0, nullptr, 1};
+                          nullptr, 0, 0, 0, nullptr, 1, nullptr, 0, 0};
   return mx4_dense(pl, p, out_type == SFC_OUT_BF16, cus, static_cast<float*>(ws), st);
 }
 
@@ -168,6 +205,17 @@ int sfc_mx4_linear(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, 
   if (rc != SFC_OK) return rc;
   const int64_t blocks = sfc::mx4_blocks(K), ldq = 16 * blocks, lds = round_up(blocks, 4);
   const Mx4Plan pl = mx4_plan(M, N, 32 * blocks, cus);
+  // Few rows brought to 4 bits by the product's own launch: every workgroup converts them, which
+  // costs less than a launch while they or the workgroups are few (us in a graph, both
+  // launches against one: 1x4096x4096 7.2 / 5.6, 16x4096x4096 7.4 / 8.0 but 3.5 us less host time,
+  // 8x14336x4096 11.6 / 11.6, 16x14336x4096 11.7 / 13.0).
+  if (pl.few && K > 0 && K <= sfc::kConvertDepth && (M <= 8 || N <= 32 * (int64_t)cus)) {
+    const sfc::Mx4GemmParams p = {M, N, 32 * blocks, nullptr, nullptr, bytes(W), bytes(Ws), 0, 0, ldw, ldws, 0, 0, Y, ldy,
+                                  0, nullptr, 0, 0, 0, nullptr, 1, X, ldx, K};
+    const hipError_t e = sfc::launch_mx4_few(p, in_type == SFC_OUT_BF16 ? sfc::kRowsBf16 : sfc::kRowsF32, cus,
+                                             out_type == SFC_OUT_BF16, st);
+    return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "4-bit product of few rows");
+  }
   // the stream's workspace: codes and scales of X, then the layer copies
   const size_t code_bytes = (size_t)M * (size_t)ldq, scale_bytes = (size_t)round_up(M * lds, 16);
   void* ws = nullptr;
@@ -180,7 +228,7 @@ int sfc_mx4_linear(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, 
     if (rc != SFC_OK) return rc;
   }
   sfc::Mx4GemmParams p = {M, N, 32 * blocks, q, q + code_bytes, bytes(W), bytes(Ws), ldq, lds, ldw, ldws, 0, 0, Y, ldy,
-                          0, nullptr, 0, 0, 0, nullptr, 1};
+                          0, nullptr, 0, 0, 0, nullptr, 1, nullptr, 0, 0};
   return mx4_dense(pl, p, out_type == SFC_OUT_BF16, cus, reinterpret_cast<float*>(q + code_bytes + scale_bytes), st);
 }
 
@@ -197,12 +245,11 @@ int sfc_moe_gemm_mx4_ex(int64_t rows, int64_t N, int64_t K, int experts, const v
   const int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
   sfc::Mx4GemmParams p = {rows, N, K, bytes(A), bytes(As), bytes(B), bytes(Bs), lda, ldas, ldb, ldbs, stride_b,
-                          stride_bs, C, ldc, 0, nullptr, 0, 0, experts, offsets, 1};
+                          stride_bs, C, ldc, 0, nullptr, 0, 0, experts, offsets, 1, nullptr, 0, 0};
   const bool ob = out_type == SFC_OUT_BF16;
   hipError_t e;
   if (rows <= 32 * (int64_t)experts) {
-    const int64_t turns = sfc::ceil_div(K, 512);
-    e = sfc::launch_mx4_rows(p, sfc::kMxRows, rows <= 16 * (int64_t)experts ? 1 : 2, 2, turns >= 8 ? 8 : 4, ob, st);
+    e = sfc::launch_mx4_rows(p, sfc::kMxRows, rows <= 16 * (int64_t)experts ? 1 : 2, false, ob, st);
   } else {
     const int64_t large = (rows / 256 + experts) * sfc::ceil_div(N, 256);
     const bool big = rows >= 192 * (int64_t)experts && 2 * large >= cus;
@@ -228,7 +275,7 @@ int sfc_moe_wgrad_mx4_ex(int64_t M, int64_t N, int64_t rows, int experts, const 
   int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
   sfc::Mx4GemmParams p = {M, N, rows, bytes(A), bytes(As), bytes(B), bytes(Bs), lda, ldas, ldb, ldbs, 0, 0, C, ldc,
-                          stride_c, nullptr, 0, 0, experts, offsets, 1};
+                          stride_c, nullptr, 0, 0, experts, offsets, 1, nullptr, 0, 0};
   const bool ob = out_type == SFC_OUT_BF16;
   const int64_t large = sfc::ceil_div(M, 256) * sfc::ceil_div(N, 256) * experts;
   const bool big = 2 * large >= cus;

@@ -53,15 +53,23 @@ struct Mx4GemmParams {
   int experts;
   const int32_t* offsets;    // experts + 1
   int layers;                // kMxDense: ranges of K, each with a copy of C
+  // launch_mx4_few: A as fp32 or bf16 rows (X, ldx elements, x_cols of them in a row), brought
+  // to 4 bits on the way in
+  const void* X;
+  int64_t ldx, x_cols;
 };
+enum Mx4Rows { kRowsCodes = 0, kRowsBf16 = 1, kRowsF32 = 2 };    // what A is
 // Blocks of 256 x 256, one workgroup to a CU, or of 128 x 128, two.
 hipError_t launch_mx4_256x256(const Mx4GemmParams& p, Mx4Mode mode, bool out_bf16, int grid, hipStream_t stream);
 hipError_t launch_mx4_128x128(const Mx4GemmParams& p, Mx4Mode mode, bool out_bf16, int grid, hipStream_t stream);
 
-// Few rows (of A, or of each expert): a workgroup of `waves` waves streams 16 * fn rows of
-// B past 16 * fm rows of A.
-hipError_t launch_mx4_rows(const Mx4GemmParams& p, Mx4Mode mode, int fm, int fn, int waves, bool out_bf16,
-                           hipStream_t stream);
+// Few rows of A, or of each expert: a workgroup streams 32 rows of B (`narrow`, fm = 1: 16) past
+// 16 * fm rows of A at a time (fm = 1, 2, 4).
+hipError_t launch_mx4_rows(const Mx4GemmParams& p, Mx4Mode mode, int fm, bool narrow, bool out_bf16, hipStream_t stream);
+// Up to 16 rows of A, given as `rows` says, and K up to kFewDepth (kConvertDepth for rows that
+// are not codes); dense products.
+constexpr int64_t kFewDepth = 32 * 512, kConvertDepth = 8 * 512;
+hipError_t launch_mx4_few(const Mx4GemmParams& p, Mx4Rows rows, int num_cus, bool out_bf16, hipStream_t stream);
 
 // Slots sorted by expert.
 struct MoeSortParams {
