@@ -4,7 +4,7 @@
 namespace sfc {
 
 hipError_t launch_mx4_256x256(const Mx4GemmParams& p, Mx4Mode mode, bool out_bf16, int grid, hipStream_t stream) {
-  return out_bf16 ? mx4_launch<256, 256, true>(p, mode, grid, stream) : mx4_launch<256, 256, false>(p, mode, grid, stream);
+  return mx4_launch<256, 256>(p, mode, out_bf16, grid, stream);
 }
 
 }  // namespace sfc

@@ -85,7 +85,8 @@ struct MxTask {
   char* C;
 };
 
-template <int BM, int BN, bool OB, bool FULL>
+// PAST: past the caches (a template argument: the compiler joins a branch's stores into one).
+template <int BM, int BN, bool OB, bool FULL, bool PAST>
 __device__ __forceinline__ void mx_store(const Mx4GemmParams& p, const MxTask& t, f32x16 (&acc)[BM / 64][BN / 64],
                                          uint32_t lds0, int wave, int lane) {
   using T = MxTile<BM, BN>;
@@ -126,9 +127,10 @@ __device__ __forceinline__ void mx_store(const Mx4GemmParams& p, const MxTask& t
         }
         v = o;
       }
-      struct __attribute__((packed, aligned(OB ? 2 : 4))) Any { u32x4 v; };
+      typedef u32x4 any_u32x4 __attribute__((aligned(2)));
       if (FULL || (in && n_left >= CPL)) {
-        reinterpret_cast<Any*>(dst)->v = v;
+        if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<any_u32x4*>(dst));
+        else *reinterpret_cast<any_u32x4*>(dst) = v;
       } else if (in) {
 #pragma unroll
         for (int e = 0; e < CPL; ++e) {
@@ -142,7 +144,7 @@ __device__ __forceinline__ void mx_store(const Mx4GemmParams& p, const MxTask& t
   }
 }
 
-template <int BM, int BN, bool OB>
+template <int BM, int BN, bool OB, bool PAST>
 __device__ __forceinline__ void mx_block(const Mx4GemmParams& p, const MxTask& t, uint32_t lds0, int wave, int lane) {
   using T = MxTile<BM, BN>;
   const int wm = wave >> 1, wn = wave & 1;
@@ -330,14 +332,14 @@ __device__ __forceinline__ void mx_block(const Mx4GemmParams& p, const MxTask& t
   }
   __syncthreads();                // every wave is done with the ring
   const bool full = t.m_valid == BM && t.n_valid == BN;
-  if (full) mx_store<BM, BN, OB, true>(p, t, acc, lds0, wave, lane);
-  else mx_store<BM, BN, OB, false>(p, t, acc, lds0, wave, lane);
+  if (full) mx_store<BM, BN, OB, true, PAST>(p, t, acc, lds0, wave, lane);
+  else mx_store<BM, BN, OB, false, PAST>(p, t, acc, lds0, wave, lane);
   __syncthreads();                // the ring may be filled again
 }
 
 // Blocks of C in this order: curve positions (dense products, and each expert's in turn
 // for kMxDepth); for kMxRows supertiles of up to 8 blocks of rows by all blocks of columns.
-template <int BM, int BN, bool OB, int MODE>
+template <int BM, int BN, bool OB, bool PAST, int MODE>
 __global__ __launch_bounds__(256, (MxTile<BM, BN>::PER_CU)) void mx4_gemm_kernel(Mx4GemmParams p) {
   using T = MxTile<BM, BN>;
   __shared__ __attribute__((aligned(16))) unsigned char smem[T::LDS];
@@ -409,7 +411,7 @@ __global__ __launch_bounds__(256, (MxTile<BM, BN>::PER_CU)) void mx4_gemm_kernel
       t.hi = blocks;
       t.B = p.B + (int64_t)e * p.stride_b;
       t.Bs = p.Bs + (int64_t)e * p.stride_bs;
-      mx_block<BM, BN, OB>(p, t, lds0, wave, lane);
+      mx_block<BM, BN, OB, PAST>(p, t, lds0, wave, lane);
     }
     // rows of no expert: behind the last segment
     int used = 0;
@@ -462,16 +464,22 @@ __global__ __launch_bounds__(256, (MxTile<BM, BN>::PER_CU)) void mx4_gemm_kernel
       t.lo = (int)(b0 - t.block0);
       t.hi = (int)(b1 - t.block0);
       if (b1 == b0) t.hi = t.lo = 0;
-      mx_block<BM, BN, OB>(p, t, lds0, wave, lane);
+      mx_block<BM, BN, OB, PAST>(p, t, lds0, wave, lane);
     }
   }
 }
 
-template <int BM, int BN, bool OB>
-static hipError_t mx4_launch(const Mx4GemmParams& p, Mx4Mode mode, int grid, hipStream_t stream) {
-  const void* k = mode == kMxDense ? reinterpret_cast<const void*>(&mx4_gemm_kernel<BM, BN, OB, kMxDense>)
-                  : mode == kMxRows ? reinterpret_cast<const void*>(&mx4_gemm_kernel<BM, BN, OB, kMxRows>)
-                                    : reinterpret_cast<const void*>(&mx4_gemm_kernel<BM, BN, OB, kMxDepth>);
+template <int BM, int BN, bool OB, bool PAST>
+static const void* mx4_kernel(Mx4Mode mode) {
+  return mode == kMxDense  ? reinterpret_cast<const void*>(&mx4_gemm_kernel<BM, BN, OB, PAST, kMxDense>)
+         : mode == kMxRows ? reinterpret_cast<const void*>(&mx4_gemm_kernel<BM, BN, OB, PAST, kMxRows>)
+                           : reinterpret_cast<const void*>(&mx4_gemm_kernel<BM, BN, OB, PAST, kMxDepth>);
+}
+
+template <int BM, int BN>
+static hipError_t mx4_launch(const Mx4GemmParams& p, Mx4Mode mode, bool out_bf16, int grid, hipStream_t stream) {
+  const void* k = !out_bf16 ? mx4_kernel<BM, BN, false, false>(mode)
+                  : p.past  ? mx4_kernel<BM, BN, true, true>(mode) : mx4_kernel<BM, BN, true, false>(mode);
   Mx4GemmParams local = p;
   void* args[] = {&local};
   return hipLaunchKernel(k, dim3((unsigned)grid), dim3(256), args, 0, stream);

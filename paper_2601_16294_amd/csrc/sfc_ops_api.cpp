@@ -20,6 +20,11 @@ hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 const uint8_t* bytes(const void* p) { return static_cast<const uint8_t*>(p); }
 int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
+// Whether a bf16 C of so many elements goes past the caches: 32 MB, as for the row operators
+// (4096x4096x1024 18.7 -> 17.3 us, 4096x14336x4096 141 -> 139, and what is read next is still
+// cached; fp32 loses as much as it gains: 4096x4096x4096 44.1, 44.4).
+bool past_caches(int64_t elements) { return elements >= (int64_t)16 << 20; }
+
 // How a dense product runs.
 struct Mx4Plan {
   bool few = false;                    // up to 16 rows: A stays in registers
@@ -189,7 +194,7 @@ int sfc_gemm_mx4_ex(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda,
   if (need) rc = sfc::host_workspace(st, need, &ws);
   if (rc != SFC_OK) return rc;
   sfc::Mx4GemmParams p = {M, N, K, bytes(A), bytes(As), bytes(B), bytes(Bs), lda, ldas, ldb, ldbs, 0, 0, C, ldc, 0,
-                          nullptr, 0, 0, 0, nullptr, 1, nullptr, 0, 0};
+                          nullptr, 0, 0, 0, nullptr, 1, past_caches(M * N), nullptr, 0, 0};
   return mx4_dense(pl, p, out_type == SFC_OUT_BF16, cus, static_cast<float*>(ws), st);
 }
 
@@ -211,7 +216,7 @@ int sfc_mx4_linear(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, 
   // 8x14336x4096 11.6 / 11.6, 16x14336x4096 11.7 / 13.0).
   if (pl.few && K > 0 && K <= sfc::kConvertDepth && (M <= 8 || N <= 32 * (int64_t)cus)) {
     const sfc::Mx4GemmParams p = {M, N, 32 * blocks, nullptr, nullptr, bytes(W), bytes(Ws), 0, 0, ldw, ldws, 0, 0, Y, ldy,
-                                  0, nullptr, 0, 0, 0, nullptr, 1, X, ldx, K};
+                                  0, nullptr, 0, 0, 0, nullptr, 1, false, X, ldx, K};
     const hipError_t e = sfc::launch_mx4_few(p, in_type == SFC_OUT_BF16 ? sfc::kRowsBf16 : sfc::kRowsF32, cus,
                                              out_type == SFC_OUT_BF16, st);
     return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "4-bit product of few rows");
@@ -228,7 +233,7 @@ int sfc_mx4_linear(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, 
     if (rc != SFC_OK) return rc;
   }
   sfc::Mx4GemmParams p = {M, N, 32 * blocks, q, q + code_bytes, bytes(W), bytes(Ws), ldq, lds, ldw, ldws, 0, 0, Y, ldy,
-                          0, nullptr, 0, 0, 0, nullptr, 1, nullptr, 0, 0};
+                          0, nullptr, 0, 0, 0, nullptr, 1, past_caches(M * N), nullptr, 0, 0};
   return mx4_dense(pl, p, out_type == SFC_OUT_BF16, cus, reinterpret_cast<float*>(q + code_bytes + scale_bytes), st);
 }
 
@@ -245,7 +250,7 @@ int sfc_moe_gemm_mx4_ex(int64_t rows, int64_t N, int64_t K, int experts, const v
   const int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
   sfc::Mx4GemmParams p = {rows, N, K, bytes(A), bytes(As), bytes(B), bytes(Bs), lda, ldas, ldb, ldbs, stride_b,
-                          stride_bs, C, ldc, 0, nullptr, 0, 0, experts, offsets, 1, nullptr, 0, 0};
+                          stride_bs, C, ldc, 0, nullptr, 0, 0, experts, offsets, 1, past_caches(rows * N), nullptr, 0, 0};
   const bool ob = out_type == SFC_OUT_BF16;
   hipError_t e;
   if (rows <= 32 * (int64_t)experts) {
@@ -275,7 +280,7 @@ int sfc_moe_wgrad_mx4_ex(int64_t M, int64_t N, int64_t rows, int experts, const 
   int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
   sfc::Mx4GemmParams p = {M, N, rows, bytes(A), bytes(As), bytes(B), bytes(Bs), lda, ldas, ldb, ldbs, 0, 0, C, ldc,
-                          stride_c, nullptr, 0, 0, experts, offsets, 1, nullptr, 0, 0};
+                          stride_c, nullptr, 0, 0, experts, offsets, 1, past_caches(M * N * experts), nullptr, 0, 0};
   const bool ob = out_type == SFC_OUT_BF16;
   const int64_t large = sfc::ceil_div(M, 256) * sfc::ceil_div(N, 256) * experts;
   const bool big = 2 * large >= cus;
