@@ -347,6 +347,16 @@ __global__ __launch_bounds__(256, (MxTile<BM, BN>::PER_CU)) void mx4_gemm_kernel
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t lds0 = lds_addr(smem);
   const int P = gridDim.x, rank = xcd_rank(blockIdx.x, P);
+  // Tasks of this workgroup: its rank of every full round, and in the last, partial one its
+  // rank among as many workgroups as there are tasks left.  Those are the first, which spreads them
+  // over all chiplets, and one to a CU where two fit (by full ranks they would fill some
+  // chiplets and leave the others idle).
+  auto next_task = [&](int64_t task, int64_t total) {
+    const int64_t from = task < 0 ? 0 : (task / P + 1) * P;       // the round's first task
+    if (from + P <= total) return from + rank;
+    const int left = (int)(total - from);
+    return (int)blockIdx.x < left ? from + xcd_rank(blockIdx.x, left) : (int64_t)-1;
+  };
   constexpr int ES = OB ? 2 : 4;
   MxTask t;
   t.B = p.B;
@@ -361,8 +371,8 @@ __global__ __launch_bounds__(256, (MxTile<BM, BN>::PER_CU)) void mx4_gemm_kernel
       lo = lo < 0 ? 0 : lo > p.M ? p.M : lo;
       hi = hi < lo ? lo : hi > p.M ? p.M : hi;
     };
-    // the expert that holds block of rows `mt` (counted over all experts): -1 if there are
-    // fewer; the blocks before it and its own
+    // the expert that holds block of rows `mt` (counted over all experts; there is one), the
+    // blocks before it and its own
     auto find = [&](int mt, int& first, int& gm) {
       int carry = 0;
       for (int e0 = 0; e0 < p.experts; e0 += 64) {
@@ -390,10 +400,23 @@ __global__ __launch_bounds__(256, (MxTile<BM, BN>::PER_CU)) void mx4_gemm_kernel
       return -1;
     };
     const int blocks = (int)(p.K >> 5);
-    for (int64_t task = rank;; task += P) {
+    int blocks_of_rows = 0, used = 0;        // of all experts; rows up to the end of the last segment
+    for (int e = lane; e < p.experts; e += 64) {
+      int64_t lo, hi;
+      segment(e, lo, hi);
+      blocks_of_rows += (int)((hi - lo + BM - 1) / BM);
+      used = hi > used ? (int)hi : used;
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) {
+      const int other = __shfl_xor(used, d);
+      used = other > used ? other : used;
+      blocks_of_rows += __shfl_xor(blocks_of_rows, d);
+    }
+    const int64_t total = (int64_t)__builtin_amdgcn_readfirstlane(blocks_of_rows) * p.gn;
+    for (int64_t task = next_task(-1, total); task >= 0; task = next_task(task, total)) {
       int first = 0, gm = 0;
       const int e = __builtin_amdgcn_readfirstlane(find((int)(task / p.gn), first, gm));
-      if (e < 0) break;
       int64_t lo, hi;
       segment(e, lo, hi);
       const int64_t local = task - (int64_t)first * p.gn;
@@ -413,18 +436,7 @@ __global__ __launch_bounds__(256, (MxTile<BM, BN>::PER_CU)) void mx4_gemm_kernel
       t.Bs = p.Bs + (int64_t)e * p.stride_bs;
       mx_block<BM, BN, OB, PAST>(p, t, lds0, wave, lane);
     }
-    // rows of no expert: behind the last segment
-    int used = 0;
-    for (int e = lane; e < p.experts; e += 64) {
-      int64_t lo, hi;
-      segment(e, lo, hi);
-      used = hi > used ? (int)hi : used;
-    }
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) {
-      const int other = __shfl_xor(used, d);
-      used = other > used ? other : used;
-    }
+    // rows of no expert
     for (int64_t r = (int64_t)used + blockIdx.x; r < p.M; r += P)
       for (int64_t c = tid; c < p.N; c += 256) {
         if constexpr (OB) reinterpret_cast<uint16_t*>(p.C)[r * p.ldc + c] = 0;
@@ -435,7 +447,7 @@ __global__ __launch_bounds__(256, (MxTile<BM, BN>::PER_CU)) void mx4_gemm_kernel
     const int groups = MODE == kMxDepth ? p.experts : p.layers;
     const int64_t total = cells * groups;
     const int blocks = (int)((p.K + 31) >> 5);
-    for (int64_t task = rank; task < total; task += P) {
+    for (int64_t task = next_task(-1, total); task >= 0; task = next_task(task, total)) {
       const int g = (int)(task / cells);
       const int cell = load_scalar_i32(p.table + (task - (int64_t)g * cells));
       const int im = cell / p.gn, in = cell - im * p.gn;

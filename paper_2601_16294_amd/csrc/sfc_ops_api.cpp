@@ -34,22 +34,22 @@ struct Mx4Plan {
 };
 
 // Microseconds of `tasks` blocks over `stages` 256-deep stages on the tile kernels, fitted to
-// timings of random operands (M, N from 100 to 14336, K from 1024 to 16384; within 10 %):
+// timings of random operands (M, N from 100 to 14336, K from 1024 to 16384; mostly within 10 %):
 // 256x256 blocks take 1.9 us a stage on a full chip (1.5 on few CUs: the clock), 128x128
-// blocks 0.6 alone on a CU and 1.15 for the two that share one.
-double mx4_tile_us(bool large, int64_t tasks, double stages, int num_cus) {
-  const int64_t slots = large ? num_cus : 2 * (int64_t)num_cus;
-  const double part = (double)(tasks % slots) / (double)slots;
-  double us = (double)(tasks / slots) * (large ? 1.9 * stages + 5.5 : 1.15 * stages + 2.5);
+// blocks 0.6 alone on a CU and 1.15 for the two that share one; then the store of a round.
+double mx4_tile_us(bool large, double tasks, double stages, bool out_f32, int num_cus) {
+  const double slots = large ? num_cus : 2 * num_cus;
+  const double full = (double)(int64_t)(tasks / slots), part = tasks / slots - full;
+  double us = full * (large ? 1.9 * stages + (out_f32 ? 11.0 : 5.5) : 1.15 * stages + (out_f32 ? 4.5 : 2.5));
   if (part > 0) {
-    if (large) us += (1.5 + 0.4 * part) * stages + 2.0 + 3.5 * part;
-    else if (part <= 0.5) us += (0.55 + 0.2 * part) * stages + 0.4 + 2.2 * part;
-    else us += (0.3 + 0.85 * part) * stages + 2.5;
+    if (large) us += (1.5 + 0.4 * part) * stages + 2.0 + (out_f32 ? 9.0 : 3.5) * part;
+    else if (part <= 0.5) us += (0.55 + 0.2 * part) * stages + 0.4 + (out_f32 ? 4.5 : 2.2) * part;
+    else us += (0.3 + 0.85 * part) * stages + (out_f32 ? 4.0 : 2.5);
   }
   return us;
 }
 
-Mx4Plan mx4_plan(int64_t M, int64_t N, int64_t K, int num_cus) {
+Mx4Plan mx4_plan(int64_t M, int64_t N, int64_t K, bool out_f32, int num_cus) {
   Mx4Plan pl;
   if (M <= 16) {
     // (one block of columns to a workgroup and several turns to a wave: no loads ahead to gain.
@@ -73,7 +73,7 @@ Mx4Plan mx4_plan(int64_t M, int64_t N, int64_t K, int num_cus) {
     const int64_t b = large ? 256 : 128, blocks = sfc::ceil_div(M, b) * sfc::ceil_div(N, b);
     const int64_t stages = K > 0 ? sfc::ceil_div(K, 256) : 1;
     for (int c = 1; c <= sfc::kAutoLayers && (c == 1 || 2 * c <= stages); c *= 2) {
-      double us = mx4_tile_us(large, blocks * c, (double)sfc::ceil_div(stages, c), num_cus);
+      double us = mx4_tile_us(large, (double)(blocks * c), (double)sfc::ceil_div(stages, c), out_f32 || c > 1, num_cus);
       if (c > 1) us += 2.5 + 8.0 * (double)c * (double)M * (double)N / 6.0e6;
       if (best == 0 || us < best) {
         best = us;
@@ -188,7 +188,7 @@ int sfc_gemm_mx4_ex(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda,
   int cus = 0;
   int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
-  const Mx4Plan pl = mx4_plan(M, N, K, cus);
+  const Mx4Plan pl = mx4_plan(M, N, K, out_type == SFC_OUT_F32, cus);
   void* ws = nullptr;
   const size_t need = mx4_copies(pl, M, N);
   if (need) rc = sfc::host_workspace(st, need, &ws);
@@ -209,7 +209,7 @@ int sfc_mx4_linear(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, 
   int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
   const int64_t blocks = sfc::mx4_blocks(K), ldq = 16 * blocks, lds = round_up(blocks, 4);
-  const Mx4Plan pl = mx4_plan(M, N, 32 * blocks, cus);
+  const Mx4Plan pl = mx4_plan(M, N, 32 * blocks, out_type == SFC_OUT_F32, cus);
   // Few rows brought to 4 bits by the product's own launch: every workgroup converts them, which
   // costs less than a launch while they or the workgroups are few (us in a graph, both
   // launches against one: 1x4096x4096 7.2 / 5.6, 16x4096x4096 7.4 / 8.0 but 3.5 us less host time,
@@ -253,15 +253,21 @@ int sfc_moe_gemm_mx4_ex(int64_t rows, int64_t N, int64_t K, int experts, const v
                           stride_bs, C, ldc, 0, nullptr, 0, 0, experts, offsets, 1, past_caches(rows * N), nullptr, 0, 0};
   const bool ob = out_type == SFC_OUT_BF16;
   hipError_t e;
-  if (rows <= 32 * (int64_t)experts) {
-    e = sfc::launch_mx4_rows(p, sfc::kMxRows, rows <= 16 * (int64_t)experts ? 1 : 2, false, ob, st);
+  const double stages = (double)sfc::ceil_div(K > 0 ? K : 1, 256);
+  // blocks of rows: every expert's last one is on average half full
+  auto tasks = [&](int64_t b) { return ((double)rows / (double)b + 0.5 * experts) * (double)sfc::ceil_div(N, b); };
+  if (rows <= 32 * (int64_t)experts && experts * sfc::ceil_div(N, 128) < cus) {
+    // Few rows to an expert, and too few blocks of columns to fill the chip (us, the streaming
+    // kernel / 128x128 blocks, 2 rows to an expert: 8 experts 2048x4096 11.1 / 15.2, 4 experts
+    // 4096x4096 10.7 / 15.3; 64 experts 2048x4096 66 / 58, 16 rows to one of 16 experts
+    // 2048x4096 33 / 17: an expert's rows past 16 fm read its weights again)
+    e = sfc::launch_mx4_rows(p, sfc::kMxRows, rows <= 8 * (int64_t)experts ? 1 : 2, false, ob, st);
   } else {
-    const int64_t large = (rows / 256 + experts) * sfc::ceil_div(N, 256);
-    const bool big = rows >= 192 * (int64_t)experts && 2 * large >= cus;
+    const bool big = mx4_tile_us(true, tasks(256), stages, !ob, cus) < mx4_tile_us(false, tasks(128), stages, !ob, cus);
     const int b = big ? 256 : 128;
     p.gn = (int)sfc::ceil_div(N, b);
-    const int64_t tasks = (sfc::ceil_div(rows, b) + experts) * p.gn, slots = big ? cus : 2 * cus;
-    const int grid = (int)(tasks < slots ? tasks : slots);
+    const int64_t most = (sfc::ceil_div(rows, b) + experts) * p.gn, slots = big ? cus : 2 * cus;
+    const int grid = (int)(most < slots ? most : slots);
     e = big ? sfc::launch_mx4_256x256(p, sfc::kMxRows, ob, grid, st) : sfc::launch_mx4_128x128(p, sfc::kMxRows, ob, grid, st);
   }
   return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "experts' 4-bit product");
@@ -282,8 +288,11 @@ int sfc_moe_wgrad_mx4_ex(int64_t M, int64_t N, int64_t rows, int experts, const 
   sfc::Mx4GemmParams p = {M, N, rows, bytes(A), bytes(As), bytes(B), bytes(Bs), lda, ldas, ldb, ldbs, 0, 0, C, ldc,
                           stride_c, nullptr, 0, 0, experts, offsets, 1, past_caches(M * N * experts), nullptr, 0, 0};
   const bool ob = out_type == SFC_OUT_BF16;
-  const int64_t large = sfc::ceil_div(M, 256) * sfc::ceil_div(N, 256) * experts;
-  const bool big = 2 * large >= cus;
+  const double stages = (double)sfc::ceil_div(rows > 0 ? rows : 1, 256 * (int64_t)experts);
+  auto us = [&](int64_t b) {
+    return mx4_tile_us(b == 256, (double)(sfc::ceil_div(M, b) * sfc::ceil_div(N, b) * experts), stages, !ob, cus);
+  };
+  const bool big = us(256) < us(128);
   const int b = big ? 256 : 128;
   p.gm = (int)sfc::ceil_div(M, b);
   p.gn = (int)sfc::ceil_div(N, b);
