@@ -19,7 +19,7 @@ import ctypes
 
 import torch
 
-from paper_2601_16294_amd.sfcgemm import SFC_OUT_BF16, SFC_OUT_F32, SFC_OK, SfcError, _stream_handle, lib
+from paper_2601_16294_amd.sfcgemm import SFC_OUT_BF16, SFC_OUT_F32, SFC_OK, SfcError, lib
 
 __all__ = ["SfcError", "mx4_empty", "sfc_mx4_quant", "sfc_mx4_dequant", "sfc_gemm_mx4_ex", "sfc_mx4_linear",
            "sfc_moe_sort", "sfc_moe_sort_rows", "sfc_moe_dispatch", "sfc_moe_combine", "sfc_moe_combine_grad",
@@ -52,8 +52,16 @@ _declare()
 
 _TYPES = {torch.float32: SFC_OUT_F32, torch.bfloat16: SFC_OUT_BF16}
 _Tensor, _U8, _I32, _F32 = torch.Tensor, torch.uint8, torch.int32, torch.float32
-# (the accessor behind torch.cuda.current_device; a small call is bound by its host time)
+# (the accessors behind torch.cuda.current_device and current_stream; a small call is bound by
+# its host time)
 _current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream(stream):
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(_current()) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
 def _check(code: int, what: str) -> None:
@@ -175,7 +183,7 @@ def sfc_mx4_quant(X, Q=None, S=None, Qt=None, St=None, order=None, topk: int = 1
         raise ValueError(f"{what}: no output")
     a = _mx4(Q, S, "Q", what, rows, cols) if Q is not None else (None, 0, None, 0)
     b = _mx4(Qt, St, "Qt", what, cols, rows) if Qt is not None else (None, 0, None, 0)
-    _check(lib.sfc_mx4_quant(rows, cols, px, ldx, kind, po, x_rows, topk, *a, *b, _stream_handle(stream)), what)
+    _check(lib.sfc_mx4_quant(rows, cols, px, ldx, kind, po, x_rows, topk, *a, *b, _stream(stream)), what)
 
 
 def sfc_mx4_dequant(Q, S, Y, stream=None) -> None:
@@ -183,7 +191,7 @@ def sfc_mx4_dequant(Q, S, Y, stream=None) -> None:
     what = "sfc_mx4_dequant"
     py, ldy, kind = _rows(Y, "Y", what)
     rows, cols = Y.shape
-    _check(lib.sfc_mx4_dequant(rows, cols, *_mx4(Q, S, "Q", what, rows, cols), py, ldy, kind, _stream_handle(stream)),
+    _check(lib.sfc_mx4_dequant(rows, cols, *_mx4(Q, S, "Q", what, rows, cols), py, ldy, kind, _stream(stream)),
            what)
 
 
@@ -195,7 +203,7 @@ def sfc_gemm_mx4_ex(A, As, B, Bs, C, stream=None) -> None:
     if Bs.shape[1] != As.shape[1]:
         raise ValueError(f"{what}: shape mismatch: A {tuple(A.shape)} B {tuple(B.shape)}")
     pc, ldc, kind = _rows(C, "C", what, (M, N))
-    _check(lib.sfc_gemm_mx4_ex(M, N, K, *a, *b, pc, ldc, kind, _stream_handle(stream)), what)
+    _check(lib.sfc_gemm_mx4_ex(M, N, K, *a, *b, pc, ldc, kind, _stream(stream)), what)
 
 
 def sfc_mx4_linear(X, W, Ws, Y, stream=None) -> None:
@@ -207,7 +215,7 @@ def sfc_mx4_linear(X, W, Ws, Y, stream=None) -> None:
     N = W.shape[0]
     w = _mx4(W, Ws, "W", what, N, K)
     py, ldy, out = _rows(Y, "Y", what, (M, N))
-    _check(lib.sfc_mx4_linear(M, N, K, px, ldx, kind, *w, py, ldy, out, _stream_handle(stream)), what)
+    _check(lib.sfc_mx4_linear(M, N, K, px, ldx, kind, *w, py, ldy, out, _stream(stream)), what)
 
 
 def sfc_moe_sort_rows(slots: int, experts: int, align: int = 1) -> int:
@@ -227,7 +235,7 @@ def sfc_moe_sort(ids, offsets, order, pos, align: int = 1, workspace=None, strea
         _tensor(workspace, "workspace", what)
         ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     _check(lib.sfc_moe_sort(slots, offsets.numel() - 1, align, pi, order.numel(), po, pr, pp, ws, ws_bytes,
-                            _stream_handle(stream)), what)
+                            _stream(stream)), what)
 
 
 def sfc_moe_dispatch(X, order, Xs, topk: int = 1, weights=None, stream=None) -> None:
@@ -241,7 +249,7 @@ def sfc_moe_dispatch(X, order, Xs, topk: int = 1, weights=None, stream=None) -> 
     if out != kind:
         raise TypeError(f"{what}: Xs must hold X's type")
     _check(lib.sfc_moe_dispatch(rows, cols, tokens, _topk(topk, what), px, ldx, kind, _ints(order, "order", what, rows),
-                                _weights(weights, what, tokens * topk), ps, lds, _stream_handle(stream)), what)
+                                _weights(weights, what, tokens * topk), ps, lds, _stream(stream)), what)
 
 
 def sfc_moe_combine(Ys, pos, Y, weights=None, stream=None) -> None:
@@ -259,7 +267,7 @@ def sfc_moe_combine(Ys, pos, Y, weights=None, stream=None) -> None:
     slots = pos.numel()
     topk = _slots_per_token(slots, tokens, what)
     _check(lib.sfc_moe_combine(tokens, cols, rows, topk, pr, ldr, kind, _ints(pos, "pos", what, slots),
-                               _weights(weights, what, slots), py, ldy, _stream_handle(stream)), what)
+                               _weights(weights, what, slots), py, ldy, _stream(stream)), what)
 
 
 def _slots_per_token(slots, tokens, what):
@@ -289,7 +297,7 @@ def sfc_moe_combine_grad(dY, Ys, order, pos, weights, dYs, dW, stream=None) -> N
     topk = _slots_per_token(slots, tokens, what)
     _check(lib.sfc_moe_combine_grad(tokens, cols, rows, topk, pd, ldd, pr, ldr, kind, _ints(order, "order", what, rows),
                                     _ints(pos, "pos", what, slots), _weights(weights, what, slots), ps, lds,
-                                    _vector(dW, "dW", what, _F32, slots), _stream_handle(stream)), what)
+                                    _vector(dW, "dW", what, _F32, slots), _stream(stream)), what)
 
 
 def sfc_moe_gemm_mx4_ex(A, As, B, Bs, offsets, C, stream=None) -> None:
@@ -302,7 +310,7 @@ def sfc_moe_gemm_mx4_ex(A, As, B, Bs, offsets, C, stream=None) -> None:
         raise ValueError(f"{what}: shape mismatch: A {tuple(A.shape)} B {tuple(B.shape)}")
     pc, ldc, kind = _rows(C, "C", what, (rows, N))
     _check(lib.sfc_moe_gemm_mx4_ex(rows, N, K, E, *a, b[0], b[1], B.stride(0), b[2], b[3], Bs.stride(0),
-                                   _ints(offsets, "offsets", what, E + 1), pc, ldc, kind, _stream_handle(stream)), what)
+                                   _ints(offsets, "offsets", what, E + 1), pc, ldc, kind, _stream(stream)), what)
 
 
 def sfc_moe_wgrad_mx4_ex(A, As, B, Bs, offsets, C, stream=None) -> None:
@@ -321,4 +329,4 @@ def sfc_moe_wgrad_mx4_ex(A, As, B, Bs, offsets, C, stream=None) -> None:
         raise ValueError(f"{what}: shape mismatch: A {tuple(A.shape)} B {tuple(B.shape)} offsets "
                          f"{tuple(offsets.shape)} C {tuple(C.shape)}")
     pc, ldc, kind = _rows(C[0], "C", what, (M, N))
-    _check(lib.sfc_moe_wgrad_mx4_ex(M, N, rows, E, *a, *b, po, pc, ldc, C.stride(0), kind, _stream_handle(stream)), what)
+    _check(lib.sfc_moe_wgrad_mx4_ex(M, N, rows, E, *a, *b, po, pc, ldc, C.stride(0), kind, _stream(stream)), what)
