@@ -66,15 +66,15 @@ Mx4Plan mx4_plan(int64_t M, int64_t N, int64_t K, bool out_f32, int num_cus) {
     pl.fm = M <= 32 ? 2 : 4;
     return pl;
   }
-  // block shape and layers of the least estimated time; copies are written and read back
-  // (6 bytes a ns) by a second launch (2.5 us)
+  // block shape and layers of the least estimated time; copies are written, and read back by a
+  // second launch (2.5 us and 0.3 a layer), at 6 TB/s
   double best = 0;
   for (int large = 1; large >= 0; --large) {
     const int64_t b = large ? 256 : 128, blocks = sfc::ceil_div(M, b) * sfc::ceil_div(N, b);
     const int64_t stages = K > 0 ? sfc::ceil_div(K, 256) : 1;
     for (int c = 1; c <= sfc::kAutoLayers && (c == 1 || 2 * c <= stages); c *= 2) {
       double us = mx4_tile_us(large, (double)(blocks * c), (double)sfc::ceil_div(stages, c), out_f32 || c > 1, num_cus);
-      if (c > 1) us += 2.5 + 8.0 * (double)c * (double)M * (double)N / 6.0e6;
+      if (c > 1) us += 2.5 + 0.3 * c + 8.0 * (double)c * (double)M * (double)N / 6.0e6;
       if (best == 0 || us < best) {
         best = us;
         pl.large = large != 0;

@@ -80,7 +80,7 @@ def _tensor(t, name, what):
 
 def _rows(t, name, what, shape=None):
     """(pointer, leading dimension, type code) of a 2-D fp32 or bf16 tensor with unit column stride."""
-    if t.__class__ is not _Tensor or t.get_device() != _current():     # (what the checks come to for a good one)
+    if not (t.__class__ is _Tensor and t.is_cuda and t.get_device() == _current()):     # (all that a good one needs)
         _tensor(t, name, what)
     code = _TYPES.get(t.dtype)
     if code is None:
@@ -99,9 +99,8 @@ def _rows(t, name, what, shape=None):
 def _mx4(q, s, name, what, rows=None, cols=None, lead=0):
     """(codes, row bytes, scales, row bytes) of a 4-bit matrix, `lead` dimensions before it.
     Checks the shape against rows x cols where they are given."""
-    cur = _current()
-    if (q.__class__ is not _Tensor or s.__class__ is not _Tensor or q.get_device() != cur
-            or s.get_device() != cur):
+    if not (q.__class__ is _Tensor and s.__class__ is _Tensor and q.is_cuda and s.is_cuda
+            and q.get_device() == s.get_device() == _current()):
         _tensor(q, name, what)
         _tensor(s, f"{name}'s scales", what)
     if q.dtype != _U8 or s.dtype != _U8:
@@ -115,9 +114,9 @@ def _mx4(q, s, name, what, rows=None, cols=None, lead=0):
                          "(16 bytes of codes to a scale)")
     if (dq[-1] != 1 and half > 1) or (ds[-1] != 1 and blocks > 1):
         raise ValueError(f"{what}: {name} and its scales must have unit column stride")
-    if rows is not None and (r != rows or blocks != (cols + 31) // 32):
+    if cols is not None and ((rows is not None and r != rows) or blocks != (cols + 31) // 32):
         raise ValueError(f"{what}: shape mismatch: {name} is {tuple(sq)}, expected "
-                         f"{(rows, 16 * ((cols + 31) // 32))}")
+                         f"{(r if rows is None else rows, 16 * ((cols + 31) // 32))}")
     padded = (blocks + 3) & ~3
     if padded != blocks and q.numel():
         # the last row of scales, too, is read in whole groups of 4
@@ -132,7 +131,7 @@ def _mx4(q, s, name, what, rows=None, cols=None, lead=0):
 
 def _vector(t, name, what, dtype, count):
     """Pointer of a contiguous tensor of `count` elements (None: any number)."""
-    if t.__class__ is not _Tensor or t.get_device() != _current():
+    if not (t.__class__ is _Tensor and t.is_cuda and t.get_device() == _current()):
         _tensor(t, name, what)
     if t.dtype != dtype:
         raise TypeError(f"{what}: {name} must be {str(dtype)[6:]} (got {t.dtype})")
@@ -212,8 +211,8 @@ def sfc_mx4_linear(X, W, Ws, Y, stream=None) -> None:
     what = "sfc_mx4_linear"
     px, ldx, kind = _rows(X, "X", what)
     M, K = X.shape
+    w = _mx4(W, Ws, "W", what, cols=K)
     N = W.shape[0]
-    w = _mx4(W, Ws, "W", what, N, K)
     py, ldy, out = _rows(Y, "Y", what, (M, N))
     _check(lib.sfc_mx4_linear(M, N, K, px, ldx, kind, *w, py, ldy, out, _stream(stream)), what)
 
@@ -227,8 +226,8 @@ def sfc_moe_sort(ids, offsets, order, pos, align: int = 1, workspace=None, strea
     """Slots sorted by expert.  ids (int32, any shape; slot = flat index), offsets
     (experts + 1,), order (at least sfc_moe_sort_rows(...),), pos (as many as ids): int32."""
     what = "sfc_moe_sort"
-    slots = ids.numel()
-    pi, pp = _ints(ids, "ids", what, None), _ints(pos, "pos", what, slots)
+    pi, slots = _ints(ids, "ids", what, None), ids.numel()
+    pp = _ints(pos, "pos", what, slots)
     po, pr = _ints(offsets, "offsets", what, None), _ints(order, "order", what, None)
     ws, ws_bytes = None, 0
     if workspace is not None:
@@ -244,11 +243,11 @@ def sfc_moe_dispatch(X, order, Xs, topk: int = 1, weights=None, stream=None) -> 
     what = "sfc_moe_dispatch"
     px, ldx, kind = _rows(X, "X", what)
     tokens, cols = X.shape
-    rows = order.numel()
+    po, rows = _ints(order, "order", what, None), order.numel()
     ps, lds, out = _rows(Xs, "Xs", what, (rows, cols))
     if out != kind:
         raise TypeError(f"{what}: Xs must hold X's type")
-    _check(lib.sfc_moe_dispatch(rows, cols, tokens, _topk(topk, what), px, ldx, kind, _ints(order, "order", what, rows),
+    _check(lib.sfc_moe_dispatch(rows, cols, tokens, _topk(topk, what), px, ldx, kind, po,
                                 _weights(weights, what, tokens * topk), ps, lds, _stream(stream)), what)
 
 
@@ -264,9 +263,9 @@ def sfc_moe_combine(Ys, pos, Y, weights=None, stream=None) -> None:
         raise ValueError(f"{what}: shape mismatch: Ys {tuple(Ys.shape)} Y {tuple(Y.shape)}")
     if out != kind:
         raise TypeError(f"{what}: Y must hold Ys's type")
-    slots = pos.numel()
+    pp, slots = _ints(pos, "pos", what, None), pos.numel()
     topk = _slots_per_token(slots, tokens, what)
-    _check(lib.sfc_moe_combine(tokens, cols, rows, topk, pr, ldr, kind, _ints(pos, "pos", what, slots),
+    _check(lib.sfc_moe_combine(tokens, cols, rows, topk, pr, ldr, kind, pp,
                                _weights(weights, what, slots), py, ldy, _stream(stream)), what)
 
 
@@ -293,10 +292,10 @@ def sfc_moe_combine_grad(dY, Ys, order, pos, weights, dYs, dW, stream=None) -> N
     ps, lds, ks = _rows(dYs, "dYs", what, (rows, cols))
     if kr != kind or ks != kind:
         raise TypeError(f"{what}: Ys and dYs must hold dY's type")
-    slots = pos.numel()
+    pp, slots = _ints(pos, "pos", what, None), pos.numel()
     topk = _slots_per_token(slots, tokens, what)
     _check(lib.sfc_moe_combine_grad(tokens, cols, rows, topk, pd, ldd, pr, ldr, kind, _ints(order, "order", what, rows),
-                                    _ints(pos, "pos", what, slots), _weights(weights, what, slots), ps, lds,
+                                    pp, _weights(weights, what, slots), ps, lds,
                                     _vector(dW, "dW", what, _F32, slots), _stream(stream)), what)
 
 

@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 import torch
 
+from mx4_cases import DEPTHS, EXPERTS
 from oracle import mx4
 from test_gpu_mx4 import BF16, F32, check, host, inputs, operand
 
@@ -182,20 +183,12 @@ def weights(E, N, K, seed):
     return q, s, [x[2] for x in parts]
 
 
-PRODUCTS = [
-    # rows of every expert (0: none), N, K
-    ([1], 16, 32), ([0, 0, 3], 100, 96), ([2, 1, 0, 5, 16, 17, 0, 1], 333, 544), ([40, 0, 1, 90], 64, 1024),
-    ([70, 200, 0, 129], 200, 160), ([128, 128, 256], 257, 512), ([0, 0, 0], 70, 64), ([1000, 3, 0, 1500], 4100, 288),
-    ([300] * 8, 4096, 160), ([0, 2000, 1], 4096, 1056)]
-
-
 @pytest.mark.parametrize("out", [F32, BF16])
-@pytest.mark.parametrize("counts,N,K", PRODUCTS)
+@pytest.mark.parametrize("counts,N,K", [case for case, _ in EXPERTS])
 @pytest.mark.parametrize("spare", [0, 37])
 def test_experts_product(so, counts, N, K, spare, out):
-    E, rows = len(counts), sum(counts) + spare
-    if rows == 0:
-        spare = rows = 5
+    # (at least the rows that the routing test passes)
+    E, rows = len(counts), max(sum(counts) + spare, 5)
     A, As, a = operand(rows, K, 3)
     B, Bs, b = weights(E, N, K, 50)
     offsets = torch.tensor(np.cumsum([0] + counts), dtype=torch.int32, device="cuda")
@@ -210,9 +203,7 @@ def test_experts_product(so, counts, N, K, spare, out):
 
 
 @pytest.mark.parametrize("out", [F32, BF16])
-@pytest.mark.parametrize("starts,M,N", [
-    ([0, 32], 16, 16), ([0, 0, 64, 64, 96], 130, 70), ([0, 32, 160, 2048], 200, 300), ([0, 96, 96, 800, 1000], 129, 257),
-    ([0, 4096], 100, 60), ([0, 512, 1024, 3136, 4000], 1030, 2050)])
+@pytest.mark.parametrize("starts,M,N", [case for case, _ in DEPTHS])
 def test_weight_gradient(so, starts, M, N, out):
     rows = starts[-1] + 31
     Kp = -(-rows // 32) * 32

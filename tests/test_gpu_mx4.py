@@ -8,6 +8,7 @@ import numpy as np
 import pytest
 import torch
 
+from mx4_cases import PRODUCTS
 from oracle import mx4
 
 pytestmark = pytest.mark.gpu
@@ -188,21 +189,11 @@ def check(C, a, b, K, exact):
     assert ((got - want).abs() <= bound).all()
 
 
-PRODUCTS = [
-    # few rows: every fragment count, odd widths, one turn and many, K ending inside a turn
-    (1, 1, 32), (1, 4096, 4096), (3, 5, 96), (16, 1000, 512), (17, 77, 544), (32, 4100, 1024), (33, 130, 2080),
-    (64, 8192, 480), (64, 16, 32),
-    # 128x128 blocks: edges, short K, layers
-    (65, 1, 32), (65, 200, 128), (128, 128, 160), (129, 257, 512), (300, 500, 1056), (100, 100, 16384),
-    (257, 130, 8224), (1000, 333, 2048),
-    # 256x256 blocks
-    (2049, 4097, 416), (2048, 4096, 1024), (4096, 2050, 2080)]
-
-
 @pytest.mark.parametrize("out", [F32, BF16])
-@pytest.mark.parametrize("M,N,K", PRODUCTS)
+@pytest.mark.parametrize("M,N,K", [shape for shape, _ in PRODUCTS])
 def test_product_exact(so, M, N, K, out):
     # |a b| <= 36 * 4 in steps of 1/4: sums of up to 2^24 / (4 * 144) = 29127 terms are exact
+    assert K <= 29127
     A, As, a = operand(M, K, M + 7 * K)
     B, Bs, b = operand(N, K, N + 3 * K)
     C = torch.full((M, N + 3), 99.0, dtype=out, device="cuda")
@@ -212,7 +203,7 @@ def test_product_exact(so, M, N, K, out):
 
 
 @pytest.mark.parametrize("out", [F32, BF16])
-@pytest.mark.parametrize("M,N,K", [(5, 300, 4096), (64, 64, 1056), (200, 300, 4096), (128, 256, 8192), (2300, 4000, 1024)])
+@pytest.mark.parametrize("M,N,K", [(5, 300, 4096), (16, 4200, 12000 // 32 * 32), (64, 64, 1056), (200, 300, 4096), (128, 256, 8192), (4000, 4090, 3136)])
 def test_product_wide_scales(so, M, N, K, out):
     A, As, a = operand(M, K, 11, 100, 150, 128)
     B, Bs, b = operand(N, K, 12, 100, 150, 256)
@@ -224,7 +215,7 @@ def test_product_wide_scales(so, M, N, K, out):
     assert torch.equal(C, again)
 
 
-@pytest.mark.parametrize("M,N,K", [(4, 70, 1056), (150, 140, 1056), (2300, 4000, 544)])
+@pytest.mark.parametrize("M,N,K", [(4, 70, 1056), (9, 4200, 9056), (20, 70, 1056), (150, 140, 1056), (4000, 4090, 3136)])
 def test_nan_scales_reach_their_row_and_column_only(so, M, N, K):
     A, As, a = operand(M, K, 1)
     B, Bs, b = operand(N, K, 2)
@@ -257,8 +248,8 @@ def test_empty_sums_are_zero(so, M, N):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("M,N,K", [(1, 256, 4096), (16, 100, 77), (50, 333, 2047), (333, 500, 100), (128, 128, 8000),
-                                   (2100, 4100, 520)])
+@pytest.mark.parametrize("M,N,K", [(1, 256, 4096), (16, 100, 77), (9, 300, 2050), (16, 9000, 4000), (3, 200, 4100),
+                                   (50, 333, 2047), (333, 500, 100), (128, 128, 8000), (2100, 4100, 520)])
 def test_linear_is_quantisation_and_product(so, M, N, K, dtype):
     x = inputs(M, K, dtype, 3, K + 5, 1)
     Kp = -(-K // 32) * 32
