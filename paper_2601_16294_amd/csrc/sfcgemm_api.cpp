@@ -688,23 +688,39 @@ int host_error(int code, const char* what) { return set_error(code, what); }
 int host_hip_error(hipError_t e, const char* where) { return hip_fail(e, where); }
 std::mutex& host_mutex() { return g_mu; }
 
+// The maps behind these may run out of host memory: no exception leaves through the C entries.
+template <class F>
+static int no_throw(F f) {
+  try {
+    return f();
+  } catch (...) {
+    return set_error(SFC_ERR_HIP, "out of host memory");
+  }
+}
+
 int host_num_cus(int* num_cus) {
-  DeviceState* st = nullptr;
-  const int rc = device_state(&st);
-  if (rc == SFC_OK) *num_cus = st->num_cus;
-  return rc;
+  return no_throw([&] {
+    DeviceState* st = nullptr;
+    const int rc = device_state(&st);
+    if (rc == SFC_OK) *num_cus = st->num_cus;
+    return rc;
+  });
 }
 
 int host_table(int gm, int gn, hipStream_t stream, const int32_t** table) {
-  DeviceState* st = nullptr;
-  const int rc = device_state(&st);
-  return rc != SFC_OK ? rc : get_table(*st, gm, gn, SFC_ORDER_HILBERT, stream, table);
+  return no_throw([&] {
+    DeviceState* st = nullptr;
+    const int rc = device_state(&st);
+    return rc != SFC_OK ? rc : get_table(*st, gm, gn, SFC_ORDER_HILBERT, stream, table);
+  });
 }
 
 int host_workspace(hipStream_t stream, size_t bytes, void** ws) {
-  DeviceState* st = nullptr;
-  const int rc = device_state(&st);
-  return rc != SFC_OK ? rc : stream_workspace(*st, stream, bytes, ws);
+  return no_throw([&] {
+    DeviceState* st = nullptr;
+    const int rc = device_state(&st);
+    return rc != SFC_OK ? rc : stream_workspace(*st, stream, bytes, ws);
+  });
 }
 
 }  // namespace sfc
