@@ -308,7 +308,7 @@ int sfc_moe_wgrad_mx4_ex(int64_t M, int64_t N, int64_t rows, int experts, const 
 size_t sfc_moe_sort_ws_size(int64_t slots, int experts) {
   if (slots < 0 || slots >= sfc::kMaxDim || experts < 1 || experts > sfc::kMaxExperts) return 0;
   const int64_t chunks = sfc::ceil_div(slots, sfc::kSortChunk);
-  return chunks > 1 ? (size_t)chunks * (size_t)experts * 4u : 0;
+  return chunks > 1 ? (size_t)(chunks > sfc::kSortScan ? chunks + 1 : chunks) * (size_t)experts * 4u : 0;
 }
 
 int sfc_moe_sort(int64_t slots, int experts, int align, const int32_t* ids, int64_t rows, int32_t* offsets,

@@ -79,9 +79,10 @@ struct MoeSortParams {
   const int32_t* ids;
   int64_t rows;              // entries of `order`
   int32_t *offsets, *order, *pos;
-  int32_t* counts;           // [chunks][experts] (more than one chunk)
+  int32_t* counts;           // [chunks (+ 1: sums, past kSortScan)][experts] (more than one chunk)
 };
 constexpr int kSortChunk = 4096;     // slots that one workgroup ranks
+constexpr int kSortScan = 128;       // chunks up to which every workgroup of the sort adds up the counts itself
 hipError_t launch_moe_sort(const MoeSortParams& p, hipStream_t stream);
 
 struct MoeRowsParams {

@@ -53,6 +53,25 @@ def test_sort(so, T, k, E, align, dropped):
     assert all(torch.equal(a, b) for a, b in zip(got, again))
 
 
+# 128 chunks of 4096 slots are the most whose counts every workgroup adds up itself
+@pytest.mark.parametrize("slots,E,align", [(128 * 4096, 70, 1), (128 * 4096 + 1, 70, 32), (700001, 1024, 1), (1000003, 1, 64)])
+def test_sort_of_many_slots(so, slots, E, align):
+    rng = np.random.default_rng(slots)
+    ids = rng.integers(-1, E, (slots, 1)).astype(np.int32)
+    offsets, order, pos = (t.cpu().numpy() for t in sort(so, ids, E, align, extra=3))
+    flat = ids.ravel()
+    counts = np.bincount(flat[flat >= 0], minlength=E)
+    ends = np.cumsum((counts + align - 1) // align * align)
+    assert (offsets == np.concatenate([[0], ends])).all()
+    want = np.full(order.size, -1, dtype=np.int32)
+    for e in range(E):
+        want[offsets[e]:offsets[e] + counts[e]] = np.flatnonzero(flat == e)
+    assert (order == want).all()
+    back = np.full(slots, -1, dtype=np.int32)
+    back[order[order >= 0]] = np.flatnonzero(order >= 0)
+    assert (pos == back).all()
+
+
 def test_sort_of_dropped_slots_only(so):
     ids = np.full((10, 2), -1, dtype=np.int32)
     offsets, order, pos = sort(so, ids, 4, 8)
