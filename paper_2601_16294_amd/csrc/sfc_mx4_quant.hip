@@ -58,7 +58,11 @@ __global__ __launch_bounds__(256) void mx4_quant_rows_kernel(Mx4QuantParams p, R
 // the same read.  A workgroup of 8 waves takes 256 rows x 128 columns: a lane holds 32 rows
 // of two columns in registers, so a column block's maximum needs no other lane, and a row
 // block is 16 lanes.  Codes and scales meet in LDS and leave as 128-byte (64-byte: rows)
-// pieces.
+// pieces.  Stores go through the caches, since a product reads them next: past them this
+// kernel takes 2-3 us less and the weight gradients 14 us more.
+// 8192 x 4096 bf16: 20.3 us (4.2 TB/s), both ways 27.4 (3.75; two calls 38); bounded by memory
+// and, both ways, by a workgroup's phases (load, convert, store) with two workgroups to a CU:
+// three (80 registers) spill and take 36 us.
 constexpr int kQtCols = 128, kQtStride = 144;        // LDS bytes from one column to the next
 
 typedef uint16_t q_u16x2 __attribute__((ext_vector_type(2)));
@@ -66,18 +70,41 @@ typedef uint16_t q_u16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t max16x2(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(q_u16x2, a), __builtin_bit_cast(q_u16x2, b)));
 }
-// The maxima of both halves over the 16 lanes of a row of lanes.
-__device__ __forceinline__ uint32_t row16_max16x2(uint32_t v) {
-  v = max16x2(v, __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, true));      // lanes 1 0 3 2
-  v = max16x2(v, __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, true));      // lanes 2 3 0 1
-  v = max16x2(v, __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, true));     // mirrored in 8
-  return max16x2(v, __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, true));  // mirrored in 16
+// Of 16 words a lane (two rows' maxima each), lane j of a row of 16 lanes is left with the
+// maximum of word row_pair(j) over the row: every step halves the words and doubles the lanes
+// that they cover (60 instructions; the maximum of each word in every lane took 128).
+__device__ __forceinline__ int row_pair(int lane) {
+  return ((lane >> 2) & 1) * 8 + (lane & 1) * 4 + ((lane >> 1) & 1) * 2 + ((lane >> 3) & 1);
+}
+// The lane that holds word i.
+constexpr int row_pair_lane(int i) { return ((i >> 3) & 1) * 4 + ((i >> 2) & 1) + ((i >> 1) & 1) * 2 + (i & 1) * 8; }
+template <int DPP>
+__device__ __forceinline__ void row_halve(uint32_t* m, int n, bool upper) {
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
+    const uint32_t keep = upper ? m[i + n] : m[i], give = upper ? m[i] : m[i + n];
+    m[i] = max16x2(keep, __builtin_amdgcn_update_dpp(0, give, DPP, 0xF, 0xF, true));
+  }
+}
+__device__ __forceinline__ uint32_t row_maxima(uint32_t (&m)[16], int lane) {
+  row_halve<0x141>(m, 8, lane & 4);      // lanes mirrored in 8
+  row_halve<0xB1>(m, 4, lane & 1);       // lanes 1 0 3 2
+  row_halve<0x4E>(m, 2, lane & 2);       // lanes 2 3 0 1
+  row_halve<0x128>(m, 1, lane & 8);      // lanes 8 further in 16
+  return m[0];
+}
+// Word I's value in every lane of the row.
+template <int I>
+__device__ __forceinline__ uint32_t row_word(uint32_t v) {
+  return __builtin_amdgcn_update_dpp(0, v, 0x150 + row_pair_lane(I), 0xF, 0xF, true);
 }
 // Scale code from the upper 16 bits of the largest magnitude (its exponent field is all that counts).
 __device__ __forceinline__ uint32_t scale_code16(uint32_t top) { return scale_code(top << 16); }
 
 template <bool BF16, bool BOTH>
 __global__ __launch_bounds__(512, 4) void mx4_quant_cols_kernel(Mx4QuantParams p, int row_groups) {
+  // column 2 i + k of the block lies in place 64 k + i: lanes that write neighbouring even (odd)
+  // columns meet 36 banks apart
   __shared__ __attribute__((aligned(16))) uint8_t codes[kQtCols * kQtStride];
   __shared__ __attribute__((aligned(16))) uint8_t scales[kQtCols * 8];
   __shared__ __attribute__((aligned(16))) uint32_t row_codes[BOTH ? 64 * 64 : 4];    // [4 rows][2 columns]: a byte a row
@@ -85,7 +112,11 @@ __global__ __launch_bounds__(512, 4) void mx4_quant_cols_kernel(Mx4QuantParams p
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col_groups = gridDim.x / (unsigned)row_groups;
-  const int rg = blockIdx.x / (unsigned)col_groups, cb = blockIdx.x - rg * col_groups;
+  // BOTH: two neighbouring column blocks, whose 64-byte pieces of rows make a line, go to one XCD
+  // (8192 x 4096 bf16: 27.4 us, neighbours on different ones 28.9)
+  unsigned task = blockIdx.x;
+  if (BOTH && task < (gridDim.x & ~15u)) task = (task & ~15u) + 2 * (task & 7) + ((task >> 3) & 1);
+  const int rg = task / (unsigned)col_groups, cb = task - rg * col_groups;
   const int64_t c0 = (int64_t)cb * kQtCols, c = c0 + 2 * lane;
   const int64_t r0 = (int64_t)rg * 256 + 32 * wave;
   // the wave's 32 source rows (-1: zeros), all loads before any use
@@ -104,13 +135,14 @@ __global__ __launch_bounds__(512, 4) void mx4_quant_cols_kernel(Mx4QuantParams p
 #pragma unroll
   for (int i = 0; i < 32; ++i) raw[0][i] = raw[BF16 ? 0 : 1][i] = 0;
   if (p.x_rows > 0 && c < p.cols) {
-    const char* x = reinterpret_cast<const char*>(p.X) + c * ES;
+    const char* x = reinterpret_cast<const char*>(p.X) + c0 * ES;
+    const uint32_t off = 2 * lane * ES;
     if (c + 1 < p.cols) {
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
         const int r = __builtin_amdgcn_readlane(source, i);
         struct __attribute__((packed, aligned(ES))) Pair { uint32_t v[BF16 ? 1 : 2]; };
-        const Pair w = *reinterpret_cast<const Pair*>(x + (int64_t)(r < 0 ? 0 : r) * p.ldx * ES);
+        const Pair w = *reinterpret_cast<const Pair*>(x + (int64_t)(r < 0 ? 0 : r) * p.ldx * ES + off);
         raw[0][i] = w.v[0];
         if constexpr (!BF16) raw[1][i] = w.v[1];
       }
@@ -118,87 +150,115 @@ __global__ __launch_bounds__(512, 4) void mx4_quant_cols_kernel(Mx4QuantParams p
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
         const int r = __builtin_amdgcn_readlane(source, i);
-        const char* e = x + (int64_t)(r < 0 ? 0 : r) * p.ldx * ES;
+        const char* e = x + (int64_t)(r < 0 ? 0 : r) * p.ldx * ES + off;
         raw[0][i] = BF16 ? *reinterpret_cast<const uint16_t*>(e) : *reinterpret_cast<const uint32_t*>(e);
       }
     }
   }
+  if (__ballot(source < 0) & 0xFFFFFFFFull) {
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    const bool zero = __builtin_amdgcn_readlane(source, i) < 0;
+    for (int i = 0; i < 32; ++i) {
+      const bool zero = __builtin_amdgcn_readlane(source, i) < 0;
 #pragma unroll
-    for (int k = 0; k < (BF16 ? 1 : 2); ++k) raw[k][i] = zero ? 0u : raw[k][i];
+      for (int k = 0; k < (BF16 ? 1 : 2); ++k) raw[k][i] = zero ? 0u : raw[k][i];
+    }
   }
-  // row i of column k as fp32, and the upper halves of the row's magnitudes
-  auto value = [&](int k, int i) {
-    return __builtin_bit_cast(float, !BF16 ? raw[BF16 ? 0 : k][i] : k ? raw[0][i] & 0xFFFF0000u : raw[0][i] << 16);
+  // rows 2 i and 2 i + 1 of column k: the values as bf16 (the upper halves of fp32)
+  auto upper = [&](int k, int i) {
+    return __builtin_amdgcn_perm(raw[BF16 ? 0 : k][2 * i + 1], raw[BF16 ? 0 : k][2 * i], BF16 && k == 0 ? 0x05040100u : 0x07060302u);
   };
-  auto mag = [&](int i) {
-    return (BF16 ? raw[0][i] : (raw[0][i] >> 16) | (raw[BF16 ? 0 : 1][i] & 0xFFFF0000u)) & 0x7FFF7FFFu;
-  };
-  uint32_t top = 0;
+  // rows 2 i and 2 i + 1 of column k, or both columns of row i, to codes: byte n of q
+#define SFC_CVT_COL(q, k, i, n)                                                                                        \
+  q = BF16 ? __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(qbf16x2, upper(k, i)), scale, n)          \
+           : __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, __builtin_bit_cast(float, raw[BF16 ? 0 : k][2 * (i)]),        \
+                                                      __builtin_bit_cast(float, raw[BF16 ? 0 : k][2 * (i) + 1]), scale, n)
+#define SFC_CVT_ROW(q, i, scale, n)                                                                                    \
+  q = BF16 ? __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(qbf16x2, raw[0][i]), scale, n)            \
+           : __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, __builtin_bit_cast(float, raw[0][i]),                         \
+                                                      __builtin_bit_cast(float, raw[BF16 ? 0 : 1][i]), scale, n)
+  uint32_t rows2[16], top[2] = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 32; ++i) top = max16x2(top, mag(i));
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t a = upper(0, i) & 0x7FFF7FFFu, b = upper(1, i) & 0x7FFF7FFFu;
+    top[0] = max16x2(top[0], a);
+    top[1] = max16x2(top[1], b);
+    rows2[i] = max16x2(a, b);
+  }
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    const uint32_t sc = scale_code16(k ? top >> 16 : top & 0xFFFFu);
+    const uint32_t t = max16x2(top[k], top[k] >> 16);
+    const uint32_t sc = scale_code16(t & 0xFFFFu);
     const float scale = scale_value(sc);
     row_u32x4 q;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       uint32_t o = 0;
-#define SFC_CVT(n)                                                                                                  \
-  o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, value(k, 8 * w + 2 * n), value(k, 8 * w + 2 * n + 1), scale, n)
-      SFC_CVT(0);
-      SFC_CVT(1);
-      SFC_CVT(2);
-      SFC_CVT(3);
-#undef SFC_CVT
+      SFC_CVT_COL(o, k, 4 * w, 0);
+      SFC_CVT_COL(o, k, 4 * w + 1, 1);
+      SFC_CVT_COL(o, k, 4 * w + 2, 2);
+      SFC_CVT_COL(o, k, 4 * w + 3, 3);
       q[w] = o;
     }
-    *reinterpret_cast<row_u32x4*>(codes + (2 * lane + k) * kQtStride + 16 * wave) = q;
-    scales[(2 * lane + k) * 8 + wave] = (uint8_t)sc;
+    *reinterpret_cast<row_u32x4*>(codes + (64 * k + lane) * kQtStride + 16 * wave) = q;
+    scales[(64 * k + lane) * 8 + wave] = (uint8_t)sc;
   }
   if constexpr (BOTH) {
-#pragma unroll
-    for (int i = 0; i < 32; i += 4) {
-      uint32_t q = 0;
-#pragma unroll
-      for (int u = 0; u < 4; u += 2) {
-        // the two rows' maxima over the lane's columns, then over 16 lanes
-        const uint32_t a = mag(i + u), b = mag(i + u + 1);
-        const uint32_t m = row16_max16x2(max16x2((a & 0xFFFFu) | (b << 16), (a >> 16) | (b & 0xFFFF0000u)));
-        const uint32_t s0 = scale_code16(m & 0xFFFFu), s1 = scale_code16(m >> 16);
-        // (the conversion's byte selector is a constant)
-        const float x0 = value(0, i + u), y0 = value(1, i + u), x1 = value(0, i + u + 1), y1 = value(1, i + u + 1);
-        if (u == 0) {
-          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x0, y0, scale_value(s0), 0);
-          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x1, y1, scale_value(s1), 1);
-        } else {
-          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x0, y0, scale_value(s0), 2);
-          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, x1, y1, scale_value(s1), 3);
-        }
-        if ((lane & 15) == 0) {
-          row_scales[(32 * wave + i + u) * 4 + (lane >> 4)] = (uint8_t)s0;
-          row_scales[(32 * wave + i + u + 1) * 4 + (lane >> 4)] = (uint8_t)s1;
-        }
-      }
-      row_codes[(8 * wave + i / 4) * 64 + lane] = q;
-    }
+    // a lane makes the scales of two rows, whose upper halves (all that is not 0 in them) the
+    // others take from it
+    const uint32_t m = row_maxima(rows2, lane);
+    const uint32_t s0 = scale_code16(m & 0xFFFFu), s1 = scale_code16(m >> 16);
+    const int row = 32 * wave + 2 * row_pair(lane);
+    row_scales[row * 4 + (lane >> 4)] = (uint8_t)s0;
+    row_scales[(row + 1) * 4 + (lane >> 4)] = (uint8_t)s1;
+    const uint32_t both = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, scale_value(s1)),
+                                                __builtin_bit_cast(uint32_t, scale_value(s0)), 0x07060302u);
+    uint32_t* out = row_codes + 8 * wave * 64 + lane;
+#define SFC_FOUR_ROWS(w)                                                         \
+  {                                                                              \
+    const uint32_t sa = row_word<2 * w>(both), sb = row_word<2 * w + 1>(both);   \
+    uint32_t q = 0;                                                              \
+    SFC_CVT_ROW(q, 4 * w, __builtin_bit_cast(float, sa << 16), 0);               \
+    SFC_CVT_ROW(q, 4 * w + 1, __builtin_bit_cast(float, sa & 0xFFFF0000u), 1);   \
+    SFC_CVT_ROW(q, 4 * w + 2, __builtin_bit_cast(float, sb << 16), 2);           \
+    SFC_CVT_ROW(q, 4 * w + 3, __builtin_bit_cast(float, sb & 0xFFFF0000u), 3);   \
+    out[w * 64] = q;                                                             \
   }
+    SFC_FOUR_ROWS(0)
+    SFC_FOUR_ROWS(1)
+    SFC_FOUR_ROWS(2)
+    SFC_FOUR_ROWS(3)
+    SFC_FOUR_ROWS(4)
+    SFC_FOUR_ROWS(5)
+    SFC_FOUR_ROWS(6)
+    SFC_FOUR_ROWS(7)
+#undef SFC_FOUR_ROWS
+  }
+#undef SFC_CVT_COL
+#undef SFC_CVT_ROW
   __syncthreads();
   const int64_t blocks = (p.rows + 31) >> 5, b0 = (int64_t)rg * 8;
+#pragma unroll
   for (int i = tid; i < kQtCols * 8; i += 512) {
-    const int col = i >> 3, b = i & 7;
+    const int col = i >> 3, b = i & 7, place = 64 * (col & 1) + (col >> 1);
     if (c0 + col < p.cols && b0 + b < blocks) {
       *reinterpret_cast<row_u32x4*>(p.Qt + (c0 + col) * p.ldqt + (b0 + b) * 16) =
-          *reinterpret_cast<const row_u32x4*>(codes + col * kQtStride + 16 * b);
-      p.St[(c0 + col) * p.ldst + b0 + b] = scales[col * 8 + b];
+          *reinterpret_cast<const row_u32x4*>(codes + place * kQtStride + 16 * b);
+    }
+  }
+  if (tid < kQtCols && c0 + tid < p.cols) {
+    const uint8_t* from = scales + (64 * (tid & 1) + (tid >> 1)) * 8;
+    uint8_t* to = p.St + (c0 + tid) * p.ldst + b0;
+    if (b0 + 8 <= blocks) {
+      reinterpret_cast<uint32_t*>(to)[0] = reinterpret_cast<const uint32_t*>(from)[0];
+      reinterpret_cast<uint32_t*>(to)[1] = reinterpret_cast<const uint32_t*>(from)[1];
+    } else {
+      for (int b = 0; b0 + b < blocks; ++b) to[b] = from[b];
     }
   }
   if constexpr (BOTH) {
     const int64_t row_blocks = (p.cols + 31) >> 5, cb0 = c0 >> 5, top_row = (int64_t)rg * 256;
-    // a thread takes a block of four rows: 16 words of a byte per row, turned into 4 x 16 bytes
+    // half of the threads take a block of four rows each: 16 words of a byte per row, turned into
+    // 4 x 16 bytes; the others a row's scales
     if (tid < 256) {
       const int quad = tid >> 2, b = tid & 3;
       row_u32x4 in[4], out[4];
@@ -218,12 +278,16 @@ __global__ __launch_bounds__(512, 4) void mx4_quant_cols_kernel(Mx4QuantParams p
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int r = 4 * quad + u;
-          if (top_row + r < p.rows) {
+          if (top_row + r < p.rows)
             *reinterpret_cast<row_u32x4*>(p.Q + (top_row + r) * p.ldq + (cb0 + b) * 16) = out[u];
-            p.S[(top_row + r) * p.lds + cb0 + b] = row_scales[r * 4 + b];
-          }
         }
       }
+    } else if (top_row + tid - 256 < p.rows) {
+      const uint8_t* from = row_scales + (tid - 256) * 4;
+      uint8_t* to = p.S + (top_row + tid - 256) * p.lds + cb0;
+      if (cb0 + 4 <= row_blocks) *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
+      else
+        for (int b = 0; cb0 + b < row_blocks; ++b) to[b] = from[b];
     }
   }
 }
