@@ -79,7 +79,7 @@ struct MxTask {
   int64_t a_row, b_row;        // first row of A and of B
   int64_t c_row;               // first row of C (relative to C)
   int m_valid, n_valid;        // rows of A and of B inside the matrix
-  int64_t block0;              // first block of K (a multiple of 4), with `lo` blocks to skip
+  int64_t block0;              // first block of K (a multiple of 8), with `lo` blocks to skip
   int lo, hi;                  // blocks lo .. hi-1 from block0 count
   const uint8_t *B, *Bs;
   char* C;
@@ -474,7 +474,7 @@ __global__ __launch_bounds__(256, (MxTile<BM, BN>::PER_CU)) void mx4_gemm_kernel
         b1 = units * (g + 1) / groups * 16;
         if (b1 > blocks) b1 = blocks;
       }
-      t.block0 = b0 & ~(int64_t)3;
+      t.block0 = b0 & ~(int64_t)7;     // whole 128-byte lines of codes
       t.lo = (int)(b0 - t.block0);
       t.hi = (int)(b1 - t.block0);
       if (b1 == b0) t.hi = t.lo = 0;
@@ -492,8 +492,8 @@ static const void* mx4_kernel(Mx4Mode mode) {
 
 template <int BM, int BN>
 static hipError_t mx4_launch(const Mx4GemmParams& p, Mx4Mode mode, bool out_bf16, int grid, hipStream_t stream) {
-  const void* k = !out_bf16 ? mx4_kernel<BM, BN, false, false>(mode)
-                  : p.past  ? mx4_kernel<BM, BN, true, true>(mode) : mx4_kernel<BM, BN, true, false>(mode);
+  const void* k = out_bf16 ? (p.past ? mx4_kernel<BM, BN, true, true>(mode) : mx4_kernel<BM, BN, true, false>(mode))
+                           : (p.past ? mx4_kernel<BM, BN, false, true>(mode) : mx4_kernel<BM, BN, false, false>(mode));
   Mx4GemmParams local = p;
   void* args[] = {&local};
   return hipLaunchKernel(k, dim3((unsigned)grid), dim3(256), args, 0, stream);

@@ -20,10 +20,11 @@ hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 const uint8_t* bytes(const void* p) { return static_cast<const uint8_t*>(p); }
 int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
-// Whether a bf16 C of so many elements goes past the caches: 32 MB, as for the row operators
-// (4096x4096x1024 18.7 -> 17.3 us, 4096x14336x4096 141 -> 139, and what is read next is still
-// cached; fp32 loses as much as it gains: 4096x4096x4096 44.1, 44.4).
-bool past_caches(int64_t elements) { return elements >= (int64_t)16 << 20; }
+// Whether a C of so many elements goes past the caches: from 32 MB on, as for the row operators
+// (us, through / past: bf16 4096x4096x1024 18.7 / 17.3, 4096x14336x4096 141 / 139; fp32
+// 2048x4096x1024 14.7 / 12.9, 4096x14336x1024 77.7 / 67.4, 8192^3 276 / 268, the weight gradients of
+// 8 experts 2048x4096 with 8192 rows 113 / 89), and what is read next is still cached.
+bool past_caches(int64_t elements, int out_type) { return elements * (out_type == SFC_OUT_BF16 ? 2 : 4) >= (int64_t)32 << 20; }
 
 // How a dense product runs.
 struct Mx4Plan {
@@ -110,6 +111,7 @@ int mx4_dense(const Mx4Plan& pl, sfc::Mx4GemmParams& p, bool ob, int num_cus, fl
     p.C = copies;
     p.ldc = p.N;
     p.stride_c = p.M * p.N;
+    p.past = false;                    // (read next)
   }
   const int64_t tasks = (int64_t)p.gm * p.gn * pl.layers, slots = pl.large ? num_cus : 2 * num_cus;
   const int grid = (int)(tasks < slots ? tasks : slots);
@@ -194,7 +196,7 @@ int sfc_gemm_mx4_ex(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda,
   if (need) rc = sfc::host_workspace(st, need, &ws);
   if (rc != SFC_OK) return rc;
   sfc::Mx4GemmParams p = {M, N, K, bytes(A), bytes(As), bytes(B), bytes(Bs), lda, ldas, ldb, ldbs, 0, 0, C, ldc, 0,
-                          nullptr, 0, 0, 0, nullptr, 1, past_caches(M * N), nullptr, 0, 0};
+                          nullptr, 0, 0, 0, nullptr, 1, past_caches(M * N, out_type), nullptr, 0, 0};
   return mx4_dense(pl, p, out_type == SFC_OUT_BF16, cus, static_cast<float*>(ws), st);
 }
 
@@ -233,7 +235,7 @@ int sfc_mx4_linear(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, 
     if (rc != SFC_OK) return rc;
   }
   sfc::Mx4GemmParams p = {M, N, 32 * blocks, q, q + code_bytes, bytes(W), bytes(Ws), ldq, lds, ldw, ldws, 0, 0, Y, ldy,
-                          0, nullptr, 0, 0, 0, nullptr, 1, past_caches(M * N), nullptr, 0, 0};
+                          0, nullptr, 0, 0, 0, nullptr, 1, past_caches(M * N, out_type), nullptr, 0, 0};
   return mx4_dense(pl, p, out_type == SFC_OUT_BF16, cus, reinterpret_cast<float*>(q + code_bytes + scale_bytes), st);
 }
 
@@ -250,7 +252,7 @@ int sfc_moe_gemm_mx4_ex(int64_t rows, int64_t N, int64_t K, int experts, const v
   const int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
   sfc::Mx4GemmParams p = {rows, N, K, bytes(A), bytes(As), bytes(B), bytes(Bs), lda, ldas, ldb, ldbs, stride_b,
-                          stride_bs, C, ldc, 0, nullptr, 0, 0, experts, offsets, 1, past_caches(rows * N), nullptr, 0, 0};
+                          stride_bs, C, ldc, 0, nullptr, 0, 0, experts, offsets, 1, past_caches(rows * N, out_type), nullptr, 0, 0};
   const bool ob = out_type == SFC_OUT_BF16;
   hipError_t e;
   const double stages = (double)sfc::ceil_div(K > 0 ? K : 1, 256);
@@ -286,7 +288,7 @@ int sfc_moe_wgrad_mx4_ex(int64_t M, int64_t N, int64_t rows, int experts, const 
   int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
   sfc::Mx4GemmParams p = {M, N, rows, bytes(A), bytes(As), bytes(B), bytes(Bs), lda, ldas, ldb, ldbs, 0, 0, C, ldc,
-                          stride_c, nullptr, 0, 0, experts, offsets, 1, past_caches(M * N * experts), nullptr, 0, 0};
+                          stride_c, nullptr, 0, 0, experts, offsets, 1, past_caches(M * N * experts, out_type), nullptr, 0, 0};
   const bool ob = out_type == SFC_OUT_BF16;
   const double stages = (double)sfc::ceil_div(rows > 0 ? rows : 1, 256 * (int64_t)experts);
   auto us = [&](int64_t b) {
