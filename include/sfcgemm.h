@@ -389,10 +389,12 @@ int sfc_mx4_dequant(int64_t rows, int64_t cols,
  * sfc_gemm_mx4_ex -- C = A * B^T, A (M x K) and B (N x K) in 4 bits, both with their
  * blocks along K; C fp32 or bf16 (rounded to nearest even from the fp32 sums).
  *   K          a multiple of 32 (SFC_ERR_INVALID_ARG otherwise); K == 0: C = 0.
- * Products and block sums are exact, sums of blocks fp32.  Up to 64 rows run on a
- * kernel that streams B once; the others on 256x256 or 128x128 blocks along the curve,
- * K in up to 16 layers where that fills the chip (copies in library memory, as for
- * sfc_gemm).  The choice depends on M, N and K alone, so equal calls give equal bits.
+ * Products and block sums are exact, sums of blocks fp32.  Few rows run on kernels that
+ * stream B once: up to 16 with A in registers while K <= 8192 (16384 where N is large),
+ * and up to 64 while K <= 4096.  The others run on 256x256 or 128x128 blocks along the
+ * curve, K in up to 16 layers where an estimate of the time favours it (copies in
+ * library memory, as for sfc_gemm).  The choice depends on M, N, K and out_type alone, so
+ * equal calls give equal bits.
  * The gradients of C = A * B^T are two such calls: dA = dC * B with dC's blocks along N
  * and the transposed B (Qt of sfc_mx4_quant), dB = dC^T * A with both transposed.
  */
@@ -404,8 +406,9 @@ int sfc_gemm_mx4_ex(int64_t M, int64_t N, int64_t K,
 /*
  * sfc_mx4_linear -- Y = X * W^T with X (M x K, fp32 or bf16) brought to 4 bits within the
  * call and W (N x K) kept in 4 bits.  K is the row length of X, W's rows hold
- * ceil(K/32) blocks; the result is that of sfc_mx4_quant and sfc_gemm_mx4_ex.  X's codes
- * lie in library memory, one per stream, as layer copies do.
+ * ceil(K/32) blocks; the result is that of sfc_mx4_quant and sfc_gemm_mx4_ex.  Up to 16
+ * rows may be converted by the product's own launch; otherwise X's codes lie in library
+ * memory, one per stream, as layer copies do.
  */
 int sfc_mx4_linear(int64_t M, int64_t N, int64_t K,
                    const void *X, int64_t ldx, int in_type,
@@ -468,7 +471,8 @@ int sfc_moe_combine_grad(int64_t tokens, int64_t cols, int64_t rows, int topk,
 
 /*
  * sfc_moe_gemm_mx4_ex -- C[p] = A[p] * B[e]^T for the rows p of every expert e; rows behind
- * the last segment are set to 0.  A rows x K, B `experts` matrices of N x K that lie
+ * the last segment are set to 0 (sfc_moe_sort's offsets start at 0; rows before a first
+ * segment that starts later are not written).  A rows x K, B `experts` matrices of N x K that lie
  * stride_b (codes) and stride_bs (scales) bytes apart, multiples of 16 and 4; K a multiple
  * of 32.  The same call with the transposed weights gives the gradient of A.  The kernel
  * and its block shape are chosen from rows, N, K and experts; segment lengths are read

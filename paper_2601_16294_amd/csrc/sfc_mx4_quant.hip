@@ -8,7 +8,9 @@
 // to the even code, at most 6 in magnitude: the conversion instruction does the
 // scaling, rounding and saturation (subnormal inputs and the scale 2^-127 included).
 //
-// Bound: memory.  Every value is read once, 17/32 byte written.
+// Bound: memory.  Every value is read once, 17/32 byte written.  8192 x 4096 bf16: along the
+// rows 17.5 us (4.8 TB/s), back 13.4 (6.3; the codes are still cached); a copy of as many
+// values 25.9 (5.2).
 #include "sfc_ops_params.h"
 #include "sfc_mx4_convert.h"
 

@@ -1,5 +1,7 @@
 // Products of few rows with 4-bit weights, C = A B^T (a decode step's tokens, or the few
-// rows of each expert): the calls whose time is one read of B.
+// rows of each expert): the calls whose time is one read of B.  16x14336x4096: 9.0 us
+// (3.5 TB/s: 2 us of launch and the first loads' way, then 31 MB), 16x16384x16384 26.8 (5.3,
+// about the rate at which memory is read here at best).
 //
 // A workgroup computes 16*FN columns (rows of B) for 16*FM rows of A at a time.  Its waves
 // deal K out between them, 512 values a turn: a turn reads 256 bytes of codes and 16 bytes
