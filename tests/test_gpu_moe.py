@@ -239,6 +239,21 @@ def test_weight_gradient(so, starts, M, N, out):
         check(C[e, :M, 1:1 + N], a[:, lo:hi], b[:, lo:hi], max(hi - lo, 1), True)
 
 
+@pytest.mark.parametrize("out", [F32, BF16])
+def test_large_weight_gradients_of_short_segments(so, out):
+    # 128x128 blocks whose output (33.6 and 34.6 MB) is stored past the caches, segments starting
+    # at every eighth of a stage
+    E, M, N = (20, 600, 700) if out == F32 else (40, 601, 720)
+    starts = np.cumsum([0] + [32 * (1 + 5 * e % 11) for e in range(E)])
+    A, As, a = operand(M, int(starts[-1]), 5)
+    B, Bs, b = operand(N, int(starts[-1]), 6)
+    C = torch.full((E, M, N + 3), 99.0, dtype=out, device="cuda")
+    so.sfc_moe_wgrad_mx4_ex(A, As, B, Bs, torch.tensor(starts, dtype=torch.int32, device="cuda"), C[:, :, 2:2 + N])
+    assert (C[:, :, :2] == 99).all() and (C[:, :, 2 + N:] == 99).all()
+    for e in range(E):
+        check(C[e, :, 2:2 + N], a[:, starts[e]:starts[e + 1]], b[:, starts[e]:starts[e + 1]], int(starts[e + 1] - starts[e]), True)
+
+
 def test_offsets_outside_the_rows_are_cut(so):
     A, As, a = operand(100, 64, 1)
     B, Bs, b = weights(3, 40, 64, 2)
