@@ -21,6 +21,11 @@ import torch
 
 from paper_2601_16294_amd.sfcgemm import SFC_OUT_BF16, SFC_OUT_F32, SFC_OK, SfcError, lib
 
+try:
+    from paper_2601_16294_amd import _sfcargs
+except ImportError as e:
+    raise ImportError("paper_2601_16294_amd/_sfcargs.so is not built; run `python -m paper_2601_16294_amd.build`") from e
+
 __all__ = ["SfcError", "mx4_empty", "sfc_mx4_quant", "sfc_mx4_dequant", "sfc_gemm_mx4_ex", "sfc_mx4_linear",
            "sfc_moe_sort", "sfc_moe_sort_rows", "sfc_moe_dispatch", "sfc_moe_combine", "sfc_moe_combine_grad",
            "sfc_moe_gemm_mx4_ex", "sfc_moe_wgrad_mx4_ex"]
@@ -58,6 +63,12 @@ _current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_devi
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+# Each gives what the function of its name below gives where the argument is as it should be, else
+# None: the code behind it then names the fault.
+_rows_of, _mx4_of, _vector_of, _empty_of = _sfcargs.rows, _sfcargs.mx4, _sfcargs.vector, _sfcargs.empty
+_ANY = (-1, -1)
+
+
 def _stream(stream):
     if stream is not None:
         return stream.cuda_stream
@@ -80,8 +91,10 @@ def _tensor(t, name, what):
 
 def _rows(t, name, what, shape=None):
     """(pointer, leading dimension, type code) of a 2-D fp32 or bf16 tensor with unit column stride."""
-    if not (t.__class__ is _Tensor and t.is_cuda and t.get_device() == _current()):     # (all that a good one needs)
-        _tensor(t, name, what)
+    got = _rows_of(t, *(shape or _ANY))
+    if got is not None:
+        return got
+    _tensor(t, name, what)
     code = _TYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"{what}: {name} must be float32 or bfloat16 (got {t.dtype})")
@@ -99,10 +112,14 @@ def _rows(t, name, what, shape=None):
 def _mx4(q, s, name, what, rows=None, cols=None, lead=0):
     """(codes, row bytes, scales, row bytes) of a 4-bit matrix, `lead` dimensions before it.
     Checks the shape against rows x cols where they are given."""
-    if not (q.__class__ is _Tensor and s.__class__ is _Tensor and q.is_cuda and s.is_cuda
-            and q.get_device() == s.get_device() == _current()):
-        _tensor(q, name, what)
-        _tensor(s, f"{name}'s scales", what)
+    if cols is None:
+        got = _mx4_of(q, s, lead, -1, -1)
+    else:
+        got = _mx4_of(q, s, lead, -1 if rows is None else rows, (cols + 31) // 32)
+    if got is not None:
+        return got
+    _tensor(q, name, what)
+    _tensor(s, f"{name}'s scales", what)
     if q.dtype != _U8 or s.dtype != _U8:
         raise TypeError(f"{what}: {name} and its scales must be uint8 (got {q.dtype} and {s.dtype})")
     sq, ss, dq, ds = q.shape, s.shape, q.stride(), s.stride()
@@ -131,8 +148,10 @@ def _mx4(q, s, name, what, rows=None, cols=None, lead=0):
 
 def _vector(t, name, what, dtype, count):
     """Pointer of a contiguous tensor of `count` elements (None: any number)."""
-    if not (t.__class__ is _Tensor and t.is_cuda and t.get_device() == _current()):
-        _tensor(t, name, what)
+    got = _vector_of(t, dtype is _F32, -1 if count is None else count)
+    if got is not None:
+        return got
+    _tensor(t, name, what)
     if t.dtype != dtype:
         raise TypeError(f"{what}: {name} must be {str(dtype)[6:]} (got {t.dtype})")
     if not t.is_contiguous():
@@ -158,6 +177,10 @@ def _topk(topk, what):
 
 def mx4_empty(rows: int, cols: int, lead=(), device="cuda"):
     """Uninitialised (codes, scales) of a rows x cols 4-bit matrix (or of `lead` such matrices)."""
+    if lead == () and device == "cuda":
+        got = _empty_of(rows, cols)
+        if got is not None:
+            return got
     b = (cols + 31) // 32
     padded = (b + 3) & ~3
     codes = torch.empty((*lead, rows, 16 * b), dtype=_U8, device=device)
