@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256) void mx4_quant_rows_kernel(Mx4QuantParams p, R
 }
 
 // Blocks along the columns, the result transposed, and (BOTH) blocks along the rows from
-// the same read.  A workgroup of 8 waves takes 256 rows x 128 columns: a lane holds 32 rows
+// the same read.  A workgroup of W = 8 (4) waves takes 256 (128) rows x 128 columns: a lane holds 32 rows
 // of two columns in registers, so a column block's maximum needs no other lane, and a row
 // block is 16 lanes.  Codes and scales meet in LDS and leave as 128-byte (64-byte: rows)
 // pieces.  Stores go through the caches, since a product reads them next: past them this
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256) void mx4_quant_rows_kernel(Mx4QuantParams p, R
 // 8192 x 4096 bf16: 20.3 us (4.2 TB/s), both ways 27.4 (3.75; two calls 38); bounded by memory
 // and, both ways, by a workgroup's phases (load, convert, store) with two workgroups to a CU:
 // three (80 registers) spill and take 36 us.
-constexpr int kQtCols = 128, kQtStride = 144;        // LDS bytes from one column to the next
+constexpr int kQtCols = 128;
 
 typedef uint16_t q_u16x2 __attribute__((ext_vector_type(2)));
 
@@ -103,14 +103,15 @@ __device__ __forceinline__ uint32_t row_word(uint32_t v) {
 // Scale code from the upper 16 bits of the largest magnitude (its exponent field is all that counts).
 __device__ __forceinline__ uint32_t scale_code16(uint32_t top) { return scale_code(top << 16); }
 
-template <bool BF16, bool BOTH>
-__global__ __launch_bounds__(512, 4) void mx4_quant_cols_kernel(Mx4QuantParams p, int row_groups) {
+template <bool BF16, bool BOTH, int W>
+__global__ __launch_bounds__(64 * W, 4) void mx4_quant_cols_kernel(Mx4QuantParams p, int row_groups) {
   // column 2 i + k of the block lies in place 64 k + i: lanes that write neighbouring even (odd)
   // columns meet 36 banks apart
-  __shared__ __attribute__((aligned(16))) uint8_t codes[kQtCols * kQtStride];
-  __shared__ __attribute__((aligned(16))) uint8_t scales[kQtCols * 8];
-  __shared__ __attribute__((aligned(16))) uint32_t row_codes[BOTH ? 64 * 64 : 4];    // [4 rows][2 columns]: a byte a row
-  __shared__ __attribute__((aligned(16))) uint8_t row_scales[BOTH ? 256 * 4 : 16];
+  constexpr int kRows = 32 * W, kStride = 16 * W + 16;         // kStride: LDS bytes from one column to the next
+  __shared__ __attribute__((aligned(16))) uint8_t codes[kQtCols * kStride];
+  __shared__ __attribute__((aligned(16))) uint8_t scales[kQtCols * W];
+  __shared__ __attribute__((aligned(16))) uint32_t row_codes[BOTH ? kRows / 4 * 64 : 4];    // [4 rows][2 columns]: a byte a row
+  __shared__ __attribute__((aligned(16))) uint8_t row_scales[BOTH ? kRows * 4 : 16];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col_groups = gridDim.x / (unsigned)row_groups;
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(512, 4) void mx4_quant_cols_kernel(Mx4QuantParams p
   if (BOTH && task < (gridDim.x & ~15u)) task = (task & ~15u) + 2 * (task & 7) + ((task >> 3) & 1);
   const int rg = task / (unsigned)col_groups, cb = task - rg * col_groups;
   const int64_t c0 = (int64_t)cb * kQtCols, c = c0 + 2 * lane;
-  const int64_t r0 = (int64_t)rg * 256 + 32 * wave;
+  const int64_t r0 = (int64_t)rg * kRows + 32 * wave;
   // the wave's 32 source rows (-1: zeros), all loads before any use
   int source = -1;
   if (lane < 32 && r0 + lane < p.rows) {
@@ -201,8 +202,8 @@ __global__ __launch_bounds__(512, 4) void mx4_quant_cols_kernel(Mx4QuantParams p
       SFC_CVT_COL(o, k, 4 * w + 3, 3);
       q[w] = o;
     }
-    *reinterpret_cast<row_u32x4*>(codes + (64 * k + lane) * kQtStride + 16 * wave) = q;
-    scales[(64 * k + lane) * 8 + wave] = (uint8_t)sc;
+    *reinterpret_cast<row_u32x4*>(codes + (64 * k + lane) * kStride + 16 * wave) = q;
+    scales[(64 * k + lane) * W + wave] = (uint8_t)sc;
   }
   if constexpr (BOTH) {
     // a lane makes the scales of two rows, whose upper halves (all that is not 0 in them) the
@@ -238,30 +239,30 @@ __global__ __launch_bounds__(512, 4) void mx4_quant_cols_kernel(Mx4QuantParams p
 #undef SFC_CVT_COL
 #undef SFC_CVT_ROW
   __syncthreads();
-  const int64_t blocks = (p.rows + 31) >> 5, b0 = (int64_t)rg * 8;
+  const int64_t blocks = (p.rows + 31) >> 5, b0 = (int64_t)rg * W;
 #pragma unroll
-  for (int i = tid; i < kQtCols * 8; i += 512) {
-    const int col = i >> 3, b = i & 7, place = 64 * (col & 1) + (col >> 1);
+  for (int i = tid; i < kQtCols * W; i += 64 * W) {
+    const int col = i / W, b = i % W, place = 64 * (col & 1) + (col >> 1);
     if (c0 + col < p.cols && b0 + b < blocks) {
       *reinterpret_cast<row_u32x4*>(p.Qt + (c0 + col) * p.ldqt + (b0 + b) * 16) =
-          *reinterpret_cast<const row_u32x4*>(codes + place * kQtStride + 16 * b);
+          *reinterpret_cast<const row_u32x4*>(codes + place * kStride + 16 * b);
     }
   }
   if (tid < kQtCols && c0 + tid < p.cols) {
-    const uint8_t* from = scales + (64 * (tid & 1) + (tid >> 1)) * 8;
+    const uint8_t* from = scales + (64 * (tid & 1) + (tid >> 1)) * W;
     uint8_t* to = p.St + (c0 + tid) * p.ldst + b0;
-    if (b0 + 8 <= blocks) {
-      reinterpret_cast<uint32_t*>(to)[0] = reinterpret_cast<const uint32_t*>(from)[0];
-      reinterpret_cast<uint32_t*>(to)[1] = reinterpret_cast<const uint32_t*>(from)[1];
+    if (b0 + W <= blocks) {
+#pragma unroll
+      for (int k = 0; k < W / 4; ++k) reinterpret_cast<uint32_t*>(to)[k] = reinterpret_cast<const uint32_t*>(from)[k];
     } else {
       for (int b = 0; b0 + b < blocks; ++b) to[b] = from[b];
     }
   }
   if constexpr (BOTH) {
-    const int64_t row_blocks = (p.cols + 31) >> 5, cb0 = c0 >> 5, top_row = (int64_t)rg * 256;
+    const int64_t row_blocks = (p.cols + 31) >> 5, cb0 = c0 >> 5, top_row = (int64_t)rg * kRows;
     // half of the threads take a block of four rows each: 16 words of a byte per row, turned into
     // 4 x 16 bytes; the others a row's scales
-    if (tid < 256) {
+    if (tid < kRows) {
       const int quad = tid >> 2, b = tid & 3;
       row_u32x4 in[4], out[4];
 #pragma unroll
@@ -284,14 +285,22 @@ __global__ __launch_bounds__(512, 4) void mx4_quant_cols_kernel(Mx4QuantParams p
             *reinterpret_cast<row_u32x4*>(p.Q + (top_row + r) * p.ldq + (cb0 + b) * 16) = out[u];
         }
       }
-    } else if (top_row + tid - 256 < p.rows) {
-      const uint8_t* from = row_scales + (tid - 256) * 4;
-      uint8_t* to = p.S + (top_row + tid - 256) * p.lds + cb0;
+    } else if (top_row + tid - kRows < p.rows) {
+      const uint8_t* from = row_scales + (tid - kRows) * 4;
+      uint8_t* to = p.S + (top_row + tid - kRows) * p.lds + cb0;
       if (cb0 + 4 <= row_blocks) *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
       else
         for (int b = 0; cb0 + b < row_blocks; ++b) to[b] = from[b];
     }
   }
+}
+
+template <int W>
+static void launch_cols(const Mx4QuantParams& p, bool in_bf16, dim3 g, dim3 b, int rg, hipStream_t stream) {
+  if (in_bf16 && p.Q) hipLaunchKernelGGL((mx4_quant_cols_kernel<true, true, W>), g, b, 0, stream, p, rg);
+  else if (in_bf16) hipLaunchKernelGGL((mx4_quant_cols_kernel<true, false, W>), g, b, 0, stream, p, rg);
+  else if (p.Q) hipLaunchKernelGGL((mx4_quant_cols_kernel<false, true, W>), g, b, 0, stream, p, rg);
+  else hipLaunchKernelGGL((mx4_quant_cols_kernel<false, false, W>), g, b, 0, stream, p, rg);
 }
 
 hipError_t launch_mx4_quant(const Mx4QuantParams& p, bool in_bf16, int num_cus, hipStream_t stream) {
@@ -302,12 +311,15 @@ hipError_t launch_mx4_quant(const Mx4QuantParams& p, bool in_bf16, int num_cus, 
     else hipLaunchKernelGGL((mx4_quant_rows_kernel<false>), g, b, 0, stream, p, sh);
     return hipGetLastError();
   }
-  const int rg = (int)((p.rows + 255) / 256);
-  const dim3 g((unsigned)(rg * ((p.cols + kQtCols - 1) / kQtCols))), b(512);
-  if (in_bf16 && p.Q) hipLaunchKernelGGL((mx4_quant_cols_kernel<true, true>), g, b, 0, stream, p, rg);
-  else if (in_bf16) hipLaunchKernelGGL((mx4_quant_cols_kernel<true, false>), g, b, 0, stream, p, rg);
-  else if (p.Q) hipLaunchKernelGGL((mx4_quant_cols_kernel<false, true>), g, b, 0, stream, p, rg);
-  else hipLaunchKernelGGL((mx4_quant_cols_kernel<false, false>), g, b, 0, stream, p, rg);
+  const int col_groups = (int)((p.cols + kQtCols - 1) / kQtCols);
+  // 256 rows to a workgroup, 128 while that leaves half of the CUs without one (us, 256 / 128 rows, both
+  // ways: bf16 128x4096 5.4 / 4.3, 1024x1024 5.0 / 4.3, 2048x2048 6.2 / 5.7, 4096x4096 15.2 / 16.5,
+  // 16384x4096 48.1 / 49.8; fp32 along the columns 128x4096 5.0 / 3.5, 2048x4096 10.2 / 10.7)
+  const bool wide = (p.rows + 255) / 256 * col_groups * 2 > num_cus;
+  const int rows = wide ? 256 : 128, rg = (int)((p.rows + rows - 1) / rows);
+  const dim3 g((unsigned)(rg * col_groups)), b(2 * rows);
+  if (wide) launch_cols<8>(p, in_bf16, g, b, rg, stream);
+  else launch_cols<4>(p, in_bf16, g, b, rg, stream);
   return hipGetLastError();
 }
 

@@ -127,6 +127,17 @@ def test_quant_through_an_order(so, rows, cols, topk, rows_out):
         assert (b.cpu().numpy() == e).all() and (a.cpu().numpy() == mx4.pack(c)).all()
 
 
+# (256 rows to a workgroup once those fill half of the CUs)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols,ld,offset", [(2100, 2570, 7, 1), (4097, 1300, 0, 0), (33000, 130, 0, 0), (200, 17000, 3, 0)])
+def test_quant_bits_of_large_matrices(so, dtype, rows, cols, ld, offset):
+    test_quant_bits(so, dtype, rows, cols, ld, offset)
+
+
+def test_quant_of_many_rows_through_an_order(so):
+    test_quant_through_an_order(so, 40, 4100, 30, 1100)
+
+
 def test_quant_writes_its_own_bytes_only(so):
     x = inputs(70, 100, BF16, 2)
     q, s, qv, sv = padded_mx4(70, 100, 128)
