@@ -264,10 +264,10 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(MoeRowsParams p, RowSh
 }
 
 // ---- gradient of combine -------------------------------------------------------------------
-// W waves per token, two choices at a time (dy is read once for both); before the tokens'
+// L lanes per token, two choices at a time (dy is read once for both); before the tokens'
 // workgroups, others clear the rows that no slot has, 16 rows to each (they lie together: 256
 // rows to a workgroup took 28 us longer for 8191 tokens in segments of 32).
-template <bool BF16, bool PAST, int W>
+template <bool BF16, bool PAST, int L>
 __global__ __launch_bounds__(256) void moe_combine_grad_kernel(MoeRowsParams p, int64_t clear_groups) {
   __shared__ float part[2][4];
   const int lane = threadIdx.x & 63;
@@ -284,8 +284,8 @@ __global__ __launch_bounds__(256) void moe_combine_grad_kernel(MoeRowsParams p, 
     }
     return;
   }
-  const int64_t t = ((int64_t)blockIdx.x - clear_groups) * (4 / W) + wave / W;
-  const int part_of = W == 4 ? wave : 0;       // this wave's share of the token's chunks
+  const int64_t t = ((int64_t)blockIdx.x - clear_groups) * (256 / L) + threadIdx.x / L;
+  const int lane_t = threadIdx.x & (L - 1);
   const bool in = t < p.tokens;
   const char* dy = reinterpret_cast<const char*>(p.X) + (in ? t : 0) * p.ldx * ES;
   for (int j = 0; j < p.topk; j += 2) {
@@ -303,11 +303,11 @@ __global__ __launch_bounds__(256) void moe_combine_grad_kernel(MoeRowsParams p, 
     }
     if (valid[0] || valid[1]) {
       constexpr int U = 2;
-      for (int64_t c = part_of * 64 + lane; c < chunks; c += U * 64 * W) {
+      for (int64_t c = lane_t; c < chunks; c += U * L) {
         Raw8<BF16> a[U], b[U][2];
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-          const int64_t ck = c + k * 64 * W;
+          const int64_t ck = c + k * L;
           if (ck < chunks) {
             a[k] = load8<BF16>(dy, ck * 8, p.cols);
 #pragma unroll
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(256) void moe_combine_grad_kernel(MoeRowsParams p, 
         }
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-          const int64_t ck = c + k * 64 * W;
+          const int64_t ck = c + k * L;
           if (ck < chunks) {
             float f[8];
             to_float<BF16>(a[k], f);
@@ -340,8 +340,8 @@ __global__ __launch_bounds__(256) void moe_combine_grad_kernel(MoeRowsParams p, 
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int d = 32; d >= 1; d >>= 1) dot[u] += __shfl_xor(dot[u], d);
-    if constexpr (W == 4) {
+      for (int d = L < 64 ? L / 2 : 32; d >= 1; d >>= 1) dot[u] += __shfl_xor(dot[u], d);
+    if constexpr (L == 256) {
       if (lane == 0) {
         part[0][wave] = dot[0];
         part[1][wave] = dot[1];
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(256) void moe_combine_grad_kernel(MoeRowsParams p, 
       for (int u = 0; u < 2; ++u) dot[u] = (part[u][0] + part[u][1]) + (part[u][2] + part[u][3]);
       __syncthreads();
     }
-    if (in && lane == 0 && part_of == 0) {
+    if (in && lane_t == 0) {
       p.dW[t * p.topk + j] = dot[0];
       if (j + 1 < p.topk) p.dW[t * p.topk + j + 1] = dot[1];
     }
@@ -381,21 +381,23 @@ hipError_t launch_moe_combine(const MoeRowsParams& p, bool bf16, int num_cus, hi
 }
 
 template <bool BF16, bool PAST>
-static const void* grad_kernel(bool wide) {
-  return wide ? reinterpret_cast<const void*>(&moe_combine_grad_kernel<BF16, PAST, 4>)
-              : reinterpret_cast<const void*>(&moe_combine_grad_kernel<BF16, PAST, 1>);
+static const void* grad_kernel(int lanes) {
+  return lanes == 256  ? reinterpret_cast<const void*>(&moe_combine_grad_kernel<BF16, PAST, 256>)
+         : lanes == 64 ? reinterpret_cast<const void*>(&moe_combine_grad_kernel<BF16, PAST, 64>)
+                       : reinterpret_cast<const void*>(&moe_combine_grad_kernel<BF16, PAST, 16>);
 }
 
 hipError_t launch_moe_combine_grad(const MoeRowsParams& p, bool bf16, int num_cus, hipStream_t stream) {
-  // four waves to a token where each has two loads of its row or more (8192 tokens x 4096 bf16:
-  // 67 us, one wave 81; 16384 x 1024: one wave 35 us)
-  const bool wide = p.cols >= 2048;
+  // as many lanes to a token as have about two loads of its row (us, 4 waves / one / 16 lanes: 8192 tokens
+  // x 4096 bf16 67 / 81 / -, 16384 x 1024 - / 35 / -, 16384 x 200 - / 12.5 / 8.1,
+  // 16384 x 64 - / 10.5 / 5.2)
+  const int lanes = p.cols >= 2048 ? 256 : p.cols > 256 ? 64 : 16;
   const bool past = streams_past_caches(p.rows * p.cols * (bf16 ? 2 : 4));
-  const int64_t groups = wide ? p.tokens : (p.tokens + 3) / 4;
+  const int64_t groups = (p.tokens * lanes + 255) / 256;
   const int64_t clear = (p.rows + 15) / 16;
   const dim3 g((unsigned)(groups + clear)), b(256);
-  const void* k = bf16 ? (past ? grad_kernel<true, true>(wide) : grad_kernel<true, false>(wide))
-                       : (past ? grad_kernel<false, true>(wide) : grad_kernel<false, false>(wide));
+  const void* k = bf16 ? (past ? grad_kernel<true, true>(lanes) : grad_kernel<true, false>(lanes))
+                       : (past ? grad_kernel<false, true>(lanes) : grad_kernel<false, false>(lanes));
   MoeRowsParams local = p;
   int64_t clear_groups = clear;
   void* args[] = {&local, &clear_groups};
