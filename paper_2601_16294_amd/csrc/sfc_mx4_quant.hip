@@ -366,10 +366,11 @@ __global__ __launch_bounds__(256) void mx4_dequant_kernel(Mx4DequantParams p, Ro
 hipError_t launch_mx4_dequant(const Mx4DequantParams& p, bool out_bf16, int num_cus, hipStream_t stream) {
   const RowShape sh = row_shape(p.rows, (p.cols + 7) / 8, num_cus);
   const dim3 g((unsigned)(sh.row_blocks * sh.splits)), b(256);
-  const bool past = streams_past_caches(p.rows * p.cols * (out_bf16 ? 2 : 4));
-  if (out_bf16 && past) hipLaunchKernelGGL((mx4_dequant_kernel<true, true>), g, b, 0, stream, p, sh);
+  // (fp32: a lane's two stores leave holes in a line, which only the caches fill: 8192x4096 51 us past
+  // them, 26 through)
+  const bool past = out_bf16 && streams_past_caches(p.rows * p.cols * 2);
+  if (past) hipLaunchKernelGGL((mx4_dequant_kernel<true, true>), g, b, 0, stream, p, sh);
   else if (out_bf16) hipLaunchKernelGGL((mx4_dequant_kernel<true, false>), g, b, 0, stream, p, sh);
-  else if (past) hipLaunchKernelGGL((mx4_dequant_kernel<false, true>), g, b, 0, stream, p, sh);
   else hipLaunchKernelGGL((mx4_dequant_kernel<false, false>), g, b, 0, stream, p, sh);
   return hipGetLastError();
 }
