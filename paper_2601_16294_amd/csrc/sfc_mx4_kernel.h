@@ -63,12 +63,12 @@ struct MxTile {
   static_assert(PER_CU * LDS <= 160 * 1024, "LDS of one CU");
 };
 
-// 16 bytes per lane from descriptor base + voffset + koffset to LDS lds + 16 * lane, behind the
-// compiler's back: whoever reads them waits for them (it counts the other loads, which
-// return in order).
-__device__ __forceinline__ void mx_dma16(const i32x4& rsrc, uint32_t lds, int voffset, int koffset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-               :: "s"(lds), "v"(voffset), "s"(rsrc), "s"(koffset) : "memory");
+// 16 bytes per lane from descriptor base + voffset to LDS lds + 16 * lane, zeros past the
+// descriptor's range, behind the compiler's back: whoever reads them waits for them (it counts
+// the other loads, which return in order).
+__device__ __forceinline__ void mx_dma16(const i32x4& rsrc, uint32_t lds, uint32_t voffset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :: "s"(lds), "v"(voffset), "s"(rsrc) : "memory");
 }
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_rsrc(const uint8_t* base, uint32_t range) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, (int)range, 0x00020000);
@@ -189,25 +189,27 @@ __device__ __forceinline__ void mx_block(const Mx4GemmParams& p, const MxTask& t
     }
   };
   // Scales: a load takes 32 bytes of 32 rows (of A's, then B's).  They end with the last
-  // row's (whole dwords): nothing past it is read.
+  // row's (whole dwords): nothing past it is read, whatever comes of the last loads, which run
+  // ahead of the range (so all of their offset is in the lane's, which the range is checked against).
   const int s_row_end = (t.hi + 3) & ~3;
   const i32x4 qas = make_rsrc_addr(reinterpret_cast<uint64_t>(p.As) + (uint64_t)(t.a_row * p.ldas + t.block0),
                                    t.hi > 0 ? (uint32_t)((t.m_valid - 1) * p.ldas + s_row_end) : 0u);
   const i32x4 qbs = make_rsrc_addr(reinterpret_cast<uint64_t>(t.Bs) + (uint64_t)(t.b_row * p.ldbs + t.block0),
                                    t.hi > 0 ? (uint32_t)((t.n_valid - 1) * p.ldbs + s_row_end) : 0u);
-  int sv[T::SC];
+  uint32_t sv[T::SC];                          // of the next group of four stages
 #pragma unroll
   for (int k = 0; k < T::SC; ++k) {
     const bool of_a = (wave * T::SC + k) * 32 < BM;
     const int r = (wave * T::SC + k) * 32 - (of_a ? 0 : BM) + (lane & 31);
-    sv[k] = r < (of_a ? t.m_valid : t.n_valid) ? (int)(r * (of_a ? p.ldas : p.ldbs)) + 16 * (lane >> 5) : kOobOffset;
+    sv[k] = r < (of_a ? t.m_valid : t.n_valid) ? (uint32_t)(r * (of_a ? p.ldas : p.ldbs)) + 16 * (lane >> 5) : (uint32_t)kOobOffset;
   }
-  auto load_scales = [&](int group) {        // four stages of scales, number `group`, into their slot
+  auto load_scales = [&](int group) {        // four stages of scales, number `group` (one after another), into their slot
     const uint32_t at = lds0 + (uint32_t)(T::SA_OFF + (group & 1) * T::S_SLOT + wave * T::SC * 1024);
 #pragma unroll
     for (int k = 0; k < T::SC; ++k) {
       const bool of_a = (wave * T::SC + k) * 32 < BM;
-      mx_dma16(of_a ? qas : qbs, at + (uint32_t)(k * 1024), sv[k], 32 * group);
+      mx_dma16(of_a ? qas : qbs, at + (uint32_t)(k * 1024), sv[k]);
+      sv[k] += 32;
     }
   };
 
