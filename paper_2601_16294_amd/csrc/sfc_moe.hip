@@ -277,7 +277,8 @@ __global__ __launch_bounds__(256) void moe_combine_grad_kernel(MoeRowsParams p, 
   if ((int64_t)blockIdx.x < clear_groups) {
     for (int i = 0; i < 4; ++i) {
       const int64_t r = (int64_t)blockIdx.x * 16 + 4 * wave + i;
-      const int32_t slot = r < p.rows ? p.order[r] : 0;
+      if (r >= p.rows) break;
+      const int32_t slot = p.order[r];
       if (slot >= 0 && (int64_t)slot < p.tokens * p.topk) continue;
       char* y = reinterpret_cast<char*>(p.Y) + r * p.ldy * ES;
       for (int64_t c = lane; c < chunks; c += 64) store8<BF16, PAST>(y, c * 8, p.cols, zero8<BF16>());
