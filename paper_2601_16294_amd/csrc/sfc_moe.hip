@@ -276,8 +276,8 @@ __global__ __launch_bounds__(256) void moe_combine_grad_kernel(MoeRowsParams p, 
   constexpr int ES = BF16 ? 2 : 4;
   if ((int64_t)blockIdx.x < clear_groups) {
     for (int i = 0; i < 4; ++i) {
-      const int64_t r = (int64_t)blockIdx.x * 16 + 4 * wave + i;
-      if (r >= p.rows) break;
+      const int64_t r = p.first_row + (int64_t)blockIdx.x * 16 + 4 * wave + i;
+      if (r >= p.end_row) break;
       const int32_t slot = p.order[r];
       if (slot >= 0 && (int64_t)slot < p.tokens * p.topk) continue;
       char* y = reinterpret_cast<char*>(p.Y) + r * p.ldy * ES;
@@ -285,9 +285,9 @@ __global__ __launch_bounds__(256) void moe_combine_grad_kernel(MoeRowsParams p, 
     }
     return;
   }
-  const int64_t t = ((int64_t)blockIdx.x - clear_groups) * (256 / L) + threadIdx.x / L;
+  const int64_t t = p.first_token + ((int64_t)blockIdx.x - clear_groups) * (256 / L) + threadIdx.x / L;
   const int lane_t = threadIdx.x & (L - 1);
-  const bool in = t < p.tokens;
+  const bool in = t < p.end_token;
   const char* dy = reinterpret_cast<const char*>(p.X) + (in ? t : 0) * p.ldx * ES;
   for (int j = 0; j < p.topk; j += 2) {
     bool valid[2];
@@ -403,8 +403,8 @@ hipError_t launch_moe_combine_grad(const MoeRowsParams& p, bool bf16, int num_cu
   // 16384 x 64 - / 10.5 / 5.2)
   const int lanes = p.cols >= 2048 ? 256 : p.cols > 256 ? 64 : 16;
   const bool past = streams_past_caches(p.rows * p.cols * (bf16 ? 2 : 4));
-  const int64_t groups = (p.tokens * lanes + 255) / 256;
-  const int64_t clear = (p.rows + 15) / 16;
+  const int64_t groups = ((p.end_token - p.first_token) * lanes + 255) / 256;
+  const int64_t clear = (p.end_row - p.first_row + 15) / 16;
   const dim3 g((unsigned)(groups + clear)), b(256);
   const void* k = bf16 ? (past ? grad_kernel<true, true>(lanes) : grad_kernel<true, false>(lanes))
                        : (past ? grad_kernel<false, true>(lanes) : grad_kernel<false, false>(lanes));

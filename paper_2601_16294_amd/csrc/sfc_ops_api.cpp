@@ -62,8 +62,9 @@ Mx4Plan mx4_plan(int64_t M, int64_t N, int64_t K, bool out_f32, int num_cus) {
   // Up to 64 rows: the streaming kernel reads A once for every 32 columns, which pays while a
   // wave has one turn of K (us, streaming against 128x128 blocks with their best layers:
   // 32x4096x4096 7.6 / 10.6, 32x14336x4096 13.7 / 14.5, 32x4096x14336 20.5 / 16.0; 64x4096x4096
-  // 10.3 / 11.7, 64x1024x1024 4.4 / 6.2, 64x14336x4096 21.0 / 15.5).
-  if (M <= 64 && K <= 8 * 512 && (M <= 32 || N <= 4096)) {
+  // 10.3 / 11.7, 64x1024x1024 4.4 / 6.2, 64x14336x4096 21.0 / 15.5).  (2^28: 512 threads for every 32
+  // columns have to fit a launch.)
+  if (M <= 64 && K <= 8 * 512 && (M <= 32 ? N < (int64_t)1 << 28 : N <= 4096)) {
     pl.fm = M <= 32 ? 2 : 4;
     return pl;
   }
@@ -126,8 +127,48 @@ int mx4_dense(const Mx4Plan& pl, sfc::Mx4GemmParams& p, bool ob, int num_cus, fl
   return SFC_OK;
 }
 
+int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
+const char* at(const void* p, int64_t offset) { return p ? static_cast<const char*>(p) + offset : nullptr; }
+uint8_t* at(uint8_t* p, int64_t offset) { return p ? p + offset : nullptr; }
+
+// Rows first .. first + count - 1 of X for every launch that `rows` of them take.
+template <class F>
+hipError_t row_launches(int64_t rows, F launch) {
+  for (int64_t first = 0; first < rows; first += sfc::kLaunchRows) {
+    const hipError_t e = launch(first, least(sfc::kLaunchRows, rows - first));
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+// A part of a quantisation: `count` rows from row `first` (a multiple of 256) and `width` columns from
+// column `col` (a multiple of 128).
+hipError_t quant_part(const sfc::Mx4QuantParams& all, int64_t first, int64_t count, int64_t col, int64_t width, bool bf16,
+                      int num_cus, hipStream_t stream) {
+  sfc::Mx4QuantParams p = all;
+  p.rows = count;
+  p.cols = width;
+  p.X = at(all.X, ((all.order ? 0 : first * all.ldx) + col) * (bf16 ? 2 : 4));
+  if (all.order) p.order += first;
+  else p.x_rows = count;
+  p.Q = at(all.Q, first * all.ldq + col / 2);
+  p.S = at(all.S, first * all.lds + col / 32);
+  p.Qt = at(all.Qt, col * all.ldqt + first / 2);
+  p.St = at(all.St, col * all.ldst + first / 32);
+  return sfc::launch_mx4_quant(p, bf16, num_cus, stream);
+}
+
 int quant_launch(const sfc::Mx4QuantParams& p, bool bf16, int num_cus, hipStream_t stream) {
-  const hipError_t e = sfc::launch_mx4_quant(p, bf16, num_cus, stream);
+  // along the columns as many whole blocks of 128 columns as a launch has workgroups for
+  const int64_t row_groups = sfc::ceil_div(least(p.rows, sfc::kLaunchRows), 128);
+  const int64_t cols = p.Qt ? sfc::kLaunchBlocks / row_groups * 128 : p.cols;
+  const hipError_t e = row_launches(p.rows, [&](int64_t first, int64_t count) {
+    for (int64_t c = 0; c < p.cols; c += cols) {
+      const hipError_t part = quant_part(p, first, count, c, least(cols, p.cols - c), bf16, num_cus, stream);
+      if (part != hipSuccess) return part;
+    }
+    return hipSuccess;
+  });
   return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "4-bit quantisation");
 }
 
@@ -174,8 +215,11 @@ int sfc_mx4_dequant(int64_t rows, int64_t cols, const void* Q, int64_t ldq, cons
   int cus = 0;
   const int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
-  const sfc::Mx4DequantParams p = {rows, cols, bytes(Q), bytes(S), ldq, lds, Y, ldy};
-  const hipError_t e = sfc::launch_mx4_dequant(p, out_type == SFC_OUT_BF16, cus, as_stream(stream));
+  const hipError_t e = row_launches(rows, [&](int64_t first, int64_t count) {
+    const sfc::Mx4DequantParams p = {count, cols, bytes(Q) + first * ldq, bytes(S) + first * lds, ldq, lds,
+                                     static_cast<char*>(Y) + first * ldy * sfc::type_size(out_type), ldy};
+    return sfc::launch_mx4_dequant(p, out_type == SFC_OUT_BF16, cus, as_stream(stream));
+  });
   return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "4-bit dequantisation");
 }
 
@@ -346,8 +390,11 @@ int sfc_moe_dispatch(int64_t rows, int64_t cols, int64_t tokens, int topk, const
   int cus = 0;
   const int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
-  const sfc::MoeRowsParams p = {tokens, rows, cols, topk, X, ldx, nullptr, 0, order, nullptr, weights, Xs, ldxs, nullptr};
-  const hipError_t e = sfc::launch_moe_dispatch(p, type == SFC_OUT_BF16, cus, as_stream(stream));
+  const hipError_t e = row_launches(rows, [&](int64_t first, int64_t count) {
+    const sfc::MoeRowsParams p = {tokens, count, cols, topk, X, ldx, nullptr, 0, order + first, nullptr, weights,
+                                  static_cast<char*>(Xs) + first * ldxs * sfc::type_size(type), ldxs, nullptr, 0, 0, 0, 0};
+    return sfc::launch_moe_dispatch(p, type == SFC_OUT_BF16, cus, as_stream(stream));
+  });
   return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "dispatch");
 }
 
@@ -366,8 +413,12 @@ int sfc_moe_combine(int64_t tokens, int64_t cols, int64_t rows, int topk, const 
   int cus = 0;
   const int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
-  const sfc::MoeRowsParams p = {tokens, rows, cols, topk, Ys, ldys, nullptr, 0, nullptr, pos, weights, Y, ldy, nullptr};
-  const hipError_t e = sfc::launch_moe_combine(p, type == SFC_OUT_BF16, cus, as_stream(stream));
+  const hipError_t e = row_launches(tokens, [&](int64_t first, int64_t count) {
+    const sfc::MoeRowsParams p = {count, rows, cols, topk, Ys, ldys, nullptr, 0, nullptr, pos + first * topk,
+                                  weights ? weights + first * topk : nullptr,
+                                  static_cast<char*>(Y) + first * ldy * sfc::type_size(type), ldy, nullptr, 0, 0, 0, 0};
+    return sfc::launch_moe_combine(p, type == SFC_OUT_BF16, cus, as_stream(stream));
+  });
   return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "combine");
 }
 
@@ -388,8 +439,15 @@ int sfc_moe_combine_grad(int64_t tokens, int64_t cols, int64_t rows, int topk, c
   int cus = 0;
   const int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
-  const sfc::MoeRowsParams p = {tokens, rows, cols, topk, dY, lddy, Ys, ldys, order, pos, weights, dYs, lddys, dW};
-  const hipError_t e = sfc::launch_moe_combine_grad(p, type == SFC_OUT_BF16, cus, as_stream(stream));
+  sfc::MoeRowsParams p = {tokens, rows, cols, topk, dY, lddy, Ys, ldys, order, pos, weights, dYs, lddys, dW, 0, 0, 0, 0};
+  hipError_t e = hipSuccess;
+  while (e == hipSuccess && (p.end_token < tokens || p.end_row < rows)) {
+    p.first_token = p.end_token;
+    p.end_token = least(p.first_token + sfc::kLaunchRows, tokens);
+    p.first_row = p.end_row;
+    p.end_row = least(p.first_row + 8 * sfc::kLaunchRows, rows);
+    e = sfc::launch_moe_combine_grad(p, type == SFC_OUT_BF16, cus, as_stream(stream));
+  }
   return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "gradient of combine");
 }
 

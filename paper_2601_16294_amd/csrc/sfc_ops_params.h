@@ -9,6 +9,12 @@ namespace sfc {
 constexpr int kMxBlock = 32;         // values that share one scale
 constexpr int kMaxExperts = 1024;
 
+// A launch has less than 2^32 threads.  The row kernels take at most 256 of them for a row, the
+// gradient of combine also 256 for 16 rows to clear, quantisation along the columns 512 for
+// 256 rows x 128 columns (256 for 128 rows): longer matrices are dealt to several launches.
+constexpr int64_t kLaunchRows = (int64_t)1 << 23;
+constexpr int64_t kLaunchBlocks = (int64_t)1 << 22;
+
 // Quantisation of X, or of its rows X[order[p] / topk] (order != nullptr).
 struct Mx4QuantParams {
   int64_t rows;              // rows to quantise (entries of `order`, or rows of X)
@@ -97,6 +103,8 @@ struct MoeRowsParams {
   void* Y;                   // dispatch: rows x cols; combine: tokens x cols; gradient: rows x cols
   int64_t ldy;
   float* dW;                 // gradient: per slot
+  // gradient: the tokens and the rows to clear of this launch, first .. end - 1
+  int64_t first_token, end_token, first_row, end_row;
 };
 hipError_t launch_moe_dispatch(const MoeRowsParams& p, bool bf16, int num_cus, hipStream_t stream);
 hipError_t launch_moe_combine(const MoeRowsParams& p, bool bf16, int num_cus, hipStream_t stream);
