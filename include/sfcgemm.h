@@ -393,8 +393,9 @@ int sfc_mx4_dequant(int64_t rows, int64_t cols,
  * stream B once: up to 16 with A in registers while K <= 8192 (16384 where N is large),
  * and up to 64 while K <= 4096.  The others run on 256x256 or 128x128 blocks along the
  * curve, K in up to 16 layers where an estimate of the time favours it (copies in
- * library memory, as for sfc_gemm).  The choice depends on M, N, K and out_type alone, so
- * equal calls give equal bits.
+ * library memory, as for sfc_gemm: replays of graphs recorded on one stream must then not
+ * overlap each other, but with a workspace of their own).  The choice depends on M, N, K and
+ * out_type alone, so equal calls give equal bits.
  * The gradients of C = A * B^T are two such calls: dA = dC * B with dC's blocks along N
  * and the transposed B (Qt of sfc_mx4_quant), dB = dC^T * A with both transposed.
  */
@@ -404,16 +405,42 @@ int sfc_gemm_mx4_ex(int64_t M, int64_t N, int64_t K,
                     void *C, int64_t ldc, int out_type, void *stream);
 
 /*
+ * sfc_gemm_mx4_ws_ex -- sfc_gemm_mx4_ex with its layer copies in the caller's workspace, so
+ * that graphs with workspaces of their own may be replayed at once, wherever they were recorded.
+ *   ws         NULL (library memory of the stream) or 16-byte aligned device memory of
+ *              sfc_gemm_mx4_ws_size() bytes (SFC_ERR_WORKSPACE if ws_bytes is less); the call uses
+ *              it until its work on `stream` has finished.
+ * sfc_gemm_mx4_ws_size -- bytes that the call needs on the current device; 0 where it needs
+ * none, the sizes are bad or there is no device.
+ */
+size_t sfc_gemm_mx4_ws_size(int64_t M, int64_t N, int64_t K, int out_type);
+int sfc_gemm_mx4_ws_ex(int64_t M, int64_t N, int64_t K,
+                       const void *A, int64_t lda, const void *As, int64_t ldas,
+                       const void *B, int64_t ldb, const void *Bs, int64_t ldbs,
+                       void *C, int64_t ldc, int out_type,
+                       void *ws, size_t ws_bytes, void *stream);
+
+/*
  * sfc_mx4_linear -- Y = X * W^T with X (M x K, fp32 or bf16) brought to 4 bits within the
  * call and W (N x K) kept in 4 bits.  K is the row length of X, W's rows hold
  * ceil(K/32) blocks; the result is that of sfc_mx4_quant and sfc_gemm_mx4_ex.  Up to 16
  * rows may be converted by the product's own launch; otherwise X's codes lie in library
- * memory, one per stream, as layer copies do.
+ * memory, one per stream, as layer copies do: replays of graphs recorded on one stream must not
+ * overlap each other, but with a workspace of their own.
  */
 int sfc_mx4_linear(int64_t M, int64_t N, int64_t K,
                    const void *X, int64_t ldx, int in_type,
                    const void *W, int64_t ldw, const void *Ws, int64_t ldws,
                    void *Y, int64_t ldy, int out_type, void *stream);
+
+/* sfc_mx4_linear_ws, sfc_mx4_linear_ws_size -- the same with X's codes, scales and the layer copies
+ * in the caller's workspace, as for sfc_gemm_mx4_ws_ex. */
+size_t sfc_mx4_linear_ws_size(int64_t M, int64_t N, int64_t K, int out_type);
+int sfc_mx4_linear_ws(int64_t M, int64_t N, int64_t K,
+                      const void *X, int64_t ldx, int in_type,
+                      const void *W, int64_t ldw, const void *Ws, int64_t ldws,
+                      void *Y, int64_t ldy, int out_type,
+                      void *ws, size_t ws_bytes, void *stream);
 
 /* ---- mixture of experts -------------------------------------------------------
  * A slot is one (token, choice) pair, slot = token*topk + choice.  Sorted rows belong to
@@ -430,7 +457,8 @@ int sfc_mx4_linear(int64_t M, int64_t N, int64_t K,
  *   rows       length of `order`, >= slots + experts*(align - 1).  offsets has
  *              experts + 1 entries, offsets[experts] being the rows in use (the rest of
  *              `order` is -1); pos has `slots`.
- *   ws         NULL (library memory of the stream) or sfc_moe_sort_ws_size() bytes.
+ *   ws         NULL (library memory of the stream, see sfc_mx4_linear for graphs) or
+ *              sfc_moe_sort_ws_size() bytes.
  * At most 1024 experts.
  */
 size_t sfc_moe_sort_ws_size(int64_t slots, int experts);

@@ -92,6 +92,47 @@ size_t mx4_copies(const Mx4Plan& pl, int64_t M, int64_t N) {
   return pl.layers > 1 ? (size_t)pl.layers * (size_t)M * (size_t)N * 4u : 0;
 }
 
+// How a linear layer runs: its product, and the memory for X's codes and scales, then the product's
+// layer copies.
+struct LinearPlan {
+  Mx4Plan product;
+  bool fused = false;                  // X brought to 4 bits by the product's own launch
+  int64_t blocks = 0, ldq = 0, lds = 0;
+  size_t codes = 0, scales = 0, copies = 0;
+  size_t bytes() const { return codes + scales + copies; }
+};
+
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool out_f32, int num_cus) {
+  LinearPlan pl;
+  pl.blocks = sfc::mx4_blocks(K);
+  pl.product = mx4_plan(M, N, 32 * pl.blocks, out_f32, num_cus);
+  // Few rows brought to 4 bits by the product's own launch: every workgroup converts them, which
+  // costs less than a launch while they or the workgroups are few (us in a graph, both
+  // launches against one: 1x4096x4096 7.2 / 5.6, 16x4096x4096 7.4 / 8.0 but 3.5 us less host time,
+  // 8x14336x4096 11.6 / 11.6, 16x14336x4096 11.7 / 13.0).
+  pl.fused = pl.product.few && K > 0 && K <= sfc::kConvertDepth && (M <= 8 || N <= 32 * (int64_t)num_cus);
+  if (pl.fused) return pl;
+  pl.ldq = 16 * pl.blocks;
+  pl.lds = round_up(pl.blocks, 4);
+  pl.codes = (size_t)M * (size_t)pl.ldq;
+  pl.scales = (size_t)round_up(M * pl.lds, 16);
+  pl.copies = mx4_copies(pl.product, M, N);
+  return pl;
+}
+
+// `need` bytes at *ws: the caller's, if there are any, else the stream's.  With the lock held.
+int memory(hipStream_t stream, size_t need, size_t ws_bytes, const char* too_small, void** ws) {
+  if (*ws) return ws_bytes < need ? sfc::host_error(SFC_ERR_WORKSPACE, too_small) : SFC_OK;
+  return need ? sfc::host_workspace(stream, need, ws) : SFC_OK;
+}
+
+// For the queries of sizes: the number of CUs, if the sizes are good and not empty.
+bool ws_device(const Checked& c, int64_t M, int64_t N, int* num_cus) {
+  if (c.code != SFC_OK || M == 0 || N == 0) return false;
+  std::lock_guard<std::mutex> lock(sfc::host_mutex());
+  return sfc::host_num_cus(num_cus) == SFC_OK;
+}
+
 // Launches a dense product; `copies` holds its layer copies.  With the lock held.
 int mx4_dense(const Mx4Plan& pl, sfc::Mx4GemmParams& p, bool ob, int num_cus, float* copies, hipStream_t stream) {
   if (pl.few || pl.fm) {
@@ -226,7 +267,20 @@ int sfc_mx4_dequant(int64_t rows, int64_t cols, const void* Q, int64_t ldq, cons
 int sfc_gemm_mx4_ex(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const void* As, int64_t ldas,
                     const void* B, int64_t ldb, const void* Bs, int64_t ldbs, void* C, int64_t ldc, int out_type,
                     void* stream) {
-  const Checked c = sfc::check_gemm_mx4(M, N, K, A, lda, As, ldas, B, ldb, Bs, ldbs, C, ldc, out_type);
+  return sfc_gemm_mx4_ws_ex(M, N, K, A, lda, As, ldas, B, ldb, Bs, ldbs, C, ldc, out_type, nullptr, 0, stream);
+}
+
+size_t sfc_gemm_mx4_ws_size(int64_t M, int64_t N, int64_t K, int out_type) {
+  int cus = 0;
+  if (!ws_device(sfc::check_gemm_mx4_sizes(M, N, K, out_type), M, N, &cus)) return 0;
+  return mx4_copies(mx4_plan(M, N, K, out_type == SFC_OUT_F32, cus), M, N);
+}
+
+int sfc_gemm_mx4_ws_ex(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const void* As, int64_t ldas,
+                       const void* B, int64_t ldb, const void* Bs, int64_t ldbs, void* C, int64_t ldc, int out_type,
+                       void* ws, size_t ws_bytes, void* stream) {
+  Checked c = sfc::check_gemm_mx4(M, N, K, A, lda, As, ldas, B, ldb, Bs, ldbs, C, ldc, out_type);
+  if (c.code == SFC_OK) c = sfc::check_workspace(ws);
   if (c.code != SFC_OK) return reject(c);
   if (M == 0 || N == 0) return SFC_OK;
   const hipStream_t st = as_stream(stream);
@@ -235,9 +289,7 @@ int sfc_gemm_mx4_ex(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda,
   int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
   const Mx4Plan pl = mx4_plan(M, N, K, out_type == SFC_OUT_F32, cus);
-  void* ws = nullptr;
-  const size_t need = mx4_copies(pl, M, N);
-  if (need) rc = sfc::host_workspace(st, need, &ws);
+  rc = memory(st, mx4_copies(pl, M, N), ws_bytes, "workspace smaller than sfc_gemm_mx4_ws_size()", &ws);
   if (rc != SFC_OK) return rc;
   sfc::Mx4GemmParams p = {M, N, K, bytes(A), bytes(As), bytes(B), bytes(Bs), lda, ldas, ldb, ldbs, 0, 0, C, ldc, 0,
                           nullptr, 0, 0, 0, nullptr, 1, past_caches(M * N, out_type), nullptr, 0, 0};
@@ -246,7 +298,21 @@ int sfc_gemm_mx4_ex(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda,
 
 int sfc_mx4_linear(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, int in_type, const void* W, int64_t ldw,
                    const void* Ws, int64_t ldws, void* Y, int64_t ldy, int out_type, void* stream) {
-  const Checked c = sfc::check_mx4_linear(M, N, K, X, ldx, in_type, W, ldw, Ws, ldws, Y, ldy, out_type);
+  return sfc_mx4_linear_ws(M, N, K, X, ldx, in_type, W, ldw, Ws, ldws, Y, ldy, out_type, nullptr, 0, stream);
+}
+
+size_t sfc_mx4_linear_ws_size(int64_t M, int64_t N, int64_t K, int out_type) {
+  int cus = 0;
+  if (!ws_device(sfc::check_mx4_linear_sizes(M, N, K, out_type, out_type), M, N, &cus)) return 0;
+  const LinearPlan pl = linear_plan(M, N, K, out_type == SFC_OUT_F32, cus);
+  return pl.bytes();
+}
+
+int sfc_mx4_linear_ws(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, int in_type, const void* W, int64_t ldw,
+                      const void* Ws, int64_t ldws, void* Y, int64_t ldy, int out_type, void* ws, size_t ws_bytes,
+                      void* stream) {
+  Checked c = sfc::check_mx4_linear(M, N, K, X, ldx, in_type, W, ldw, Ws, ldws, Y, ldy, out_type);
+  if (c.code == SFC_OK) c = sfc::check_workspace(ws);
   if (c.code != SFC_OK) return reject(c);
   if (M == 0 || N == 0) return SFC_OK;
   const hipStream_t st = as_stream(stream);
@@ -254,33 +320,25 @@ int sfc_mx4_linear(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, 
   int cus = 0;
   int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
-  const int64_t blocks = sfc::mx4_blocks(K), ldq = 16 * blocks, lds = round_up(blocks, 4);
-  const Mx4Plan pl = mx4_plan(M, N, 32 * blocks, out_type == SFC_OUT_F32, cus);
-  // Few rows brought to 4 bits by the product's own launch: every workgroup converts them, which
-  // costs less than a launch while they or the workgroups are few (us in a graph, both
-  // launches against one: 1x4096x4096 7.2 / 5.6, 16x4096x4096 7.4 / 8.0 but 3.5 us less host time,
-  // 8x14336x4096 11.6 / 11.6, 16x14336x4096 11.7 / 13.0).
-  if (pl.few && K > 0 && K <= sfc::kConvertDepth && (M <= 8 || N <= 32 * (int64_t)cus)) {
-    const sfc::Mx4GemmParams p = {M, N, 32 * blocks, nullptr, nullptr, bytes(W), bytes(Ws), 0, 0, ldw, ldws, 0, 0, Y, ldy,
+  const LinearPlan pl = linear_plan(M, N, K, out_type == SFC_OUT_F32, cus);
+  if (pl.fused) {
+    const sfc::Mx4GemmParams p = {M, N, 32 * pl.blocks, nullptr, nullptr, bytes(W), bytes(Ws), 0, 0, ldw, ldws, 0, 0, Y, ldy,
                                   0, nullptr, 0, 0, 0, nullptr, 1, false, X, ldx, K};
     const hipError_t e = sfc::launch_mx4_few(p, in_type == SFC_OUT_BF16 ? sfc::kRowsBf16 : sfc::kRowsF32, cus,
                                              out_type == SFC_OUT_BF16, st);
     return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "4-bit product of few rows");
   }
-  // the stream's workspace: codes and scales of X, then the layer copies
-  const size_t code_bytes = (size_t)M * (size_t)ldq, scale_bytes = (size_t)round_up(M * lds, 16);
-  void* ws = nullptr;
-  if (K > 0 || pl.layers > 1) rc = sfc::host_workspace(st, code_bytes + scale_bytes + mx4_copies(pl, M, N), &ws);
+  rc = memory(st, pl.bytes(), ws_bytes, "workspace smaller than sfc_mx4_linear_ws_size()", &ws);
   if (rc != SFC_OK) return rc;
   uint8_t* q = static_cast<uint8_t*>(ws);
   if (K > 0) {
-    sfc::Mx4QuantParams x = {M, K, X, ldx, nullptr, M, 1, q, q + code_bytes, ldq, lds, nullptr, nullptr, 0, 0};
+    sfc::Mx4QuantParams x = {M, K, X, ldx, nullptr, M, 1, q, q + pl.codes, pl.ldq, pl.lds, nullptr, nullptr, 0, 0};
     rc = quant_launch(x, in_type == SFC_OUT_BF16, cus, st);
     if (rc != SFC_OK) return rc;
   }
-  sfc::Mx4GemmParams p = {M, N, 32 * blocks, q, q + code_bytes, bytes(W), bytes(Ws), ldq, lds, ldw, ldws, 0, 0, Y, ldy,
+  sfc::Mx4GemmParams p = {M, N, 32 * pl.blocks, q, q + pl.codes, bytes(W), bytes(Ws), pl.ldq, pl.lds, ldw, ldws, 0, 0, Y, ldy,
                           0, nullptr, 0, 0, 0, nullptr, 1, past_caches(M * N, out_type), nullptr, 0, 0};
-  return mx4_dense(pl, p, out_type == SFC_OUT_BF16, cus, reinterpret_cast<float*>(q + code_bytes + scale_bytes), st);
+  return mx4_dense(pl.product, p, out_type == SFC_OUT_BF16, cus, reinterpret_cast<float*>(q + pl.codes + pl.scales), st);
 }
 
 int sfc_moe_gemm_mx4_ex(int64_t rows, int64_t N, int64_t K, int experts, const void* A, int64_t lda, const void* As,

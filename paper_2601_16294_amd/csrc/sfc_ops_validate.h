@@ -81,12 +81,23 @@ inline Checked check_blocks(int64_t M, int64_t N, int64_t groups) {
   return ok();
 }
 
-inline Checked check_gemm_mx4(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const void* As, int64_t ldas,
-                              const void* B, int64_t ldb, const void* Bs, int64_t ldbs, const void* C, int64_t ldc,
-                              int out_type) {
+// A caller's workspace (its size is checked against what the call's plan needs).
+inline Checked check_workspace(const void* ws) {
+  if ((uintptr_t)ws % 16) return fail(SFC_ERR_UNSUPPORTED, "workspace must be 16-byte aligned");
+  return ok();
+}
+
+inline Checked check_gemm_mx4_sizes(int64_t M, int64_t N, int64_t K, int out_type) {
   SFC_RETURN_IF(check_dims(M, N, K));
   if (!type_ok(out_type)) return fail(SFC_ERR_INVALID_ARG, "unknown out_type");
   if (K % 32) return fail(SFC_ERR_INVALID_ARG, "K must be a multiple of 32");
+  return ok();
+}
+
+inline Checked check_gemm_mx4(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const void* As, int64_t ldas,
+                              const void* B, int64_t ldb, const void* Bs, int64_t ldbs, const void* C, int64_t ldc,
+                              int out_type) {
+  SFC_RETURN_IF(check_gemm_mx4_sizes(M, N, K, out_type));
   if (M == 0 || N == 0) return ok();
   SFC_RETURN_IF(check_rows(C, M, N, ldc, out_type, "C is NULL", "ldc < N"));
   SFC_RETURN_IF(check_mx4(A, lda, As, ldas, M, K));
@@ -94,10 +105,15 @@ inline Checked check_gemm_mx4(int64_t M, int64_t N, int64_t K, const void* A, in
   return check_blocks(M, N, kAutoLayers);
 }
 
-inline Checked check_mx4_linear(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, int in_type, const void* W,
-                                int64_t ldw, const void* Ws, int64_t ldws, const void* Y, int64_t ldy, int out_type) {
+inline Checked check_mx4_linear_sizes(int64_t M, int64_t N, int64_t K, int in_type, int out_type) {
   SFC_RETURN_IF(check_dims(M, N, K));
   if (!type_ok(in_type) || !type_ok(out_type)) return fail(SFC_ERR_INVALID_ARG, "unknown element type");
+  return ok();
+}
+
+inline Checked check_mx4_linear(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, int in_type, const void* W,
+                                int64_t ldw, const void* Ws, int64_t ldws, const void* Y, int64_t ldy, int out_type) {
+  SFC_RETURN_IF(check_mx4_linear_sizes(M, N, K, in_type, out_type));
   if (M == 0 || N == 0) return ok();
   SFC_RETURN_IF(check_rows(Y, M, N, ldy, out_type, "Y is NULL", "ldy < N"));
   SFC_RETURN_IF(check_rows(X, M, K, ldx, in_type, "X is NULL", "ldx < K"));

@@ -39,7 +39,8 @@ EXPORTS = ["sfc_tile_order", "sfc_tile_order_ex", "sfc_gemm", "sfc_gemm_bf16out"
            # the operators of sfcops.py
            "sfc_mx4_quant", "sfc_mx4_dequant", "sfc_gemm_mx4_ex", "sfc_mx4_linear", "sfc_moe_sort_ws_size",
            "sfc_moe_sort", "sfc_moe_dispatch", "sfc_moe_combine", "sfc_moe_combine_grad", "sfc_moe_gemm_mx4_ex",
-           "sfc_moe_wgrad_mx4_ex"]
+           "sfc_moe_wgrad_mx4_ex", "sfc_gemm_mx4_ws_size", "sfc_gemm_mx4_ws_ex", "sfc_mx4_linear_ws_size",
+           "sfc_mx4_linear_ws"]
 
 
 class SfcError(RuntimeError):

@@ -27,7 +27,7 @@ except ImportError as e:
     raise ImportError("paper_2601_16294_amd/_sfcargs.so is not built; run `python -m paper_2601_16294_amd.build`") from e
 
 __all__ = ["SfcError", "mx4_empty", "sfc_mx4_quant", "sfc_mx4_dequant", "sfc_gemm_mx4_ex", "sfc_mx4_linear",
-           "sfc_moe_sort", "sfc_moe_sort_rows", "sfc_moe_dispatch", "sfc_moe_combine", "sfc_moe_combine_grad",
+           "sfc_gemm_mx4_ws_size", "sfc_mx4_linear_ws_size", "sfc_moe_sort", "sfc_moe_sort_rows", "sfc_moe_dispatch", "sfc_moe_combine", "sfc_moe_combine_grad",
            "sfc_moe_gemm_mx4_ex", "sfc_moe_wgrad_mx4_ex"]
 
 
@@ -39,6 +39,9 @@ def _declare() -> None:
     lib.sfc_mx4_dequant.argtypes = [i64, i64] + mx + rows + [i32, p]
     lib.sfc_gemm_mx4_ex.argtypes = [i64, i64, i64] + mx + mx + rows + [i32, p]
     lib.sfc_mx4_linear.argtypes = [i64, i64, i64] + rows + [i32] + mx + rows + [i32, p]
+    lib.sfc_gemm_mx4_ws_ex.argtypes = lib.sfc_gemm_mx4_ex.argtypes[:-1] + [p, sz, p]
+    lib.sfc_mx4_linear_ws.argtypes = lib.sfc_mx4_linear.argtypes[:-1] + [p, sz, p]
+    lib.sfc_gemm_mx4_ws_size.argtypes = lib.sfc_mx4_linear_ws_size.argtypes = [i64, i64, i64, i32]
     lib.sfc_moe_sort_ws_size.argtypes = [i64, i32]
     lib.sfc_moe_sort.argtypes = [i64, i32, i32, p, i64, p, p, p, p, sz, p]
     lib.sfc_moe_dispatch.argtypes = [i64, i64, i64, i32] + rows + [i32, p, p] + rows + [p]
@@ -47,9 +50,12 @@ def _declare() -> None:
     lib.sfc_moe_gemm_mx4_ex.argtypes = [i64, i64, i64, i32] + mx + [p, i64, i64, p, i64, i64, p] + rows + [i32, p]
     lib.sfc_moe_wgrad_mx4_ex.argtypes = [i64, i64, i64, i32] + mx + mx + [p] + rows + [i64, i32, p]
     for name in __all__:
-        if name.startswith("sfc_") and name != "sfc_moe_sort_rows":
+        if name.startswith("sfc_") and name != "sfc_moe_sort_rows" and not name.endswith("_size"):
             getattr(lib, name).restype = i32
-    lib.sfc_moe_sort_ws_size.restype = sz
+    for name in ("sfc_gemm_mx4_ws_ex", "sfc_mx4_linear_ws"):
+        getattr(lib, name).restype = i32
+    for name in ("sfc_gemm_mx4_ws_size", "sfc_mx4_linear_ws_size", "sfc_moe_sort_ws_size"):
+        getattr(lib, name).restype = sz
 
 
 _declare()
@@ -169,6 +175,15 @@ def _weights(t, what, count):
     return None if t is None else _vector(t, "weights", what, _F32, count)
 
 
+def _memory(t, what):
+    """(pointer, bytes) of a caller's workspace, a contiguous tensor of any type.  An empty one, which has
+    no pointer, is still the caller's: no call that needs memory takes it."""
+    _tensor(t, "workspace", what)
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: workspace must be contiguous")
+    return t.data_ptr() or 16, t.numel() * t.element_size()
+
+
 def _topk(topk, what):
     if topk < 1:
         raise ValueError(f"{what}: topk must be >= 1")
@@ -217,26 +232,43 @@ def sfc_mx4_dequant(Q, S, Y, stream=None) -> None:
            what)
 
 
-def sfc_gemm_mx4_ex(A, As, B, Bs, C, stream=None) -> None:
-    """C (M, N), float32 or bfloat16, = A B^T with A (M, K) and B (N, K) in 4 bits."""
+def sfc_gemm_mx4_ws_size(M: int, N: int, K: int, dtype=torch.float32) -> int:
+    """Bytes of the workspace that sfc_gemm_mx4_ex takes for an output of `dtype` (0: none)."""
+    return int(lib.sfc_gemm_mx4_ws_size(M, N, K, _TYPES[dtype]))
+
+
+def sfc_mx4_linear_ws_size(M: int, N: int, K: int, dtype=torch.float32) -> int:
+    """As sfc_gemm_mx4_ws_size, for sfc_mx4_linear."""
+    return int(lib.sfc_mx4_linear_ws_size(M, N, K, _TYPES[dtype]))
+
+
+def sfc_gemm_mx4_ex(A, As, B, Bs, C, stream=None, workspace=None) -> None:
+    """C (M, N), float32 or bfloat16, = A B^T with A (M, K) and B (N, K) in 4 bits.  workspace: None
+    (library memory of the stream) or a tensor of sfc_gemm_mx4_ws_size() bytes."""
     what = "sfc_gemm_mx4_ex"
     a, b = _mx4(A, As, "A", what), _mx4(B, Bs, "B", what)
     M, K, N = A.shape[0], 32 * As.shape[1], B.shape[0]
     if Bs.shape[1] != As.shape[1]:
         raise ValueError(f"{what}: shape mismatch: A {tuple(A.shape)} B {tuple(B.shape)}")
     pc, ldc, kind = _rows(C, "C", what, (M, N))
+    if workspace is not None:
+        return _check(lib.sfc_gemm_mx4_ws_ex(M, N, K, *a, *b, pc, ldc, kind, *_memory(workspace, what), _stream(stream)), what)
     _check(lib.sfc_gemm_mx4_ex(M, N, K, *a, *b, pc, ldc, kind, _stream(stream)), what)
 
 
-def sfc_mx4_linear(X, W, Ws, Y, stream=None) -> None:
+def sfc_mx4_linear(X, W, Ws, Y, stream=None, workspace=None) -> None:
     """Y (M, N) = X W^T with X (M, K), float32 or bfloat16, brought to 4 bits in the call and
-    W (N, K) in 4 bits."""
+    W (N, K) in 4 bits.  workspace: None or a tensor of sfc_mx4_linear_ws_size() bytes; graphs
+    that are replayed at once need workspaces of their own."""
     what = "sfc_mx4_linear"
     px, ldx, kind = _rows(X, "X", what)
     M, K = X.shape
     w = _mx4(W, Ws, "W", what, cols=K)
     N = W.shape[0]
     py, ldy, out = _rows(Y, "Y", what, (M, N))
+    if workspace is not None:
+        return _check(lib.sfc_mx4_linear_ws(M, N, K, px, ldx, kind, *w, py, ldy, out, *_memory(workspace, what), _stream(stream)),
+                      what)
     _check(lib.sfc_mx4_linear(M, N, K, px, ldx, kind, *w, py, ldy, out, _stream(stream)), what)
 
 
@@ -254,8 +286,7 @@ def sfc_moe_sort(ids, offsets, order, pos, align: int = 1, workspace=None, strea
     po, pr = _ints(offsets, "offsets", what, None), _ints(order, "order", what, None)
     ws, ws_bytes = None, 0
     if workspace is not None:
-        _tensor(workspace, "workspace", what)
-        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        ws, ws_bytes = _memory(workspace, what)
     _check(lib.sfc_moe_sort(slots, offsets.numel() - 1, align, pi, order.numel(), po, pr, pp, ws, ws_bytes,
                             _stream(stream)), what)
 
