@@ -184,10 +184,17 @@ def _memory(t, what):
     return t.data_ptr() or 16, t.numel() * t.element_size()
 
 
+def _int(v, name, what):
+    """v, if it fits a C int (ctypes would cut it to 32 bits)."""
+    if not -(1 << 31) <= v < 1 << 31:
+        raise ValueError(f"{what}: {name} must be < 2^31 (got {v})")
+    return v
+
+
 def _topk(topk, what):
     if topk < 1:
         raise ValueError(f"{what}: topk must be >= 1")
-    return topk
+    return _int(topk, "topk", what)
 
 
 def mx4_empty(rows: int, cols: int, lead=(), device="cuda"):
@@ -287,7 +294,8 @@ def sfc_moe_sort(ids, offsets, order, pos, align: int = 1, workspace=None, strea
     ws, ws_bytes = None, 0
     if workspace is not None:
         ws, ws_bytes = _memory(workspace, what)
-    _check(lib.sfc_moe_sort(slots, offsets.numel() - 1, align, pi, order.numel(), po, pr, pp, ws, ws_bytes,
+    experts = _int(offsets.numel() - 1, "the number of experts", what)
+    _check(lib.sfc_moe_sort(slots, experts, _int(align, "align", what), pi, order.numel(), po, pr, pp, ws, ws_bytes,
                             _stream(stream)), what)
 
 
@@ -330,7 +338,7 @@ def _slots_per_token(slots, tokens, what):
         return 1
     if slots == 0 or slots % tokens:
         raise ValueError(f"{what}: pos has {slots} elements, expected a multiple of {tokens} tokens")
-    return slots // tokens
+    return _int(slots // tokens, "topk", what)
 
 
 def sfc_moe_combine_grad(dY, Ys, order, pos, weights, dYs, dW, stream=None) -> None:
@@ -358,7 +366,7 @@ def sfc_moe_gemm_mx4_ex(A, As, B, Bs, offsets, C, stream=None) -> None:
     expert; rows offsets[e] .. offsets[e+1]-1 are expert e's.  4-bit operands."""
     what = "sfc_moe_gemm_mx4_ex"
     a, b = _mx4(A, As, "A", what), _mx4(B, Bs, "B", what, lead=1)
-    rows, K, E, N = A.shape[0], 32 * As.shape[1], B.shape[0], B.shape[1]
+    rows, K, E, N = A.shape[0], 32 * As.shape[1], _int(B.shape[0], "the number of experts", what), B.shape[1]
     if Bs.shape[2] != As.shape[1]:
         raise ValueError(f"{what}: shape mismatch: A {tuple(A.shape)} B {tuple(B.shape)}")
     pc, ldc, kind = _rows(C, "C", what, (rows, N))
@@ -376,7 +384,7 @@ def sfc_moe_wgrad_mx4_ex(A, As, B, Bs, offsets, C, stream=None) -> None:
         raise ValueError(f"{what}: shape mismatch: A {tuple(A.shape)} B {tuple(B.shape)}")
     if not isinstance(C, _Tensor) or C.dim() != 3:
         raise ValueError(f"{what}: C must be a 3-D tensor")
-    E = C.shape[0]
+    E = _int(C.shape[0], "the number of experts", what)
     po = _ints(offsets, "offsets", what, None)
     if E < 1 or offsets.numel() != E + 1 or C.shape[1] != M or C.shape[2] != N:
         raise ValueError(f"{what}: shape mismatch: A {tuple(A.shape)} B {tuple(B.shape)} offsets "
