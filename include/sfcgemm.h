@@ -518,8 +518,9 @@ int sfc_moe_gemm_mx4_ex(int64_t rows, int64_t N, int64_t K, int experts,
  * offsets[e+1]-1, for every expert (zeros for one without rows): the weight gradient, A
  * being the transposed dY (M x rows) and B the transposed X (N x rows), both with their
  * blocks along the sorted rows.  Segments must start at multiples of 32
- * (sfc_moe_sort's align); a start that does not is taken down to one.  C[e] lies
- * stride_c elements after C[e-1], M x N, ldc.
+ * (sfc_moe_sort's align); a start that does not is taken down to one, and the end of the last
+ * segment up to one, for 32 rows share a scale.  C[e] lies stride_c elements after C[e-1],
+ * M x N, ldc; the experts' rows may lie in turn (stride_c < ldc) but not overlap.
  */
 int sfc_moe_wgrad_mx4_ex(int64_t M, int64_t N, int64_t rows, int experts,
                          const void *A, int64_t lda, const void *As, int64_t ldas,

@@ -168,7 +168,8 @@ inline Checked check_moe_wgrad_mx4(int64_t M, int64_t N, int64_t rows, int exper
   if (M == 0 || N == 0) return ok();
   SFC_RETURN_IF(check_rows(C, M, N, ldc, out_type, "C is NULL", "ldc < N"));
   if (experts > 1 && stride_c < 0) return fail(SFC_ERR_INVALID_ARG, "the stride between the experts' C must be >= 0");
-  if (experts > 1 && stride_c < (M - 1) * ldc + N)
+  // one expert's matrix behind the other, or all experts' rows m before their rows m + 1
+  if (experts > 1 && stride_c < (M - 1) * ldc + N && (stride_c < N || ldc < (experts - 1) * stride_c + N))
     return fail(SFC_ERR_INVALID_ARG, "the experts' C overlap");
   SFC_RETURN_IF(check_index(offsets, "offsets is NULL"));
   SFC_RETURN_IF(check_mx4(A, lda, As, ldas, M, rows));
