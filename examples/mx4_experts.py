@@ -9,7 +9,7 @@ y = W2 silu(W1 x), and sums the experts' outputs with the router's weights:
              silu; 4 bits; the second product; sfc_moe_combine
   backward   sfc_moe_combine_grad; each product's two gradients, the output gradient
              brought to 4 bits along both ways in one read; the gather's gradient is
-             sfc_moe_combine without weights
+             sfc_moe_combine without weights; the router's part by its formulas in fp32
 
 The experts' rows start at multiples of 32, so that no block of 32 rows, which share a
 scale in the weight gradient, crosses experts.  Master weights are bf16 and go to 4 bits
@@ -47,12 +47,26 @@ class Experts:
             self.qt.append(qt)
 
     def route(self, x):
-        p, ids = torch.softmax(x.float() @ self.router, dim=1).topk(self.topk, dim=1)
-        return ids.to(torch.int32), p / p.sum(1, keepdim=True)
+        """(ids, weights, what route_backward needs): the topk experts of each token and their shares."""
+        p = torch.softmax(x.float() @ self.router, dim=1)
+        top, ids = p.topk(self.topk, dim=1)
+        total = top.sum(1, keepdim=True)
+        weights = top / total
+        return ids.to(torch.int32), weights, (x, p, ids, weights, total)
+
+    def route_backward(self, dweights, kept):
+        """(dx, d router) from the gradient of the weights, the choice of experts being fixed.
+        weights = top / total:  d top = (d weights - <d weights, weights>) / total, 0 for the others;
+        p = softmax(l):         d l = p (d p - <d p, p>);  l = x router."""
+        x, p, ids, weights, total = kept
+        dtop = (dweights - (dweights * weights).sum(1, keepdim=True)) / total
+        dp = torch.zeros_like(p).scatter_(1, ids, dtop)
+        dl = p * (dp - (dp * p).sum(1, keepdim=True))
+        return dl @ self.router.t(), x.float().t() @ dl
 
     def forward(self, x, keep=False):
         T, dim = x.shape
-        ids, weights = self.route(x)
+        ids, weights, routing = self.route(x)
         rows = so.sfc_moe_sort_rows(ids.numel(), self.E, ALIGN if keep else 1)
         new = lambda *shape: torch.empty(shape, dtype=torch.int32, device="cuda")
         offsets, order, pos = new(self.E + 1), new(rows), new(ids.numel())
@@ -69,15 +83,15 @@ class Experts:
         y = torch.empty_like(x)
         so.sfc_moe_combine(ys, pos, y, weights=weights)
         if keep:
-            self.kept = (x, weights, offsets, order, pos, h, a, ys)
+            self.kept = (x, weights, routing, offsets, order, pos, h, a, ys)
         return y
 
     def backward(self, dy):
-        """(dx, dw1, dw2, d(router weights)) of the last forward(keep=True)."""
-        x, weights, offsets, order, pos, h, a, ys = self.kept
+        """(dx, dw1, dw2, d router) of the last forward(keep=True)."""
+        x, weights, routing, offsets, order, pos, h, a, ys = self.kept
         rows, dim, hidden = ys.shape[0], x.shape[1], a.shape[1]
-        dys, dp = torch.empty_like(ys), torch.empty_like(weights)
-        so.sfc_moe_combine_grad(dy, ys, order, pos, weights, dys, dp)
+        dys, dweights = torch.empty_like(ys), torch.empty_like(weights)
+        so.sfc_moe_combine_grad(dy, ys, order, pos, weights, dys, dweights)
 
         def product_grad(g, act, act_order, wt, n_in, n_out):
             # the output gradient in 4 bits along its rows (for d act) and its columns (for dW)
@@ -96,11 +110,13 @@ class Experts:
         dxs, dw1 = product_grad(dh, x, order, self.qt[0], dim, hidden)
         dx = torch.empty_like(x)
         so.sfc_moe_combine(dxs, pos, dx)
-        return dx, dw1, dw2, dp
+        dx_router, drouter = self.route_backward(dweights, routing)
+        return (dx.float() + dx_router).to(dx.dtype), dw1, dw2, drouter
 
-    def step(self, dw1, dw2, lr):
+    def step(self, dw1, dw2, drouter, lr):
         self.w1 -= (lr * dw1).bfloat16()
         self.w2 -= (lr * dw2).bfloat16()
+        self.router -= lr * drouter
         self.quantise()
 
 
@@ -115,8 +131,8 @@ def train(steps=20, experts=8, dim=512, hidden=1024, tokens=2000, topk=2, lr=40.
         y = layer.forward(x, keep=True)
         diff = y.float() - target
         losses.append(diff.square().mean())
-        _, dw1, dw2, _ = layer.backward((2 * diff / diff.numel()).bfloat16())
-        layer.step(dw1, dw2, lr)
+        _, dw1, dw2, drouter = layer.backward((2 * diff / diff.numel()).bfloat16())
+        layer.step(dw1, dw2, drouter, lr)
     return layer, [float(v) for v in torch.stack(losses)]
 
 
