@@ -380,6 +380,9 @@ hipError_t launch_moe_dispatch(const MoeRowsParams& in, bool bf16, int num_cus, 
 }
 
 hipError_t launch_moe_combine(const MoeRowsParams& p, bool bf16, int num_cus, hipStream_t stream) {
+  // (us, through / past, 2 choices: fp32 8192x1024 22.3 / 19.0, 131072x64 22.8 / 19.7, 16384x1024 42.4 / 40.5,
+  // 8192x4096 77.7 / 77.3, 16384x4096 155 / 153, 1 choice 8192x8192 104 / 106; bf16 16384x1024 21.5 / 17.1,
+  // 65536x256 22.3 / 16.8, 16384x4096 79.8 / 74.5)
   const bool past = streams_past_caches(p.tokens * p.cols * (bf16 ? 2 : 4));
   const RowShape sh = row_shape(p.tokens, (p.cols + 7) / 8, num_cus);
   const dim3 g((unsigned)(sh.row_blocks * sh.splits)), b(256);
@@ -402,7 +405,12 @@ hipError_t launch_moe_combine_grad(const MoeRowsParams& p, bool bf16, int num_cu
   // x 4096 bf16 67 / 81 / -, 16384 x 1024 - / 35 / -, 16384 x 200 - / 12.5 / 8.1,
   // 16384 x 64 - / 10.5 / 5.2)
   const int lanes = p.cols >= 2048 ? 256 : p.cols > 256 ? 64 : 16;
-  const bool past = streams_past_caches(p.rows * p.cols * (bf16 ? 2 : 4));
+  // fp32 rows of 128 MB or more stay in the caches, which join a line's halves (us, through / past, 2 choices:
+  // fp32 8192x1024, 64 MB, 39.3 / 33.9, 131072x64 66 / 61, 16384x1024, 128 MB, 73.3 / 75.7, 4096x4096 71.8 / 76.2,
+  // 65536x256 79 / 82, 8192x4096, 256 MB, 137 / 150, 16384x4096 268 / 295; bf16 16384x1024, 64 MB, 38.5 / 32.2,
+  // 131072x64 40 / 35, 8192x4096, 128 MB, 70.0 / 69.0, 16384x4096 137 / 136)
+  const int64_t bytes = p.rows * p.cols * (bf16 ? 2 : 4);
+  const bool past = streams_past_caches(bytes) && (bf16 || bytes < (int64_t)128 << 20);
   const int64_t groups = ((p.end_token - p.first_token) * lanes + 255) / 256;
   const int64_t clear = (p.end_row - p.first_row + 15) / 16;
   const dim3 g((unsigned)(groups + clear)), b(256);

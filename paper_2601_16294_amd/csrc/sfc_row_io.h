@@ -67,8 +67,8 @@ __device__ __forceinline__ Raw8<BF16> zero8() {
 // Whether a kernel's output of `bytes` goes past the caches: it will not be found there, and
 // the rows that are read stay.  8192 x 4096 bf16 rows: dispatch 45.6 -> 40.8 us, combine
 // 39.4 -> 36.6, its gradient 66.9 -> 64.5, dequantisation 17.4 -> 13.5; below 32 MB the next
-// kernel may find the output in the caches.  (fp32 rows, two stores a lane: combine and its gradient
-// gain or lose 10 % with the size, dispatch and dequantisation lose, see there.)
+// kernel may find the output in the caches.  fp32 rows, two stores a lane, gain less or lose: each
+// kernel's launch says which.
 inline bool streams_past_caches(int64_t bytes) { return bytes >= (int64_t)32 << 20; }
 
 typedef row_u32x4 any_u32x4 __attribute__((aligned(2)));
