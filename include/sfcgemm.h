@@ -390,8 +390,9 @@ int sfc_mx4_dequant(int64_t rows, int64_t cols,
  * blocks along K; C fp32 or bf16 (rounded to nearest even from the fp32 sums).
  *   K          a multiple of 32 (SFC_ERR_INVALID_ARG otherwise); K == 0: C = 0.
  * Products and block sums are exact, sums of blocks fp32.  Few rows run on kernels that
- * stream B once: up to 16 with A in registers while K <= 8192 (16384 where N is large),
- * and up to 64 while K <= 4096.  The others run on 256x256 or 128x128 blocks along the
+ * stream B once: up to 16 rows at any K (with A in registers while K <= 8192, or 16384 where N
+ * is large), up to 32 while K <= 4096 and N < 2^28, up to 64 while K <= 4096 and
+ * N <= 4096.  The others run on 256x256 or 128x128 blocks along the
  * curve, K in up to 16 layers where an estimate of the time favours it (copies in
  * library memory, as for sfc_gemm: replays of graphs recorded on one stream must then not
  * overlap each other, but with a workspace of their own).  The choice depends on M, N, K and

@@ -26,13 +26,18 @@
 //   * the MFMA takes B first, so a lane ends with one row of C and runs of 4 columns; the
 //     block leaves through LDS, a wave's 32-row strips at a time, as whole row segments.
 //
-// Bound: power, then the stores.  On random operands MFMAs that only read registers reach
-// 6.3-6.5 PFLOP/s (zeros: 9.5): the clock falls to 1.6 GHz.  Here (bf16 out) 8192^3 takes
-// 261 us (4.2 PFLOP/s), 16384^3 1900 (4.6), 4096x4096x16384 127 (4.3), 4096x14336x4096 136
-// (3.5; 125 without its stores), 8192x4096x4096 75 (66 without).  The next block's first stages
-// loaded before the stores, and waited for past them, gained 0-1 %: the stores wait for the
-// memory.  Weight gradients of 8 experts, 2048x4096 fp32, 8192 rows: 88 us, 68 without the
-// stores of 268 MB, five stages to a block.
+// Bound: the clock that power allows, times the share of it in which MFMAs run.  On random
+// operands MFMAs that only read registers reach 6.3-6.5 PFLOP/s (zeros: 9.5) at 1.6 GHz, always
+// busy.  Here (normal values to 4 bits, bf16 out) 8192^3 runs at 1.74 GHz with MFMAs busy in 57 % of
+// the cycles and the waves waiting in 18 %, 4096x14336x4096 at 2.0 GHz, 41 % and 20 %: 3.5 rounds of
+// blocks, whose stores all workgroups begin at once.  LDS conflicts are 13 % of LDS cycles.
+// Several hundred calls in a row: 8192^3 261 us (4.2 PFLOP/s), 16384^3 1910 (4.6), 4096x4096x16384 130
+// (4.2), 4096x14336x4096 139 (3.45; 11 less without its stores), 8192x4096x4096 80 (3.45; 9 less).  The
+// first 20 calls after a rest, before the clock has settled: 309, 1960, 142, 154, 79.
+// The next block's first stages loaded before the stores, and waited for past them, gained
+// 0-1 %: the stores wait for the memory.  Weight gradients of 8 experts, 2048x4096, 8192 rows: fp32 88 us
+// (68 without the stores of 268 MB), five stages to a block; 8672 rows, outputs in rotation, fp32 107,
+// bf16 79.
 #pragma once
 #include "sfc_gemm_kernel.h"
 #include "sfc_ops_params.h"

@@ -345,6 +345,10 @@ static const void* few_kernel(Mx4Rows rows, int tpw) {
                   : reinterpret_cast<const void*>(&mx4_few_kernel<FN, OB, kRowsCodes, 2>);
 }
 
+// Whole blocks of columns to a workgroup, as few as put at most one workgroup on a CU: 14336 columns
+// are 224 workgroups of two blocks each, and 32 CUs have none.  (us, that / up to two workgroups to a CU,
+// 448 there, weights in rotation: 16x14336x4096 9.3 / 11.0, 16x11008x4096 10.0 / 10.8, 16x28672x4096
+// 16.6 / 18.2.)
 template <int FN>
 static hipError_t few_launch(const Mx4GemmParams& p, Mx4Rows rows, int num_cus, bool ob, hipStream_t stream) {
   const int64_t turns = (p.K + kTurn - 1) / kTurn;

@@ -59,7 +59,7 @@ struct Mx4GemmParams {
   int experts;
   const int32_t* offsets;    // experts + 1
   int layers;                // kMxDense: ranges of K, each with a copy of C
-  bool past;                 // a bf16 C goes past the caches
+  bool past;                 // C goes past the caches
   // launch_mx4_few: A as fp32 or bf16 rows (X, ldx elements, x_cols of them in a row), brought
   // to 4 bits on the way in
   const void* X;
