@@ -15,6 +15,7 @@
 // Bound: memory, every row read and written once (a token's row once per choice).  8192
 // tokens x 4096 bf16, 2 of 8 experts: dispatch 40.8 us (4.9 TB/s), combine 36.7 (5.5), its
 // gradient 66 (5.1); a copy of as much runs at 5.2.
+#include "sfc_launch.h"
 #include "sfc_ops_params.h"
 #include "sfc_row_io.h"
 
@@ -178,20 +179,18 @@ __global__ __launch_bounds__(1024) void moe_sort_kernel(MoeSortParams p, int chu
 hipError_t launch_moe_sort(const MoeSortParams& p, hipStream_t stream) {
   const int chunks = p.slots > 0 ? (int)((p.slots + kSortChunk - 1) / kSortChunk) : 1;
   if (chunks > 1) {
-    hipLaunchKernelGGL(moe_count_kernel, dim3(chunks), dim3(1024), p.experts * 4u, stream, p);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = launch_kernel(moe_count_kernel, dim3(chunks), dim3(1024), p.experts * 4u, stream, p);
     if (e != hipSuccess) return e;
   }
   if (chunks > kSortScan) {
-    hipLaunchKernelGGL(moe_scan_kernel, dim3((p.experts + 15) / 16), dim3(1024), 0, stream, p.counts, p.experts, chunks);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = launch_kernel(moe_scan_kernel, dim3((p.experts + 15) / 16), dim3(1024), 0, stream, p.counts, p.experts,
+                                       chunks);
     if (e != hipSuccess) return e;
   }
   int bits = 0;
   while ((1 << bits) < p.experts) ++bits;
   const unsigned lds = (unsigned)(kSortWaves * p.experts + kSortWaves) * 4u;
-  hipLaunchKernelGGL(moe_sort_kernel, dim3(chunks), dim3(1024), lds, stream, p, chunks, bits);
-  return hipGetLastError();
+  return launch_kernel(moe_sort_kernel, dim3(chunks), dim3(1024), lds, stream, p, chunks, bits);
 }
 
 // ---- dispatch ------------------------------------------------------------------------------
@@ -373,10 +372,9 @@ hipError_t launch_moe_dispatch(const MoeRowsParams& in, bool bf16, int num_cus, 
   const bool past = bf16 && streams_past_caches(p.rows * p.cols * 2);
   const RowShape sh = row_shape(p.rows, (p.cols + 7) / 8, num_cus);
   const dim3 g((unsigned)(sh.row_blocks * sh.splits)), b(256);
-  if (past) hipLaunchKernelGGL((moe_dispatch_kernel<true, true>), g, b, 0, stream, p, sh);
-  else if (bf16) hipLaunchKernelGGL((moe_dispatch_kernel<true, false>), g, b, 0, stream, p, sh);
-  else hipLaunchKernelGGL((moe_dispatch_kernel<false, false>), g, b, 0, stream, p, sh);
-  return hipGetLastError();
+  if (past) return launch_kernel(moe_dispatch_kernel<true, true>, g, b, 0, stream, p, sh);
+  if (bf16) return launch_kernel(moe_dispatch_kernel<true, false>, g, b, 0, stream, p, sh);
+  return launch_kernel(moe_dispatch_kernel<false, false>, g, b, 0, stream, p, sh);
 }
 
 hipError_t launch_moe_combine(const MoeRowsParams& p, bool bf16, int num_cus, hipStream_t stream) {
@@ -386,11 +384,10 @@ hipError_t launch_moe_combine(const MoeRowsParams& p, bool bf16, int num_cus, hi
   const bool past = streams_past_caches(p.tokens * p.cols * (bf16 ? 2 : 4));
   const RowShape sh = row_shape(p.tokens, (p.cols + 7) / 8, num_cus);
   const dim3 g((unsigned)(sh.row_blocks * sh.splits)), b(256);
-  if (bf16 && past) hipLaunchKernelGGL((moe_combine_kernel<true, true>), g, b, 0, stream, p, sh);
-  else if (bf16) hipLaunchKernelGGL((moe_combine_kernel<true, false>), g, b, 0, stream, p, sh);
-  else if (past) hipLaunchKernelGGL((moe_combine_kernel<false, true>), g, b, 0, stream, p, sh);
-  else hipLaunchKernelGGL((moe_combine_kernel<false, false>), g, b, 0, stream, p, sh);
-  return hipGetLastError();
+  if (bf16 && past) return launch_kernel(moe_combine_kernel<true, true>, g, b, 0, stream, p, sh);
+  if (bf16) return launch_kernel(moe_combine_kernel<true, false>, g, b, 0, stream, p, sh);
+  if (past) return launch_kernel(moe_combine_kernel<false, true>, g, b, 0, stream, p, sh);
+  return launch_kernel(moe_combine_kernel<false, false>, g, b, 0, stream, p, sh);
 }
 
 template <bool BF16, bool PAST>

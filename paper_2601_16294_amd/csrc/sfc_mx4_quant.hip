@@ -12,8 +12,9 @@
 // rows 17.5 us (4.8 TB/s), back 13.4 (6.3; the codes are still cached); a copy of as many
 // values 25.9 (5.2).  Three such matrices in turn, which the caches hold in part: bf16 14.1 along the
 // rows, 14.7 along the columns, 24.6 both ways; fp32 27.9 (5.5 TB/s), 33.2 and 37.7.
-#include "sfc_ops_params.h"
+#include "sfc_launch.h"
 #include "sfc_mx4_convert.h"
+#include "sfc_ops_params.h"
 
 namespace sfc {
 
@@ -297,20 +298,19 @@ __global__ __launch_bounds__(64 * W, 4) void mx4_quant_cols_kernel(Mx4QuantParam
 }
 
 template <int W>
-static void launch_cols(const Mx4QuantParams& p, bool in_bf16, dim3 g, dim3 b, int rg, hipStream_t stream) {
-  if (in_bf16 && p.Q) hipLaunchKernelGGL((mx4_quant_cols_kernel<true, true, W>), g, b, 0, stream, p, rg);
-  else if (in_bf16) hipLaunchKernelGGL((mx4_quant_cols_kernel<true, false, W>), g, b, 0, stream, p, rg);
-  else if (p.Q) hipLaunchKernelGGL((mx4_quant_cols_kernel<false, true, W>), g, b, 0, stream, p, rg);
-  else hipLaunchKernelGGL((mx4_quant_cols_kernel<false, false, W>), g, b, 0, stream, p, rg);
+static hipError_t launch_cols(const Mx4QuantParams& p, bool in_bf16, dim3 g, dim3 b, int rg, hipStream_t stream) {
+  if (in_bf16 && p.Q) return launch_kernel(mx4_quant_cols_kernel<true, true, W>, g, b, 0, stream, p, rg);
+  if (in_bf16) return launch_kernel(mx4_quant_cols_kernel<true, false, W>, g, b, 0, stream, p, rg);
+  if (p.Q) return launch_kernel(mx4_quant_cols_kernel<false, true, W>, g, b, 0, stream, p, rg);
+  return launch_kernel(mx4_quant_cols_kernel<false, false, W>, g, b, 0, stream, p, rg);
 }
 
 hipError_t launch_mx4_quant(const Mx4QuantParams& p, bool in_bf16, int num_cus, hipStream_t stream) {
   if (!p.Qt) {
     const RowShape sh = row_shape(p.rows, (p.cols + 31) / 32 * 4, num_cus);
     const dim3 g((unsigned)(sh.row_blocks * sh.splits)), b(256);
-    if (in_bf16) hipLaunchKernelGGL((mx4_quant_rows_kernel<true>), g, b, 0, stream, p, sh);
-    else hipLaunchKernelGGL((mx4_quant_rows_kernel<false>), g, b, 0, stream, p, sh);
-    return hipGetLastError();
+    if (in_bf16) return launch_kernel(mx4_quant_rows_kernel<true>, g, b, 0, stream, p, sh);
+    return launch_kernel(mx4_quant_rows_kernel<false>, g, b, 0, stream, p, sh);
   }
   const int col_groups = (int)((p.cols + kQtCols - 1) / kQtCols);
   // 256 rows to a workgroup, 128 while that leaves half of the CUs without one (us, 256 / 128 rows, both
@@ -319,9 +319,7 @@ hipError_t launch_mx4_quant(const Mx4QuantParams& p, bool in_bf16, int num_cus, 
   const bool wide = (p.rows + 255) / 256 * col_groups * 2 > num_cus;
   const int rows = wide ? 256 : 128, rg = (int)((p.rows + rows - 1) / rows);
   const dim3 g((unsigned)(rg * col_groups)), b(2 * rows);
-  if (wide) launch_cols<8>(p, in_bf16, g, b, rg, stream);
-  else launch_cols<4>(p, in_bf16, g, b, rg, stream);
-  return hipGetLastError();
+  return wide ? launch_cols<8>(p, in_bf16, g, b, rg, stream) : launch_cols<4>(p, in_bf16, g, b, rg, stream);
 }
 
 // ---- back to fp32 or bf16 ----------------------------------------------------------------
@@ -370,10 +368,9 @@ hipError_t launch_mx4_dequant(const Mx4DequantParams& p, bool out_bf16, int num_
   // (fp32: a lane's two stores leave holes in a line, which only the caches fill: 8192x4096 51 us past
   // them, 26 through)
   const bool past = out_bf16 && streams_past_caches(p.rows * p.cols * 2);
-  if (past) hipLaunchKernelGGL((mx4_dequant_kernel<true, true>), g, b, 0, stream, p, sh);
-  else if (out_bf16) hipLaunchKernelGGL((mx4_dequant_kernel<true, false>), g, b, 0, stream, p, sh);
-  else hipLaunchKernelGGL((mx4_dequant_kernel<false, false>), g, b, 0, stream, p, sh);
-  return hipGetLastError();
+  if (past) return launch_kernel(mx4_dequant_kernel<true, true>, g, b, 0, stream, p, sh);
+  if (out_bf16) return launch_kernel(mx4_dequant_kernel<true, false>, g, b, 0, stream, p, sh);
+  return launch_kernel(mx4_dequant_kernel<false, false>, g, b, 0, stream, p, sh);
 }
 
 }  // namespace sfc

@@ -14,6 +14,7 @@
 // Instead of enumerating the whole curve, each thread descends the recursion
 // for its own position: at every level it counts the cells of the parts, picks
 // the part that holds its position, and rebases.  The depth is O(log(gm+gn)).
+#include "sfc_launch.h"
 #include "sfc_params.h"
 
 namespace sfc {
@@ -77,8 +78,7 @@ hipError_t launch_sfc_order(int gm, int gn, int order, int32_t* dev_out, hipStre
   int blocks = (int)((total + 255) / 256);
   if (blocks > 4096) blocks = 4096;
   if (blocks < 1) blocks = 1;
-  hipLaunchKernelGGL(sfc_order_kernel, dim3(blocks), dim3(256), 0, stream, gm, gn, order, dev_out);
-  return hipGetLastError();
+  return launch_kernel(sfc_order_kernel, dim3(blocks), dim3(256), 0, stream, gm, gn, order, dev_out);
 }
 
 }  // namespace sfc

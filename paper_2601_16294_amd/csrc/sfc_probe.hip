@@ -8,6 +8,7 @@
 // change from one MFMA to the next as they do in the GEMM; with constant
 // operands they do not.  Wave 0 of every workgroup samples the shader clock
 // (s_memtime) against the 100 MHz constant clock (s_memrealtime).
+#include "sfc_launch.h"
 #include "sfc_params.h"
 
 namespace sfc {
@@ -59,13 +60,9 @@ hipError_t run_mfma_probe(int random_operands, int iters, float* dev_out, double
   if (err != hipSuccess) return err;
   err = hipEventCreate(&e1);
   if (err != hipSuccess) { (void)hipEventDestroy(e0); return err; }
-  hipLaunchKernelGGL(mfma_probe_kernel, dim3(256), dim3(256), 0, nullptr, random_operands, 16, dev_out);
-  err = hipGetLastError();
+  err = launch_kernel(mfma_probe_kernel, dim3(256), dim3(256), 0, nullptr, random_operands, 16, dev_out);
   if (err == hipSuccess) err = hipEventRecord(e0, nullptr);
-  if (err == hipSuccess) {
-    hipLaunchKernelGGL(mfma_probe_kernel, dim3(256), dim3(256), 0, nullptr, random_operands, iters, dev_out);
-    err = hipGetLastError();
-  }
+  if (err == hipSuccess) err = launch_kernel(mfma_probe_kernel, dim3(256), dim3(256), 0, nullptr, random_operands, iters, dev_out);
   if (err == hipSuccess) err = hipEventRecord(e1, nullptr);
   if (err == hipSuccess) err = hipEventSynchronize(e1);
   float f = 0.f;

@@ -5,6 +5,7 @@
 //
 // A streaming, HBM-bound kernel: each thread owns 4 consecutive columns of one
 // row and reads them from every layer with 128-bit loads; grid-stride loop.
+#include "sfc_launch.h"
 #include "sfc_params.h"
 
 namespace sfc {
@@ -57,8 +58,7 @@ hipError_t launch_fill_i32(int32_t* p, int64_t n, int32_t v, hipStream_t stream)
   if (n <= 0) return hipSuccess;
   int64_t blocks = (n + 255) / 256;
   if (blocks > 1024) blocks = 1024;
-  hipLaunchKernelGGL(sfc_fill_i32_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, p, n, v);
-  return hipGetLastError();
+  return launch_kernel(sfc_fill_i32_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, p, n, v);
 }
 
 hipError_t launch_reduce(const float* W, int layers, int64_t M, int64_t N, void* C, int64_t ldc,
@@ -70,14 +70,10 @@ hipError_t launch_reduce(const float* W, int layers, int64_t M, int64_t N, void*
   int64_t blocks = (work + 255) / 256;
   if (blocks > 8192) blocks = 8192;
   const dim3 g((unsigned)blocks), b(256);
-  if (out_bf16) {
-    if (vec) hipLaunchKernelGGL((sfc_reduce_kernel<true, true>), g, b, 0, stream, W, layers, M, N, C, ldc);
-    else hipLaunchKernelGGL((sfc_reduce_kernel<true, false>), g, b, 0, stream, W, layers, M, N, C, ldc);
-  } else {
-    if (vec) hipLaunchKernelGGL((sfc_reduce_kernel<false, true>), g, b, 0, stream, W, layers, M, N, C, ldc);
-    else hipLaunchKernelGGL((sfc_reduce_kernel<false, false>), g, b, 0, stream, W, layers, M, N, C, ldc);
-  }
-  return hipGetLastError();
+  if (out_bf16 && vec) return launch_kernel(sfc_reduce_kernel<true, true>, g, b, 0, stream, W, layers, M, N, C, ldc);
+  if (out_bf16) return launch_kernel(sfc_reduce_kernel<true, false>, g, b, 0, stream, W, layers, M, N, C, ldc);
+  if (vec) return launch_kernel(sfc_reduce_kernel<false, true>, g, b, 0, stream, W, layers, M, N, C, ldc);
+  return launch_kernel(sfc_reduce_kernel<false, false>, g, b, 0, stream, W, layers, M, N, C, ldc);
 }
 
 }  // namespace sfc
