@@ -529,6 +529,48 @@ int sfc_moe_wgrad_mx4_ex(int64_t M, int64_t N, int64_t rows, int experts,
                          const int32_t *offsets,
                          void *C, int64_t ldc, int64_t stride_c, int out_type, void *stream);
 
+/* ---- products whose weights depend on the row, in bf16 --------------------------
+ * Operands are row-major bf16 at element alignment (16-byte aligned rows are fastest), sums fp32,
+ * leading dimensions in elements and below 2^22.  Weights W that act as C = A * W^T (N x K, as a
+ * linear layer holds them) are SFC_B_NK; as C = A * W (K x N) SFC_B_KN.  What a product computes
+ * with one of the two, its gradient computes with the other from the same memory.
+ */
+#define SFC_B_NK 0
+#define SFC_B_KN 1
+
+/*
+ * sfc_moe_gemm_ex -- C[p] = A[p] * B[e]^T (SFC_B_NK) or A[p] * B[e] (SFC_B_KN) for the rows p of
+ * every expert e; rows behind the last segment are set to 0 (rows before a first segment that starts
+ * later are not written).
+ *   A          rows x K; with `order` (rows slots, as sfc_moe_sort writes them) a_rows x K, and row p is
+ *              A[order[p] / topk], or a row of zeros where order[p] < 0 or that row does not exist: the
+ *              gather of sfc_moe_dispatch within the product.  It needs a_rows * lda < 2^31 - 2^11
+ *              (SFC_ERR_UNSUPPORTED otherwise).  (order NULL: a_rows and topk are not used.)
+ *   B          `experts` matrices, stride_b elements apart.
+ *   offsets    experts + 1 segment bounds, on the device; bounds outside 0 .. rows count as the
+ *              nearest of them.
+ *   C          rows x N, out_type.
+ * The gradient of A is the same call with the other layout.  The kernel and its block shape are chosen from
+ * rows, N, K and experts, so equal calls give equal bits.
+ */
+int sfc_moe_gemm_ex(int64_t rows, int64_t N, int64_t K, int experts,
+                    const void *A, int64_t lda, const int32_t *order, int64_t a_rows, int topk,
+                    const void *B, int64_t ldb, int64_t stride_b, int b_layout,
+                    const int32_t *offsets,
+                    void *C, int64_t ldc, int out_type, void *stream);
+
+/*
+ * sfc_moe_wgrad_ex -- C[e] = A[seg]^T * B[seg] with seg = offsets[e] .. offsets[e+1]-1, for every
+ * expert (zeros for one without rows): the weight gradient.  A rows x M and B rows x N, as they
+ * lie: the gradient of SFC_B_NK weights with A = dC, B = A of sfc_moe_gemm_ex, that of
+ * SFC_B_KN weights with the two exchanged.  C[e] lies stride_c elements after C[e-1],
+ * M x N, ldc, out_type; the experts' rows may lie in turn (stride_c < ldc) but not overlap.
+ */
+int sfc_moe_wgrad_ex(int64_t M, int64_t N, int64_t rows, int experts,
+                     const void *A, int64_t lda, const void *B, int64_t ldb,
+                     const int32_t *offsets,
+                     void *C, int64_t ldc, int64_t stride_c, int out_type, void *stream);
+
 /* Static text of a return code. */
 const char *sfc_strerror(int code);
 

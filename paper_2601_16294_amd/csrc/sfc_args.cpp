@@ -100,6 +100,26 @@ PyObject* vector(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// stack(t, n, r, c) -> (pointer, leading dimension, stride, type) of a 3-D fp32 or bf16 tensor with unit
+// column stride, n x r x c where they are >= 0.
+PyObject* stack(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  int64_t v[3];
+  if (n != 4) Py_RETURN_NONE;
+  if (!integers(args + 1, v)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const at::Tensor* t = tensor(args[0]);
+    if (!t || t->dim() != 3) Py_RETURN_NONE;
+    const auto type = t->scalar_type();
+    if (type != at::kFloat && type != at::kBFloat16) Py_RETURN_NONE;
+    const int64_t r = t->size(1), c = t->size(2);
+    for (int i = 0; i < 3; ++i)
+      if (v[i] >= 0 && t->size(i) != v[i]) Py_RETURN_NONE;
+    if (t->stride(2) != 1 && c > 1) Py_RETURN_NONE;
+    return Py_BuildValue("NLLi", pointer(*t), (long long)(r > 1 ? t->stride(1) : c ? c : 1), (long long)t->stride(0),
+                         type == at::kFloat ? SFC_OUT_F32 : SFC_OUT_BF16);
+  });
+}
+
 // empty(rows, cols) -> (codes, scales) on the current GPU, rows of scales padded to whole dwords.
 PyObject* empty(PyObject*, PyObject* const* args, Py_ssize_t n) {
   int64_t v[2];
@@ -119,6 +139,7 @@ PyMethodDef kMethods[] = {
     {"rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rows)), METH_FASTCALL, nullptr},
     {"mx4", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mx4)), METH_FASTCALL, nullptr},
     {"vector", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(vector)), METH_FASTCALL, nullptr},
+    {"stack", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(stack)), METH_FASTCALL, nullptr},
     {"empty", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(empty)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_sfcargs", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,103 @@
+// C ABI of the bf16 operators whose weights depend on the row (declarations and contracts in
+// include/sfcgemm.h): argument checks, the choice of kernel and launches.  No entry point
+// synchronises the device or a stream.
+#include <hip/hip_runtime.h>
+
+#include <mutex>
+
+#include "sfc_host.h"
+#include "sfc_moe_params.h"
+#include "sfc_ops_params.h"
+#include "sfc_params.h"
+#include "sfc_rows_validate.h"
+#include "sfcgemm.h"
+
+namespace {
+
+using sfc::Checked;
+
+int reject(const Checked& c) { return sfc::host_error(c.code, c.msg); }
+hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
+const uint16_t* bf16(const void* p) { return static_cast<const uint16_t*>(p); }
+
+// Whether a C of so many elements goes past the caches: from 32 MB on, as for the 4-bit products.
+bool past_caches(int64_t elements, int out_type) { return elements * sfc::type_size(out_type) >= (int64_t)32 << 20; }
+
+// Microseconds of `tasks` blocks over `stages` 64-deep stages.
+double moe_tile_us(bool large, double tasks, double stages, bool out_f32, int num_cus) {
+  const double slots = large ? num_cus : 2 * num_cus;
+  const double full = (double)(int64_t)(tasks / slots), part = tasks / slots - full;
+  double us = full * (large ? 1.4 * stages + (out_f32 ? 11.0 : 5.5) : 0.9 * stages + (out_f32 ? 4.5 : 2.5));
+  if (part > 0) {
+    if (large) us += (1.1 + 0.3 * part) * stages + 2.0 + (out_f32 ? 9.0 : 3.5) * part;
+    else if (part <= 0.5) us += (0.45 + 0.15 * part) * stages + 0.4 + (out_f32 ? 4.5 : 2.2) * part;
+    else us += (0.25 + 0.65 * part) * stages + (out_f32 ? 4.0 : 2.5);
+  }
+  return us;
+}
+
+}  // namespace
+
+extern "C" {
+
+int sfc_moe_gemm_ex(int64_t rows, int64_t N, int64_t K, int experts, const void* A, int64_t lda, const int32_t* order,
+                    int64_t a_rows, int topk, const void* B, int64_t ldb, int64_t stride_b, int b_layout,
+                    const int32_t* offsets, void* C, int64_t ldc, int out_type, void* stream) {
+  const Checked c = sfc::check_moe_gemm(rows, N, K, experts, sfc::kMaxExperts, A, lda, order, a_rows, topk, B, ldb, stride_b,
+                                        b_layout, offsets, C, ldc, out_type);
+  if (c.code != SFC_OK) return reject(c);
+  if (rows == 0 || N == 0) return SFC_OK;
+  std::lock_guard<std::mutex> lock(sfc::host_mutex());
+  int cus = 0;
+  const int rc = sfc::host_num_cus(&cus);
+  if (rc != SFC_OK) return rc;
+  sfc::MoeGemmParams p = {rows, N, K, bf16(A), lda, order, a_rows, order ? topk : 1, bf16(B), ldb, stride_b, C, ldc, 0,
+                          offsets, experts, nullptr, 0, 0, past_caches(rows * N, out_type)};
+  const bool ob = out_type == SFC_OUT_BF16;
+  const double stages = (double)sfc::ceil_div(K > 0 ? K : 1, 64);
+  // blocks of rows: every expert's last one is on average half full
+  auto tasks = [&](int64_t b) { return ((double)rows / (double)b + 0.5 * experts) * (double)sfc::ceil_div(N, b); };
+  const bool big = moe_tile_us(true, tasks(256), stages, !ob, cus) < moe_tile_us(false, tasks(128), stages, !ob, cus);
+  const int b = big ? 256 : 128;
+  p.gn = (int)sfc::ceil_div(N, b);
+  const int64_t most = (sfc::ceil_div(rows, b) + experts) * p.gn, slots = big ? cus : 2 * cus;
+  const int grid = (int)(most < slots ? most : slots);
+  const sfc::MoeLayout layout = b_layout == SFC_B_NK ? sfc::kMoeNK : sfc::kMoeKN;
+  const hipError_t e = big ? sfc::launch_moe_256x256(p, layout, ob, grid, as_stream(stream))
+                           : sfc::launch_moe_128x128(p, layout, ob, grid, as_stream(stream));
+  return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "experts' product");
+}
+
+int sfc_moe_wgrad_ex(int64_t M, int64_t N, int64_t rows, int experts, const void* A, int64_t lda, const void* B,
+                     int64_t ldb, const int32_t* offsets, void* C, int64_t ldc, int64_t stride_c, int out_type,
+                     void* stream) {
+  const Checked c = sfc::check_moe_wgrad(M, N, rows, experts, sfc::kMaxExperts, A, lda, B, ldb, offsets, C, ldc, stride_c,
+                                         out_type);
+  if (c.code != SFC_OK) return reject(c);
+  if (M == 0 || N == 0) return SFC_OK;
+  const hipStream_t st = as_stream(stream);
+  std::lock_guard<std::mutex> lock(sfc::host_mutex());
+  int cus = 0;
+  int rc = sfc::host_num_cus(&cus);
+  if (rc != SFC_OK) return rc;
+  sfc::MoeGemmParams p = {M, N, rows, bf16(A), lda, nullptr, 0, 1, bf16(B), ldb, 0, C, ldc, stride_c,
+                          offsets, experts, nullptr, 0, 0, past_caches(M * N * experts, out_type)};
+  const bool ob = out_type == SFC_OUT_BF16;
+  const double stages = (double)sfc::ceil_div(rows > 0 ? rows : 1, 64 * (int64_t)experts);
+  auto us = [&](int64_t b) {
+    return moe_tile_us(b == 256, (double)(sfc::ceil_div(M, b) * sfc::ceil_div(N, b) * experts), stages, !ob, cus);
+  };
+  const bool big = us(256) < us(128);
+  const int b = big ? 256 : 128;
+  p.gm = (int)sfc::ceil_div(M, b);
+  p.gn = (int)sfc::ceil_div(N, b);
+  rc = sfc::host_table(p.gm, p.gn, st, &p.table);
+  if (rc != SFC_OK) return rc;
+  const int64_t tasks = (int64_t)p.gm * p.gn * experts, slots = big ? cus : 2 * cus;
+  const int grid = (int)(tasks < slots ? tasks : slots);
+  const hipError_t e = big ? sfc::launch_moe_256x256(p, sfc::kMoeTN, ob, grid, st)
+                           : sfc::launch_moe_128x128(p, sfc::kMoeTN, ob, grid, st);
+  return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "experts' weight gradient");
+}
+
+}  // extern "C"

@@ -28,7 +28,10 @@ except ImportError as e:
 
 __all__ = ["SfcError", "mx4_empty", "sfc_mx4_quant", "sfc_mx4_dequant", "sfc_gemm_mx4_ex", "sfc_mx4_linear",
            "sfc_gemm_mx4_ws_size", "sfc_mx4_linear_ws_size", "sfc_moe_sort", "sfc_moe_sort_rows", "sfc_moe_dispatch", "sfc_moe_combine", "sfc_moe_combine_grad",
-           "sfc_moe_gemm_mx4_ex", "sfc_moe_wgrad_mx4_ex"]
+           "sfc_moe_gemm_mx4_ex", "sfc_moe_wgrad_mx4_ex", "SFC_B_NK", "SFC_B_KN", "sfc_moe_gemm_ex", "sfc_moe_wgrad_ex"]
+
+# layouts of weights (sfcgemm.h): N x K as a linear layer holds them, or K x N
+SFC_B_NK, SFC_B_KN = 0, 1
 
 
 def _declare() -> None:
@@ -49,6 +52,8 @@ def _declare() -> None:
     lib.sfc_moe_combine_grad.argtypes = [i64, i64, i64, i32] + rows + rows + [i32, p, p, p] + rows + [p, p]
     lib.sfc_moe_gemm_mx4_ex.argtypes = [i64, i64, i64, i32] + mx + [p, i64, i64, p, i64, i64, p] + rows + [i32, p]
     lib.sfc_moe_wgrad_mx4_ex.argtypes = [i64, i64, i64, i32] + mx + mx + [p] + rows + [i64, i32, p]
+    lib.sfc_moe_gemm_ex.argtypes = [i64, i64, i64, i32] + rows + [p, i64, i32, p, i64, i64, i32, p] + rows + [i32, p]
+    lib.sfc_moe_wgrad_ex.argtypes = [i64, i64, i64, i32] + rows + rows + [p] + rows + [i64, i32, p]
     for name in __all__:
         if name.startswith("sfc_") and name != "sfc_moe_sort_rows" and not name.endswith("_size"):
             getattr(lib, name).restype = i32
@@ -71,7 +76,8 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 # Each gives what the function of its name below gives where the argument is as it should be, else
 # None: the code behind it then names the fault.
-_rows_of, _mx4_of, _vector_of, _empty_of = _sfcargs.rows, _sfcargs.mx4, _sfcargs.vector, _sfcargs.empty
+_rows_of, _mx4_of, _vector_of, _empty_of, _stack_of = (_sfcargs.rows, _sfcargs.mx4, _sfcargs.vector,
+                                                            _sfcargs.empty, _sfcargs.stack)
 _ANY = (-1, -1)
 
 
@@ -113,6 +119,45 @@ def _rows(t, name, what, shape=None):
     if s[1] != 1 and c > 1:
         raise ValueError(f"{what}: {name} must have unit column stride")
     return t.data_ptr(), s[0] if r > 1 else c or 1, code
+
+
+def _bf16(t, name, what, shape=None):
+    """(pointer, leading dimension) of a 2-D bf16 tensor with unit column stride."""
+    p, ld, kind = _rows(t, name, what, shape)
+    if kind != SFC_OUT_BF16:
+        raise TypeError(f"{what}: {name} must be bfloat16 (got {t.dtype})")
+    return p, ld
+
+
+def _stack(t, name, what, shape=None):
+    """(pointer, leading dimension, stride, type code) of a 3-D fp32 or bf16 tensor with unit column stride;
+    sizes of `shape` that are negative may be any."""
+    got = _stack_of(t, *(shape or (-1, -1, -1)))
+    if got is not None:
+        return got
+    _tensor(t, name, what)
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what}: {name} must be float32 or bfloat16 (got {t.dtype})")
+    if t.dim() != 3:
+        raise ValueError(f"{what}: {name} must be 3-D")
+    if shape is not None and any(0 <= n != m for n, m in zip(shape, t.shape)):
+        want = ", ".join("*" if n < 0 else str(n) for n in shape)
+        raise ValueError(f"{what}: shape mismatch: {name} is {tuple(t.shape)}, expected ({want})")
+    r, c = t.shape[1:]
+    if t.stride(2) != 1 and c > 1:
+        raise ValueError(f"{what}: {name} must have unit column stride")
+    return t.data_ptr(), t.stride(1) if r > 1 else c or 1, t.stride(0), code
+
+
+def _weights_of(t, name, what, layout, inner):
+    """(pointer, leading dimension, stride) of stacked bf16 weights whose contracted side is `inner` long."""
+    if layout not in (SFC_B_NK, SFC_B_KN):
+        raise ValueError(f"{what}: layout must be SFC_B_NK or SFC_B_KN")
+    p, ld, stride, kind = _stack(t, name, what, (-1, -1, inner) if layout == SFC_B_NK else (-1, inner, -1))
+    if kind != SFC_OUT_BF16:
+        raise TypeError(f"{what}: {name} must be bfloat16 (got {t.dtype})")
+    return p, ld, stride
 
 
 def _mx4(q, s, name, what, rows=None, cols=None, lead=0):
@@ -391,3 +436,38 @@ def sfc_moe_wgrad_mx4_ex(A, As, B, Bs, offsets, C, stream=None) -> None:
                          f"{tuple(offsets.shape)} C {tuple(C.shape)}")
     pc, ldc, kind = _rows(C[0], "C", what, (M, N))
     _check(lib.sfc_moe_wgrad_mx4_ex(M, N, rows, E, *a, *b, po, pc, ldc, C.stride(0), kind, _stream(stream)), what)
+
+
+def sfc_moe_gemm_ex(A, B, offsets, C, order=None, topk: int = 1, layout: int = SFC_B_NK, stream=None) -> None:
+    """C (rows, N), float32 or bfloat16, = A (rows, K) times, row by row, the weights of the row's expert; rows
+    offsets[e] .. offsets[e+1]-1 are expert e's.  B is (experts, N, K) with SFC_B_NK, used transposed, or
+    (experts, K, N) with SFC_B_KN; A and B bfloat16.  With `order` (sfc_moe_sort's) the rows are
+    A[order // topk], zeros where order is negative."""
+    what = "sfc_moe_gemm_ex"
+    pa, lda = _bf16(A, "A", what)
+    rows, K = A.shape
+    a_rows, po = rows, None
+    if order is not None:
+        po, rows = _ints(order, "order", what, None), order.numel()
+        _topk(topk, what)
+    pb, ldb, stride = _weights_of(B, "B", what, layout, K)
+    E, N = B.shape[0], B.shape[1 if layout == SFC_B_NK else 2]
+    pc, ldc, kind = _rows(C, "C", what, (rows, N))
+    _check(lib.sfc_moe_gemm_ex(rows, N, K, _int(E, "the number of experts", what), pa, lda, po, a_rows, topk, pb, ldb, stride,
+                               layout, _ints(offsets, "offsets", what, E + 1), pc, ldc, kind, _stream(stream)), what)
+
+
+def sfc_moe_wgrad_ex(A, B, offsets, C, stream=None) -> None:
+    """C (experts, M, N), float32 or bfloat16, C[e] = A[seg]^T B[seg] over the sorted rows seg of expert e;
+    A (rows, M) and B (rows, N) bfloat16."""
+    what = "sfc_moe_wgrad_ex"
+    pa, lda = _bf16(A, "A", what)
+    pb, ldb = _bf16(B, "B", what)
+    rows, M = A.shape
+    N = B.shape[1]
+    if B.shape[0] != rows:
+        raise ValueError(f"{what}: shape mismatch: A {tuple(A.shape)} B {tuple(B.shape)}")
+    pc, ldc, stride, kind = _stack(C, "C", what, (-1, M, N))
+    E = C.shape[0]
+    _check(lib.sfc_moe_wgrad_ex(M, N, rows, _int(E, "the number of experts", what), pa, lda, pb, ldb,
+                                _ints(offsets, "offsets", what, E + 1), pc, ldc, stride, kind, _stream(stream)), what)
