@@ -529,9 +529,9 @@ int sfc_moe_wgrad_mx4_ex(int64_t M, int64_t N, int64_t rows, int experts,
                          const int32_t *offsets,
                          void *C, int64_t ldc, int64_t stride_c, int out_type, void *stream);
 
-/* ---- products whose weights depend on the row, in bf16 --------------------------
+/* ---- products of experts in bf16 ---------------------------------------------------
  * Operands are row-major bf16 at element alignment (16-byte aligned rows are fastest), sums fp32,
- * leading dimensions in elements and below 2^22.  Weights W that act as C = A * W^T (N x K, as a
+ * leading dimensions of operands in elements and below 2^22.  Weights W that act as C = A * W^T (N x K, as a
  * linear layer holds them) are SFC_B_NK; as C = A * W (K x N) SFC_B_KN.  What a product computes
  * with one of the two, its gradient computes with the other from the same memory.
  */
@@ -570,6 +570,44 @@ int sfc_moe_wgrad_ex(int64_t M, int64_t N, int64_t rows, int experts,
                      const void *A, int64_t lda, const void *B, int64_t ldb,
                      const int32_t *offsets,
                      void *C, int64_t ldc, int64_t stride_c, int out_type, void *stream);
+
+/* ---- low-rank adapters of many requests -------------------------------------------
+ * Row t of a batch belongs to adapter a = ids[t] (int32, on the device; outside 0 .. adapters-1: to
+ * none) and gets, beside what a shared projection of any type gave it,
+ *     Y[t] = base[t] + V[t] * B[a]^T,   V[t] = scales[a] * X[t] * A[a]^T
+ * with A[a] of rank x K and B[a] of N x rank, bf16, V fp32; ranks up to 256 (adapters of less are
+ * filled up with zeros).  Rows in any order: runs of one adapter's rows (prompts) read its weights
+ * least often.  A row sees its own adapter's weights only, so infinities and NaN stay with their adapter.
+ * The gradients, with U[t] = scales[a] * dY[t] * B[a]: dBase = dY; dX = U[t] * A[a] (added to the shared
+ * projection's); dA[a] = sum of U[t]^T X[t], dB[a] = sum of dY[t]^T V[t] over the adapter's rows t; all
+ * of them calls below with the weights' other layout.  X, dY and weights at element alignment.
+ */
+
+/* sfc_lora_down -- V (rows x rank, fp32, ldv) as above from X (rows x K, bf16): A as rank x K (SFC_B_NK) or
+ * K x rank (SFC_B_KN), stride_a elements from one adapter's to the next; scales NULL: 1; zeros in rows of no
+ * adapter.  U is this call with X = dY and A = B, K x rank. */
+int sfc_lora_down(int64_t rows, int64_t K, int64_t rank, int adapters,
+                  const void *X, int64_t ldx, const void *A, int64_t lda, int64_t stride_a, int layout,
+                  const int32_t *ids, const float *scales,
+                  float *V, int64_t ldv, void *stream);
+
+/* sfc_lora_up -- Y (rows x N, `type`) as above: B as N x rank (SFC_B_NK) or rank x N (SFC_B_KN); base rows x N
+ * of Y's type, NULL: 0, or Y itself; rows of no adapter are base's.  V's products with B are fp32, rounded once
+ * with base; bf16 Y: V is taken to 16 bits (2^-16 of it). */
+int sfc_lora_up(int64_t rows, int64_t N, int64_t rank, int adapters,
+                const float *V, int64_t ldv, const void *B, int64_t ldb, int64_t stride_b, int layout,
+                const int32_t *ids, const void *base, int64_t ld_base,
+                void *Y, int64_t ldy, int type, void *stream);
+
+/* sfc_lora_wgrad -- for every adapter G[a] = sum over t with ids[t] = a of Z[t]^T V[t], columns x rank
+ * (SFC_B_NK), or of V[t]^T Z[t], rank x columns (SFC_B_KN): the gradient of sfc_lora_up's B in
+ * its layout with Z = dY, that of sfc_lora_down's A in the other layout's name with V = U and Z = X (A of
+ * rank x K: SFC_B_KN).  Zeros for an adapter without rows.  Z rows x columns, bf16; G out_type, stride_g
+ * elements from one to the next, not overlapping.  Sums run over a fixed split of the rows: equal calls give
+ * equal bits. */
+int sfc_lora_wgrad(int64_t rows, int64_t columns, int64_t rank, int adapters,
+                   const void *Z, int64_t ldz, const float *V, int64_t ldv, const int32_t *ids,
+                   void *G, int64_t ldg, int64_t stride_g, int layout, int out_type, void *stream);
 
 /* Static text of a return code. */
 const char *sfc_strerror(int code);

@@ -1,0 +1,36 @@
+// Internal interface between the C-ABI layer of the low-rank adapters (sfc_rows_api.cpp) and
+// their HIP kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace sfc {
+
+constexpr int kMaxRank = 256;
+
+struct LoraParams {
+  int64_t rows;
+  int64_t cols;              // down: K; up: N; gradient: columns of Z
+  int rank, adapters;
+  int first_adapter;         // gradient: of this launch
+  const int32_t* ids;        // adapter of every row; one outside 0 .. adapters-1: none
+  // down: rows x cols; gradient: Z, rows x cols
+  const uint16_t* X;
+  int64_t ldx;
+  // down: A, rank x cols (nk) or cols x rank; up: B, cols x rank (nk) or rank x cols
+  const uint16_t* W;
+  int64_t ldw, stride_w;
+  const float* scales;       // down: per adapter, or null
+  float* V;                  // rows x rank: written by down, else read
+  int64_t ldv;
+  // up: base and Y, rows x cols (base may be null, or Y); gradient: cols x rank (nk) or rank x cols
+  const void* base;
+  int64_t ld_base;
+  void* Y;
+  int64_t ldy, stride_y;     // stride_y: gradient, between adapters
+};
+hipError_t launch_lora_down(const LoraParams& p, bool nk, int num_cus, hipStream_t stream);
+hipError_t launch_lora_up(const LoraParams& p, bool nk, bool bf16, int num_cus, hipStream_t stream);
+hipError_t launch_lora_wgrad(const LoraParams& p, bool nk, bool bf16, int num_cus, hipStream_t stream);
+
+}  // namespace sfc

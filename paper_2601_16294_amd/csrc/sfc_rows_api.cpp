@@ -6,6 +6,7 @@
 #include <mutex>
 
 #include "sfc_host.h"
+#include "sfc_lora_params.h"
 #include "sfc_moe_params.h"
 #include "sfc_ops_params.h"
 #include "sfc_params.h"
@@ -34,6 +35,22 @@ double moe_tile_us(bool large, double tasks, double stages, bool out_f32, int nu
     else us += (0.25 + 0.65 * part) * stages + (out_f32 ? 4.0 : 2.5);
   }
   return us;
+}
+
+int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
+
+// Launches a part at a time: rows first .. first + count - 1 and columns col .. col + width - 1, so
+// that a launch has less than 2^32 threads (at most 32 for a row, and 8 for a column of 64 rows).
+template <class F>
+hipError_t lora_parts(int64_t rows, int64_t cols, F launch) {
+  const int64_t width = least(cols, (int64_t)1 << 20);
+  const int64_t height = width > (1 << 12) ? (int64_t)1 << 17 : sfc::kLaunchRows;
+  for (int64_t first = 0; first < rows; first += height)
+    for (int64_t col = 0; col < cols; col += width) {
+      const hipError_t e = launch(first, least(height, rows - first), col, least(width, cols - col));
+      if (e != hipSuccess) return e;
+    }
+  return hipSuccess;
 }
 
 }  // namespace
@@ -98,6 +115,97 @@ int sfc_moe_wgrad_ex(int64_t M, int64_t N, int64_t rows, int experts, const void
   const hipError_t e = big ? sfc::launch_moe_256x256(p, sfc::kMoeTN, ob, grid, st)
                            : sfc::launch_moe_128x128(p, sfc::kMoeTN, ob, grid, st);
   return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "experts' weight gradient");
+}
+
+int sfc_lora_down(int64_t rows, int64_t K, int64_t rank, int adapters, const void* X, int64_t ldx, const void* A, int64_t lda,
+                  int64_t stride_a, int layout, const int32_t* ids, const float* scales, float* V, int64_t ldv, void* stream) {
+  const Checked c = sfc::check_lora_down(rows, K, rank, adapters, sfc::kMaxRank, X, ldx, A, lda, stride_a, layout, ids, scales,
+                                         V, ldv);
+  if (c.code != SFC_OK) return reject(c);
+  if (rows == 0 || rank == 0) return SFC_OK;
+  std::lock_guard<std::mutex> lock(sfc::host_mutex());
+  int cus = 0;
+  const int rc = sfc::host_num_cus(&cus);
+  if (rc != SFC_OK) return rc;
+  const hipError_t e = lora_parts(rows, 1, [&](int64_t first, int64_t count, int64_t, int64_t) {
+    sfc::LoraParams p = {};
+    p.rows = count;
+    p.cols = K;
+    p.rank = (int)rank;
+    p.adapters = adapters;
+    p.ids = ids + first;
+    p.X = bf16(X) + first * ldx;
+    p.ldx = ldx;
+    p.W = bf16(A);
+    p.ldw = lda;
+    p.stride_w = stride_a;
+    p.scales = scales;
+    p.V = V + first * ldv;
+    p.ldv = ldv;
+    return sfc::launch_lora_down(p, layout == SFC_B_NK, cus, as_stream(stream));
+  });
+  return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "adapters, down");
+}
+
+int sfc_lora_up(int64_t rows, int64_t N, int64_t rank, int adapters, const float* V, int64_t ldv, const void* B, int64_t ldb,
+                int64_t stride_b, int layout, const int32_t* ids, const void* base, int64_t ld_base, void* Y, int64_t ldy,
+                int type, void* stream) {
+  const Checked c = sfc::check_lora_up(rows, N, rank, adapters, sfc::kMaxRank, V, ldv, B, ldb, stride_b, layout, ids, base,
+                                       ld_base, Y, ldy, type);
+  if (c.code != SFC_OK) return reject(c);
+  if (rows == 0 || N == 0) return SFC_OK;
+  std::lock_guard<std::mutex> lock(sfc::host_mutex());
+  int cus = 0;
+  const int rc = sfc::host_num_cus(&cus);
+  if (rc != SFC_OK) return rc;
+  const int64_t size = sfc::type_size(type);
+  const hipError_t e = lora_parts(rows, N, [&](int64_t first, int64_t count, int64_t col, int64_t width) {
+    sfc::LoraParams p = {};
+    p.rows = count;
+    p.cols = width;
+    p.rank = (int)rank;
+    p.adapters = adapters;
+    p.ids = ids + first;
+    p.W = bf16(B) + (layout == SFC_B_NK ? col * ldb : col);
+    p.ldw = ldb;
+    p.stride_w = stride_b;
+    p.V = const_cast<float*>(V) + first * ldv;
+    p.ldv = ldv;
+    p.base = base ? static_cast<const char*>(base) + (first * ld_base + col) * size : nullptr;
+    p.ld_base = ld_base;
+    p.Y = static_cast<char*>(Y) + (first * ldy + col) * size;
+    p.ldy = ldy;
+    return sfc::launch_lora_up(p, layout == SFC_B_NK, type == SFC_OUT_BF16, cus, as_stream(stream));
+  });
+  return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "adapters, up");
+}
+
+int sfc_lora_wgrad(int64_t rows, int64_t columns, int64_t rank, int adapters, const void* Z, int64_t ldz, const float* V,
+                   int64_t ldv, const int32_t* ids, void* G, int64_t ldg, int64_t stride_g, int layout, int out_type,
+                   void* stream) {
+  const Checked c = sfc::check_lora_wgrad(rows, columns, rank, adapters, sfc::kMaxRank, Z, ldz, V, ldv, ids, G, ldg, stride_g,
+                                          layout, out_type);
+  if (c.code != SFC_OK) return reject(c);
+  if (columns == 0 || rank == 0) return SFC_OK;
+  std::lock_guard<std::mutex> lock(sfc::host_mutex());
+  int cus = 0;
+  const int rc = sfc::host_num_cus(&cus);
+  if (rc != SFC_OK) return rc;
+  sfc::LoraParams p = {};
+  p.rows = rows;
+  p.cols = columns;
+  p.rank = (int)rank;
+  p.adapters = adapters;
+  p.ids = ids;
+  p.X = bf16(Z);
+  p.ldx = ldz;
+  p.V = const_cast<float*>(V);
+  p.ldv = ldv;
+  p.Y = G;
+  p.ldy = ldg;
+  p.stride_y = stride_g;
+  const hipError_t e = sfc::launch_lora_wgrad(p, layout == SFC_B_NK, out_type == SFC_OUT_BF16, cus, as_stream(stream));
+  return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "adapters, weight gradient");
 }
 
 }  // extern "C"

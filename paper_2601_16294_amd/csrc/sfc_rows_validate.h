@@ -72,4 +72,64 @@ inline Checked check_moe_wgrad(int64_t M, int64_t N, int64_t rows, int experts, 
   return check_blocks(M, N, experts);
 }
 
+// Sizes shared by the adapters' calls.
+inline Checked check_lora_sizes(int64_t rows, int64_t cols, int64_t rank, int adapters, int most_rank, int layout) {
+  SFC_RETURN_IF(check_dims(rows, cols, rank));
+  SFC_RETURN_IF(check_layout(layout));
+  if (adapters < 1) return fail(SFC_ERR_INVALID_ARG, "adapters must be >= 1");
+  if (rank > most_rank) return fail(SFC_ERR_UNSUPPORTED, "ranks up to 256");
+  return ok();
+}
+
+// Stacked weights of n x k (SFC_B_NK) or k x n.
+inline Checked check_lora_weights(const void* W, int64_t n, int64_t k, int64_t ld, int64_t stride, int adapters, int layout) {
+  const bool nk = layout == SFC_B_NK;
+  SFC_RETURN_IF(check_rows(W, nk ? n : k, nk ? k : n, ld, SFC_OUT_BF16, "the adapters' weights are NULL",
+                           "rows of the adapters' weights are longer than their leading dimension"));
+  if (n > 0 && k > 0 && adapters > 1 && stride < 0) return fail(SFC_ERR_INVALID_ARG, "strides must be >= 0");
+  return ok();
+}
+
+inline Checked check_lora_down(int64_t rows, int64_t K, int64_t rank, int adapters, int most_rank, const void* X, int64_t ldx,
+                               const void* A, int64_t lda, int64_t stride_a, int layout, const void* ids, const void* scales,
+                               const void* V, int64_t ldv) {
+  SFC_RETURN_IF(check_lora_sizes(rows, K, rank, adapters, most_rank, layout));
+  if (rows == 0 || rank == 0) return ok();
+  SFC_RETURN_IF(check_rows(V, rows, rank, ldv, SFC_OUT_F32, "V is NULL", "ldv < rank"));
+  SFC_RETURN_IF(check_rows(X, rows, K, ldx, SFC_OUT_BF16, "X is NULL", "ldx < K"));
+  SFC_RETURN_IF(check_lora_weights(A, rank, K, lda, stride_a, adapters, layout));
+  SFC_RETURN_IF(check_weights(scales));
+  return check_index(ids, "ids is NULL");
+}
+
+inline Checked check_lora_up(int64_t rows, int64_t N, int64_t rank, int adapters, int most_rank, const void* V, int64_t ldv,
+                             const void* B, int64_t ldb, int64_t stride_b, int layout, const void* ids, const void* base,
+                             int64_t ld_base, const void* Y, int64_t ldy, int type) {
+  SFC_RETURN_IF(check_lora_sizes(rows, N, rank, adapters, most_rank, layout));
+  if (!type_ok(type)) return fail(SFC_ERR_INVALID_ARG, "unknown element type");
+  if (rows == 0 || N == 0) return ok();
+  SFC_RETURN_IF(check_rows(Y, rows, N, ldy, type, "Y is NULL", "ldy < N"));
+  if (base) SFC_RETURN_IF(check_rows(base, rows, N, ld_base, type, "", "ld_base < N"));
+  if (base == Y && ld_base != ldy) return fail(SFC_ERR_INVALID_ARG, "base may be Y, but not lie across it");
+  SFC_RETURN_IF(check_rows(V, rows, rank, ldv, SFC_OUT_F32, "V is NULL", "ldv < rank"));
+  SFC_RETURN_IF(check_lora_weights(B, N, rank, ldb, stride_b, adapters, layout));
+  return check_index(ids, "ids is NULL");
+}
+
+inline Checked check_lora_wgrad(int64_t rows, int64_t cols, int64_t rank, int adapters, int most_rank, const void* Z,
+                                int64_t ldz, const void* V, int64_t ldv, const void* ids, const void* G, int64_t ldg,
+                                int64_t stride_g, int layout, int out_type) {
+  SFC_RETURN_IF(check_lora_sizes(rows, cols, rank, adapters, most_rank, layout));
+  if (!type_ok(out_type)) return fail(SFC_ERR_INVALID_ARG, "unknown out_type");
+  if (cols == 0 || rank == 0) return ok();
+  const bool nk = layout == SFC_B_NK;
+  const int64_t r = nk ? cols : rank, c = nk ? rank : cols;
+  SFC_RETURN_IF(check_rows(G, r, c, ldg, out_type, "G is NULL", "rows of G are longer than ldg"));
+  SFC_RETURN_IF(check_stack(r, c, ldg, adapters, stride_g, "the adapters' G overlap"));
+  SFC_RETURN_IF(check_rows(Z, rows, cols, ldz, SFC_OUT_BF16, "Z is NULL", "ldz < columns"));
+  SFC_RETURN_IF(check_rows(V, rows, rank, ldv, SFC_OUT_F32, "V is NULL", "ldv < rank"));
+  if (rows > 0) SFC_RETURN_IF(check_index(ids, "ids is NULL"));
+  return ok();
+}
+
 }  // namespace sfc

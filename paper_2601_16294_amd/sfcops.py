@@ -28,7 +28,8 @@ except ImportError as e:
 
 __all__ = ["SfcError", "mx4_empty", "sfc_mx4_quant", "sfc_mx4_dequant", "sfc_gemm_mx4_ex", "sfc_mx4_linear",
            "sfc_gemm_mx4_ws_size", "sfc_mx4_linear_ws_size", "sfc_moe_sort", "sfc_moe_sort_rows", "sfc_moe_dispatch", "sfc_moe_combine", "sfc_moe_combine_grad",
-           "sfc_moe_gemm_mx4_ex", "sfc_moe_wgrad_mx4_ex", "SFC_B_NK", "SFC_B_KN", "sfc_moe_gemm_ex", "sfc_moe_wgrad_ex"]
+           "sfc_moe_gemm_mx4_ex", "sfc_moe_wgrad_mx4_ex", "SFC_B_NK", "SFC_B_KN", "sfc_moe_gemm_ex", "sfc_moe_wgrad_ex",
+           "sfc_lora_down", "sfc_lora_up", "sfc_lora_wgrad"]
 
 # layouts of weights (sfcgemm.h): N x K as a linear layer holds them, or K x N
 SFC_B_NK, SFC_B_KN = 0, 1
@@ -54,6 +55,10 @@ def _declare() -> None:
     lib.sfc_moe_wgrad_mx4_ex.argtypes = [i64, i64, i64, i32] + mx + mx + [p] + rows + [i64, i32, p]
     lib.sfc_moe_gemm_ex.argtypes = [i64, i64, i64, i32] + rows + [p, i64, i32, p, i64, i64, i32, p] + rows + [i32, p]
     lib.sfc_moe_wgrad_ex.argtypes = [i64, i64, i64, i32] + rows + rows + [p] + rows + [i64, i32, p]
+    stack = [p, i64, i64, i32]                   # weights, leading dimension, stride, layout
+    lib.sfc_lora_down.argtypes = [i64, i64, i64, i32] + rows + stack + [p, p] + rows + [p]
+    lib.sfc_lora_up.argtypes = [i64, i64, i64, i32] + rows + stack + [p] + rows + rows + [i32, p]
+    lib.sfc_lora_wgrad.argtypes = [i64, i64, i64, i32] + rows + rows + [p, p, i64, i64, i32, i32, p]
     for name in __all__:
         if name.startswith("sfc_") and name != "sfc_moe_sort_rows" and not name.endswith("_size"):
             getattr(lib, name).restype = i32
@@ -471,3 +476,64 @@ def sfc_moe_wgrad_ex(A, B, offsets, C, stream=None) -> None:
     E = C.shape[0]
     _check(lib.sfc_moe_wgrad_ex(M, N, rows, _int(E, "the number of experts", what), pa, lda, pb, ldb,
                                 _ints(offsets, "offsets", what, E + 1), pc, ldc, stride, kind, _stream(stream)), what)
+
+
+def _f32(t, name, what, shape=None):
+    """(pointer, leading dimension) of a 2-D fp32 tensor with unit column stride."""
+    p, ld, kind = _rows(t, name, what, shape)
+    if kind != SFC_OUT_F32:
+        raise TypeError(f"{what}: {name} must be float32 (got {t.dtype})")
+    return p, ld
+
+
+def sfc_lora_down(X, A, ids, V, scales=None, layout: int = SFC_B_NK, stream=None) -> None:
+    """V (rows, rank), float32, = scales[ids] * X (rows, K) times the transposed A of the row's adapter; zeros where
+    ids (int32, one to a row) names none.  A is (adapters, rank, K) with SFC_B_NK or (adapters, K, rank) with
+    SFC_B_KN; X and A bfloat16, scales float32 or None (1)."""
+    what = "sfc_lora_down"
+    px, ldx = _bf16(X, "X", what)
+    rows, K = X.shape
+    pa, lda, stride = _weights_of(A, "A", what, layout, K)
+    n, rank = A.shape[0], A.shape[1 if layout == SFC_B_NK else 2]
+    pv, ldv = _f32(V, "V", what, (rows, rank))
+    _check(lib.sfc_lora_down(rows, K, rank, _int(n, "the number of adapters", what), px, ldx, pa, lda, stride, layout,
+                             _ints(ids, "ids", what, rows), None if scales is None else _vector(scales, "scales", what, _F32, n),
+                             pv, ldv, _stream(stream)), what)
+
+
+def sfc_lora_up(V, B, ids, Y, base=None, layout: int = SFC_B_NK, stream=None) -> None:
+    """Y (rows, N), float32 or bfloat16, = base + V (rows, rank) times the transposed B of the row's adapter; base's
+    rows (None: 0; it may be Y) where ids names none.  B is (adapters, N, rank) with SFC_B_NK or (adapters,
+    rank, N) with SFC_B_KN, bfloat16."""
+    what = "sfc_lora_up"
+    pv, ldv = _f32(V, "V", what)
+    rows, rank = V.shape
+    pb, ldb, stride = _weights_of(B, "B", what, layout, rank)
+    n, N = B.shape[0], B.shape[1 if layout == SFC_B_NK else 2]
+    py, ldy, kind = _rows(Y, "Y", what, (rows, N))
+    p0, ld0 = None, 0
+    if base is not None:
+        p0, ld0, k0 = _rows(base, "base", what, (rows, N))
+        if k0 != kind:
+            raise TypeError(f"{what}: base must hold Y's type")
+    _check(lib.sfc_lora_up(rows, N, rank, _int(n, "the number of adapters", what), pv, ldv, pb, ldb, stride, layout,
+                           _ints(ids, "ids", what, rows), p0, ld0, py, ldy, kind, _stream(stream)), what)
+
+
+def sfc_lora_wgrad(Z, V, ids, G, layout: int = SFC_B_NK, stream=None) -> None:
+    """G[a] = the sum over the rows t of adapter a of Z[t]^T V[t], G (adapters, columns, rank) with SFC_B_NK, or of
+    V[t]^T Z[t], G (adapters, rank, columns) with SFC_B_KN; Z (rows, columns) bfloat16, V (rows, rank) float32, G
+    float32 or bfloat16."""
+    what = "sfc_lora_wgrad"
+    pz, ldz = _bf16(Z, "Z", what)
+    rows, cols = Z.shape
+    pv, ldv = _f32(V, "V", what)
+    rank = V.shape[1]
+    if V.shape[0] != rows:
+        raise ValueError(f"{what}: shape mismatch: Z {tuple(Z.shape)} V {tuple(V.shape)}")
+    if layout not in (SFC_B_NK, SFC_B_KN):
+        raise ValueError(f"{what}: layout must be SFC_B_NK or SFC_B_KN")
+    pg, ldg, stride, kind = _stack(G, "G", what, (-1, cols, rank) if layout == SFC_B_NK else (-1, rank, cols))
+    n = G.shape[0]
+    _check(lib.sfc_lora_wgrad(rows, cols, rank, _int(n, "the number of adapters", what), pz, ldz, pv, ldv,
+                              _ints(ids, "ids", what, rows), pg, ldg, stride, layout, kind, _stream(stream)), what)
