@@ -304,7 +304,8 @@ def _kernels(s):
         return [dxs, dw]
     T, R, n = c["T"], c["R"], c["adapters"]
     if f == "adapters":
-        v, y = new((T, R), "f32"), new((T, N), c["out"])
+        # (fp32 rows are added to where the shared projection left them, as the plain form does)
+        v, y = new((T, R), "f32"), s["base"] if c["out"] == "f32" else new((T, N), c["out"])
         so.sfc_lora_down(s["x"], s["a"], s["ids"], v, scales=s["scales"])
         so.sfc_lora_up(v, s["b"], s["ids"], y, base=s["base"])
         return [v, y]
