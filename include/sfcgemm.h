@@ -585,11 +585,17 @@ int sfc_moe_wgrad_ex(int64_t M, int64_t N, int64_t rows, int experts,
 
 /* sfc_lora_down -- V (rows x rank, fp32, ldv) as above from X (rows x K, bf16): A as rank x K (SFC_B_NK) or
  * K x rank (SFC_B_KN), stride_a elements from one adapter's to the next; scales NULL: 1; zeros in rows of no
- * adapter.  U is this call with X = dY and A = B, K x rank. */
+ * adapter.  U is this call with X = dY and A = B, K x rank.  ldx and lda below 2^22.
+ *   ws         NULL (library memory of the stream: replays of graphs recorded on one stream must then not
+ *              overlap each other) or 16-byte aligned device memory of sfc_lora_down_ws_size() bytes
+ *              (SFC_ERR_WORKSPACE if ws_bytes is less).
+ * sfc_lora_down_ws_size -- bytes that the call needs on the current device; 0 where it needs none, the sizes
+ * are bad or there is no device. */
+size_t sfc_lora_down_ws_size(int64_t rows, int64_t K, int64_t rank, int adapters);
 int sfc_lora_down(int64_t rows, int64_t K, int64_t rank, int adapters,
                   const void *X, int64_t ldx, const void *A, int64_t lda, int64_t stride_a, int layout,
                   const int32_t *ids, const float *scales,
-                  float *V, int64_t ldv, void *stream);
+                  float *V, int64_t ldv, void *ws, size_t ws_bytes, void *stream);
 
 /* sfc_lora_up -- Y (rows x N, `type`) as above: B as N x rank (SFC_B_NK) or rank x N (SFC_B_KN); base rows x N
  * of Y's type, NULL: 0, or Y itself; rows of no adapter are base's.  V's products with B are fp32, rounded once
@@ -604,10 +610,13 @@ int sfc_lora_up(int64_t rows, int64_t N, int64_t rank, int adapters,
  * its layout with Z = dY, that of sfc_lora_down's A in the other layout's name with V = U and Z = X (A of
  * rank x K: SFC_B_KN).  Zeros for an adapter without rows.  Z rows x columns, bf16; G out_type, stride_g
  * elements from one to the next, not overlapping.  Sums run over a fixed split of the rows: equal calls give
- * equal bits. */
+ * equal bits.
+ *   ws         as for sfc_lora_down, of sfc_lora_wgrad_ws_size() bytes. */
+size_t sfc_lora_wgrad_ws_size(int64_t rows, int64_t columns, int64_t rank, int adapters);
 int sfc_lora_wgrad(int64_t rows, int64_t columns, int64_t rank, int adapters,
                    const void *Z, int64_t ldz, const float *V, int64_t ldv, const int32_t *ids,
-                   void *G, int64_t ldg, int64_t stride_g, int layout, int out_type, void *stream);
+                   void *G, int64_t ldg, int64_t stride_g, int layout, int out_type,
+                   void *ws, size_t ws_bytes, void *stream);
 
 /* Static text of a return code. */
 const char *sfc_strerror(int code);

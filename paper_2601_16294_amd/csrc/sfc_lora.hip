@@ -10,9 +10,11 @@
 // leave, the last one rounded: two are off by at most 2^-16 of it (bf16 results, which are rounded to 2^-8),
 // three hold every bit of it (fp32 results).
 //
-// A wave takes 16 rows.  They may belong to up to 16 adapters: it computes with one
-// adapter after the other and keeps the results of that adapter's rows, so no row sees another
-// adapter's weights, infinities and NaN among them.
+// Two forms of down and up.  Where rows x rank x columns is small, as in decode steps, every row is taken by
+// itself and reads its adapter's weights (from the L2 where another row has): no order of the rows is
+// slow.  Else a wave takes tiles of 16 rows on MFMAs.  They may belong to up to 16 adapters: it computes with one adapter
+// after the other and keeps the results of that adapter's rows, so no row sees another adapter's
+// weights, infinities and NaN among them.
 #include "sfc_gemm_kernel.h"
 #include "sfc_launch.h"
 #include "sfc_lora_params.h"
@@ -24,44 +26,103 @@ namespace {
 
 __device__ __forceinline__ bf16x8 as_bf16x8(const row_u32x4& v) { return __builtin_bit_cast(bf16x8, v); }
 
-// 8 elements of a bf16 row from column c on; zeros past its end.
-__device__ __forceinline__ bf16x8 load_bf16x8(const uint16_t* row, int64_t c, int64_t cols) {
-  return as_bf16x8(load8<true>(row, c, cols).w[0]);
+// 8 elements at p, or (CHECKED) those of a row's from column c on that lie before `cols`, and zeros.
+__device__ __forceinline__ row_u32x4 load_any(const uint16_t* p) { return reinterpret_cast<const Any16<2>*>(p)->v; }
+template <bool CHECKED>
+__device__ __forceinline__ row_u32x4 load_part(const uint16_t* row, int64_t c, int64_t cols) {
+  if constexpr (!CHECKED) {
+    return load_any(row + c);
+  } else if (cols < 8) {
+    return c < cols ? load8<true>(row, c, cols).w[0] : row_u32x4{};
+  } else {
+    // the 8 elements that end with the row, moved down (no branch: a load waits for no other)
+    const int64_t at = c + 8 <= cols ? c : cols - 8;
+    const row_u32x4 v = load_any(row + at);
+    const int64_t off = c - at;
+    const uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+    const int s = off < 4 ? 16 * (int)off : off < 8 ? 16 * (int)off - 64 : 0;
+    const uint64_t low = off >= 8 ? 0 : off >= 4 ? hi >> s : s ? lo >> s | hi << (64 - s) : lo, high = off >= 4 ? 0 : hi >> s;
+    return row_u32x4{(uint32_t)low, (uint32_t)(low >> 32), (uint32_t)high, (uint32_t)(high >> 32)};
+  }
+}
+__device__ __forceinline__ row_u32x4 keep_if(bool on, const row_u32x4& v) {
+  return row_u32x4{on ? v[0] : 0u, on ? v[1] : 0u, on ? v[2] : 0u, on ? v[3] : 0u};
+}
+__device__ __forceinline__ void floats_of(const row_u32x4& v, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = (i & 1) ? bf16_high(v[i >> 1]) : bf16_low(v[i >> 1]);
 }
 
 // The adapter of row t, or -1.
 __device__ __forceinline__ int adapter_of(const LoraParams& p, int64_t t) {
-  const int a = t < p.rows ? p.ids[t] : -1;
-  return a >= 0 && a < p.adapters ? a : -1;
+  const int a = p.ids[t < p.rows ? t : p.rows - 1];
+  return t < p.rows && a >= 0 && a < p.adapters ? a : -1;
 }
 
-// Leading bf16 terms of 8 fp32 values.
+// Leading bf16 terms of 8 fp32 values.  (Upper halves of two words in one: a byte permutation.)
+__device__ __forceinline__ uint32_t upper_halves(float lo, float hi) {
+  return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
+}
+__device__ __forceinline__ float less_upper(float v) {
+  return v - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) & 0xFFFF0000u);
+}
 template <int TERMS>
 __device__ __forceinline__ void split_terms(const float (&v)[8], bf16x8 (&out)[TERMS]) {
-  uint32_t w[TERMS][4];
+  u32x4 w[TERMS];
+  float most = 0.f;                            // NaN once one value is, or is infinite
+#pragma unroll
+  for (int i = 0; i < 8; ++i) most = __builtin_fmaf(v[i], 0.f, most);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    uint32_t h[TERMS][2];
+    float lo = v[2 * i], hi = v[2 * i + 1];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float rest = v[2 * i + e];
-      const bool finite = __builtin_fabsf(rest) < __builtin_inff();
+    for (int k = 0; k + 1 < TERMS; ++k) {
+      w[k][i] = upper_halves(lo, hi);
+      lo = less_upper(lo);
+      hi = less_upper(hi);
+    }
+    w[TERMS - 1][i] = bf16_pair(lo, hi);
+  }
+  if (__ballot(most != most)) {
+    // an infinity or NaN is its first term alone (a NaN whose payload lies in the lower half has to stay one)
 #pragma unroll
-      for (int k = 0; k < TERMS; ++k) {
-        const uint32_t bits = __builtin_bit_cast(uint32_t, rest);
-        // (a NaN whose payload lies in the lower half alone has to stay one)
-        if (k == 0) h[k][e] = (bits >> 16) | (rest != rest ? 0x40u : 0u);
-        else if (k + 1 < TERMS) h[k][e] = bits >> 16;
-        else h[k][e] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)rest);
-        rest = finite ? rest - __builtin_bit_cast(float, bits & 0xFFFF0000u) : 0.f;
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float x = v[2 * i + e];
+        if (__builtin_fabsf(x) < __builtin_inff()) continue;
+        const uint32_t keep = e ? 0x0000FFFFu : 0xFFFF0000u;
+        w[0][i] |= x != x ? 0x40u << (16 * e) : 0u;
+#pragma unroll
+        for (int k = 1; k < TERMS; ++k) w[k][i] &= keep;
       }
     }
-#pragma unroll
-    for (int k = 0; k < TERMS; ++k) w[k][i] = h[k][0] | (h[k][1] << 16);
   }
 #pragma unroll
-  for (int k = 0; k < TERMS; ++k) out[k] = __builtin_bit_cast(bf16x8, u32x4{w[k][0], w[k][1], w[k][2], w[k][3]});
+  for (int k = 0; k < TERMS; ++k) out[k] = __builtin_bit_cast(bf16x8, w[k]);
 }
+
+// Ranks r .. r + 7 of a row of V; zeros past the rank (which is at least 1).
+__device__ __forceinline__ void load_ranks(const float* row, int r, int rank, float (&v)[8]) {
+  if (rank % 8 == 0) {
+    const float* q = row + (r < rank ? r : 0);
+    const f32x4 lo = __builtin_bit_cast(f32x4, reinterpret_cast<const Any16<4>*>(q)->v);
+    const f32x4 hi = __builtin_bit_cast(f32x4, reinterpret_cast<const Any16<4>*>(q + 4)->v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = r < rank ? lo[e] : 0.f;
+      v[4 + e] = r < rank ? hi[e] : 0.f;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = row[r + e < rank ? r + e : rank - 1];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = r + e < rank ? v[e] : 0.f;
+  }
+}
+// Loads before it are on their way before anything behind it (the compiler would put them next to their
+// uses, a few at a time, to save registers).
+__device__ __forceinline__ void loads_first() { __builtin_amdgcn_sched_barrier(0); }
 
 // Transposing read of 32 rows x 16 columns: lane l gets column column0(l % 16) of rows 8 (l / 16) .. + 7,
 // from LDS rows `pitch` bytes apart; `at` is this lane's address, row 8 (l / 16) + (l % 16) / 4 and the
@@ -73,346 +134,732 @@ __device__ __forceinline__ bf16x8 read_transposed(uint32_t at, int pitch) {
   return __builtin_bit_cast(bf16x8, v);
 }
 
-// ---- down ------------------------------------------------------------------------------------
+// ---- row by row ----------------------------------------------------------------------------------
 
-constexpr int kDownWaves = 8;
-
-// A workgroup takes 16 rows and 16 FR ranks; its waves deal K out in blocks of 64 and add up
-// through LDS, in the order of the waves.  Weights that lie along the ranks (KN) pass
-// through a wave's own LDS and the transposing read.
-template <int FR, bool NK>
-__global__ __launch_bounds__(kDownWaves * 64) void lora_down_kernel(LoraParams p) {
-  constexpr int PITCH = 16 * FR * 2 + 16;
-  __shared__ __attribute__((aligned(16))) float sums[kDownWaves][16][16 * FR + 4];
-  __shared__ __attribute__((aligned(16))) unsigned char slab[NK ? 16 : kDownWaves * 32 * PITCH];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int col = lane & 15, g = lane >> 4;
-  const int64_t t0 = (int64_t)blockIdx.x * 16;
-  const int r0 = blockIdx.y * 16 * FR;
-  const int64_t row = t0 + col < p.rows ? t0 + col : p.rows - 1;
-  const uint16_t* x = p.X + row * p.ldx;
-  const int id = adapter_of(p, t0 + col);
-  const uint32_t own = lds_addr(slab) + (uint32_t)(NK ? 0 : wave * 32 * PITCH);
-
-  // rows without an adapter
-  for (int i = tid; i < 16 * 16 * FR; i += kDownWaves * 64) {
-    const int tr = i / (16 * FR), r = r0 + i % (16 * FR);
-    if (t0 + tr < p.rows && r < p.rank && adapter_of(p, t0 + tr) < 0) p.V[(t0 + tr) * p.ldv + r] = 0.f;
-  }
-  uint32_t pending = (uint32_t)__ballot(id >= 0) & 0xFFFFu;
-  while (pending) {
-    const int a = __builtin_amdgcn_readlane(id, __builtin_ctz(pending));
-    pending &= ~(uint32_t)__ballot(id == a);
-    const uint16_t* w = p.W + (int64_t)a * p.stride_w;
-    f32x4 acc[FR] = {};
-    for (int64_t kb = (int64_t)wave * 64; kb < p.cols; kb += kDownWaves * 64) {
-      bf16x8 xf[2], wf[2][FR];
+// A wave takes RW ranks of a row; lanes deal K out, 8 elements at a time.
+template <int RW>
+__global__ __launch_bounds__(256) void lora_row_down_nk(LoraParams p) {
+  const int lane = threadIdx.x & 63;
+  const int groups = (p.rank + RW - 1) / RW;
+  const int64_t job = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t t = job / groups;
+  const int r0 = (int)(job - t * groups) * RW;
+  if (t >= p.rows) return;
+  const int a = __builtin_amdgcn_readfirstlane(adapter_of(p, t));
+  float sum[RW] = {};
+  if (a >= 0) {
+    const uint16_t* x = p.X + t * p.ldx;
+    const uint16_t* w[RW];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) xf[s] = load_bf16x8(x, kb + 32 * s + 8 * g, p.cols);
-      if constexpr (NK) {
+    for (int i = 0; i < RW; ++i) w[i] = p.W + a * p.stride_w + (int64_t)(r0 + i < p.rank ? r0 + i : p.rank - 1) * p.ldw;
+    auto add = [&](const row_u32x4& xv, const row_u32x4 (&wv)[RW]) {
+      float xf[8], wf[8];
+      floats_of(xv, xf);
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+      for (int i = 0; i < RW; ++i) {
+        floats_of(wv[i], wf);
 #pragma unroll
-          for (int f = 0; f < FR; ++f) {
-            const int r = r0 + 16 * f + col;
-            wf[s][f] = r < p.rank ? load_bf16x8(w + (int64_t)r * p.ldw, kb + 32 * s + 8 * g, p.cols) : bf16x8{};
-          }
-      } else {
+        for (int e = 0; e < 8; ++e) sum[i] = __builtin_fmaf(xf[e], wf[e], sum[i]);
+      }
+    };
+    constexpr int U = RW == 1 ? 8 : 4;         // loads of a row in flight
+    int64_t k = 0;
+    auto turns = [&](auto many) {
+      constexpr int n = many;
+      for (; k + n * 512 <= p.cols; k += n * 512) {
+        row_u32x4 xv[n], wv[n][RW];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          // 32 rows of 16 FR ranks, 8 of them a lane
+        for (int u = 0; u < n; ++u) {
+          xv[u] = load_any(x + k + u * 512 + 8 * lane);
 #pragma unroll
-          for (int i = lane; i < 32 * 2 * FR; i += 64) {
-            const int k = i / (2 * FR), c = i % (2 * FR);
-            const int64_t kk = kb + 32 * s + k;
-            const row_u32x4 v = kk < p.cols ? load8<true>(w + kk * p.ldw, r0 + 8 * c, p.rank).w[0] : row_u32x4{};
-            lds_write16(own + (uint32_t)(k * PITCH + 16 * c), v);
-          }
-          wait_lds_all();
-#pragma unroll
-          for (int f = 0; f < FR; ++f)
-            wf[s][f] = read_transposed(own + (uint32_t)((8 * g + (col >> 2)) * PITCH + 32 * f + 8 * (col & 3)), PITCH);
-          wait_lds_all();
+          for (int i = 0; i < RW; ++i) wv[u][i] = load_any(w[i] + k + u * 512 + 8 * lane);
         }
+        loads_first();
+#pragma unroll
+        for (int u = 0; u < n; ++u) add(xv[u], wv[u]);
       }
+    };
+    turns(std::integral_constant<int, U>{});
+    turns(std::integral_constant<int, 1>{});
+    if (k + 8 * lane < p.cols) {
+      row_u32x4 wv[RW];
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int f = 0; f < FR; ++f) acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[s][f], xf[s], acc[f], 0, 0, 0);
+      for (int i = 0; i < RW; ++i) wv[i] = load_part<true>(w[i], k + 8 * lane, p.cols);
+      add(load_part<true>(x, k + 8 * lane, p.cols), wv);
     }
-    // lane: row l % 16, ranks 4 (l / 16) .. + 3 of every fragment
 #pragma unroll
-    for (int f = 0; f < FR; ++f) *reinterpret_cast<f32x4*>(&sums[wave][col][16 * f + 4 * g]) = acc[f];
-    __syncthreads();
-    const float scale = p.scales ? p.scales[a] : 1.f;
-    for (int i = tid; i < 16 * 16 * FR; i += kDownWaves * 64) {
-      const int tr = i / (16 * FR), r = i % (16 * FR);
-      if (r0 + r < p.rank && adapter_of(p, t0 + tr) == a) {
-        float v = sums[0][tr][r];
+    for (int i = 0; i < RW; ++i)
 #pragma unroll
-        for (int k = 1; k < kDownWaves; ++k) v += sums[k][tr][r];
-        p.V[(t0 + tr) * p.ldv + r0 + r] = scale * v;
+      for (int d = 32; d >= 1; d >>= 1) sum[i] += __shfl_xor(sum[i], d);
+  }
+  const float scale = a >= 0 && p.scales ? p.scales[a] : 1.f;
+#pragma unroll
+  for (int i = 0; i < RW; ++i)
+    if (lane == 0 && r0 + i < p.rank) p.V[t * p.ldv + r0 + i] = scale * sum[i];
+}
+
+// Weights of K x rank: a workgroup takes a row.  A lane holds 8 ranks, LPR lanes a row of weights; the rows
+// go round the lanes and waves, whose sums meet by lane exchanges, then through LDS.
+constexpr int kRowWaves = 8;
+template <int LPR>
+__global__ __launch_bounds__(kRowWaves * 64) void lora_row_down_kn(LoraParams p) {
+  constexpr int STEP = kRowWaves * 64 / LPR, U = 8;
+  __shared__ float sums[kRowWaves][LPR * 8];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t t = blockIdx.x;
+  const int a = __builtin_amdgcn_readfirstlane(adapter_of(p, t));
+  const int r = 8 * (lane % LPR), first = tid / LPR;
+  float sum[8] = {};
+  if (a >= 0 && r < p.rank) {
+    const uint16_t* x = p.X + t * p.ldx;
+    const uint16_t* w = p.W + a * p.stride_w;
+    auto add = [&](uint16_t xv, const row_u32x4& wv) {
+      float wf[8];
+      floats_of(wv, wf);
+      const float xf = bf16_low(xv);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] = __builtin_fmaf(xf, wf[e], sum[e]);
+    };
+    auto run = [&](auto checked) {
+      int64_t k = first;
+      for (; k + (U - 1) * STEP < p.cols; k += U * STEP) {
+        uint16_t xv[U];
+        row_u32x4 wv[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          xv[u] = x[k + u * STEP];
+          wv[u] = load_part<checked>(w + (k + u * STEP) * p.ldw, r, p.rank);
+        }
+        loads_first();
+#pragma unroll
+        for (int u = 0; u < U; ++u) add(xv[u], wv[u]);
       }
-    }
-    __syncthreads();
+      for (; k < p.cols; k += STEP) add(x[k], load_part<checked>(w + k * p.ldw, r, p.rank));
+    };
+    if (p.rank % 8 == 0) run(std::false_type{});
+    else run(std::true_type{});
+  }
+#pragma unroll
+  for (int d = LPR; d < 64; d <<= 1)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += __shfl_xor(sum[e], d);
+  if (lane < LPR)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[wave][r + e] = sum[e];
+  __syncthreads();
+  const float scale = a >= 0 && p.scales ? p.scales[a] : 1.f;
+  if (tid < p.rank) {
+    float v = sums[0][tid];
+#pragma unroll
+    for (int k = 1; k < kRowWaves; ++k) v += sums[k][tid];
+    p.V[t * p.ldv + tid] = scale * v;
   }
 }
 
-// ---- up --------------------------------------------------------------------------------------
+template <bool OB>
+__device__ __forceinline__ float load_base(const LoraParams& p, int64_t t, int64_t n) {
+  if (!p.base) return 0.f;
+  if constexpr (OB) return bf16_low(reinterpret_cast<const uint16_t*>(p.base)[t * p.ld_base + n]);
+  else return reinterpret_cast<const float*>(p.base)[t * p.ld_base + n];
+}
 
-constexpr int kUpColumns = 64;         // columns of a unit: a lane's part of a row is 16 of them
-constexpr int kUpUnits = 4;            // units of a wave
+// A wave takes a row and 4 x 64 / LPC columns; LPC lanes share a column, 8 ranks at a time each.
+template <int LPC, bool OB>
+__global__ __launch_bounds__(256) void lora_row_up_nk(LoraParams p) {
+  constexpr int Q = 4, PER = 64 / LPC;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t t = blockIdx.y, n0 = ((int64_t)blockIdx.x * 4 + wave) * (Q * PER);
+  if (n0 >= p.cols) return;
+  const int a = __builtin_amdgcn_readfirstlane(adapter_of(p, t));
+  float sum[Q], base[Q];
+  int64_t n[Q];
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    sum[q] = 0.f;
+    n[q] = n0 + q * PER + lane / LPC;
+    base[q] = n[q] < p.cols ? load_base<OB>(p, t, n[q]) : 0.f;
+  }
+  if (a >= 0) {
+    const uint16_t* w = p.W + a * p.stride_w;
+    const float* v = p.V + t * p.ldv;
+    auto run = [&](auto checked) {
+      for (int r = 8 * (lane % LPC); r < p.rank; r += 8 * LPC) {
+        row_u32x4 wv[Q];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) wv[q] = load_part<checked>(w + (n[q] < p.cols ? n[q] : p.cols - 1) * p.ldw, r, p.rank);
+        float vf[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vf[e] = !checked || r + e < p.rank ? v[r + e] : 0.f;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+          float wf[8];
+          floats_of(wv[q], wf);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum[q] = __builtin_fmaf(vf[e], wf[e], sum[q]);
+        }
+      }
+    };
+    if (p.rank % 8 == 0) run(std::false_type{});
+    else run(std::true_type{});
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int d = 1; d < LPC; d <<= 1) sum[q] += __shfl_xor(sum[q], d);
+  }
+#pragma unroll
+  for (int q = 0; q < Q; ++q)
+    if (lane % LPC == 0 && n[q] < p.cols) {
+      const float y = base[q] + sum[q];
+      if constexpr (OB) reinterpret_cast<__bf16*>(p.Y)[t * p.ldy + n[q]] = (__bf16)y;
+      else reinterpret_cast<float*>(p.Y)[t * p.ldy + n[q]] = y;
+    }
+}
 
-// Column of a unit that lane n of fragment j computes.  bf16: a lane ends with 4 columns of each of 4
-// fragments, which make 16 in a row, 32 bytes; fp32: 4 columns of a fragment are 16 bytes.
+// Weights of rank x N: a lane takes 8 columns of a row.
+template <bool OB>
+__global__ __launch_bounds__(256) void lora_row_up_kn(LoraParams p) {
+  const int64_t t = blockIdx.y, n = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (n >= p.cols) return;
+  const int a = __builtin_amdgcn_readfirstlane(adapter_of(p, t));
+  float y[8] = {};
+  if (a >= 0) {
+    const uint16_t* w = p.W + a * p.stride_w;
+    const float* v = p.V + t * p.ldv;
+    auto add = [&](float vf, const row_u32x4& wv) {
+      float wf[8];
+      floats_of(wv, wf);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = __builtin_fmaf(vf, wf[e], y[e]);
+    };
+    auto run = [&](auto checked) {
+      int r = 0;
+      for (; r + 8 <= p.rank; r += 8) {
+        row_u32x4 wv[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) wv[u] = load_part<checked>(w + (int64_t)(r + u) * p.ldw, n, p.cols);
+        loads_first();
+#pragma unroll
+        for (int u = 0; u < 8; ++u) add(v[r + u], wv[u]);
+      }
+      for (; r < p.rank; ++r) add(v[r], load_part<checked>(w + (int64_t)r * p.ldw, n, p.cols));
+    };
+    if (n + 8 <= p.cols) run(std::false_type{});
+    else run(std::true_type{});
+  }
+  constexpr int ES = OB ? 2 : 4;
+  if (p.base) {
+    float b[8];
+    to_float<OB>(load8<OB>(static_cast<const char*>(p.base) + t * p.ld_base * ES, n, p.cols), b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] += b[e];
+  }
+  store8<OB, false>(static_cast<char*>(p.Y) + t * p.ldy * ES, n, p.cols, from_float<OB>(y));
+}
+
+// ---- up, in tiles --------------------------------------------------------------------------------
+
+// Ranks in NC chunks of 32; columns of a workgroup, so that its weights take 20 to 36 KB of LDS.
+template <int NC>
+constexpr int up_columns() { return NC <= 2 ? 256 : NC == 4 ? 128 : 64; }
+
+// Column of 64 that lane n of fragment j computes, so that a lane, which ends with 4 columns of every
+// fragment, has 16 bytes of a row at a time, and 4 lanes 64: bf16 8 columns of two fragments, fp32 4 of one.
 template <bool OB>
 __device__ __forceinline__ int up_column(int j, int n) {
-  return OB ? 16 * (n >> 2) + 4 * j + (n & 3) : 16 * j + n;
+  return OB ? 32 * (j >> 1) + 8 * (n >> 2) + 4 * (j & 1) + (n & 3) : 16 * j + n;
 }
 
-// A workgroup takes 64 rows, 16 a wave, and up to kUpUnits units of columns; ranks in chunks of 32, of
-// which a wave keeps its rows' terms in registers.
-template <int NC, bool NK, bool OB>
-__global__ __launch_bounds__(256) void lora_up_kernel(LoraParams p) {
-  constexpr int TERMS = OB ? 2 : 3;
-  constexpr int PITCH = kUpColumns * 2 + 16;
-  __shared__ __attribute__((aligned(16))) unsigned char slab[NK ? 16 : 4 * 32 * PITCH];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// A workgroup takes 64 Q rows, Q tiles for each of its 4 waves, and a block of columns, one adapter after the other: the block's weights of that
+// adapter go into LDS, and the waves take the tiles that hold rows of it, of which they load and store
+// these rows alone.  A last turn copies the rows of no adapter.  Column blocks run fastest over the
+// workgroups: those in flight cover whole rows.
+template <int Q, int NC, bool NK, bool OB>
+__global__ __launch_bounds__(256, (NC == 1 ? 3 : 2)) void lora_up_kernel(LoraParams p) {
+  constexpr int TERMS = OB ? 2 : 3, ES = OB ? 2 : 4, CB = up_columns<NC>(), UNITS = CB / 64;
+  constexpr int PITCH = NK ? NC * 64 + 16 : CB * 2 + 16;     // NK: [column][rank], else [rank][column]
+  constexpr int PIECES = OB ? 2 : 4;           // 16-byte pieces of 64 columns of a row that a lane has
+  __shared__ __attribute__((aligned(16))) unsigned char smem[NK ? CB * PITCH : 32 * NC * PITCH];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, g = lane >> 4;
-  const int64_t t0 = ((int64_t)blockIdx.x * 4 + wave) * 16;
-  if (t0 >= p.rows) return;
-  const bool live = t0 + col < p.rows;
-  const int64_t row = live ? t0 + col : p.rows - 1;
-  const int id = adapter_of(p, t0 + col);
-  const uint32_t own = lds_addr(slab) + (uint32_t)(NK ? 0 : wave * 32 * PITCH);
-  bf16x8 vf[NC][TERMS];
+  const int64_t t0 = (int64_t)blockIdx.y * (64 * Q), n0 = (int64_t)blockIdx.x * CB;
+  const uint32_t lds0 = lds_addr(smem);
+  const bool inside = n0 + CB <= p.cols;       // the block lies inside the columns
+  const bool whole = inside && p.rank % 8 == 0;
+  int id[Q];
+  uint64_t pending[Q], none[Q];
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int r = 32 * c + 8 * g + e;
-      v[e] = r < p.rank && id >= 0 ? p.V[row * p.ldv + r] : 0.f;
-    }
-    split_terms<TERMS>(v, vf[c]);
+  for (int q = 0; q < Q; ++q) {
+    id[q] = adapter_of(p, t0 + 64 * q + lane);
+    pending[q] = __ballot(id[q] >= 0);
+    none[q] = __ballot(id[q] < 0 && t0 + 64 * q + lane < p.rows);
   }
-  const uint32_t all = (uint32_t)__ballot(id >= 0) & 0xFFFFu;
-  for (int u = 0; u < kUpUnits; ++u) {
-    const int64_t n0 = ((int64_t)blockIdx.y * kUpUnits + u) * kUpColumns;
-    if (n0 >= p.cols) break;
-    float y[16];
-    // this lane's columns: OB 16 in a row, else 4 of every fragment
-    if (p.base) {
+
+  // rows `bits` of tile k: base (+ V times the weights in LDS), to Y
+  auto tile = [&](int k, uint32_t bits, auto product, auto in) {
+    const int64_t t = t0 + 16 * k + col;
+    const bool mine = bits >> col & 1;
+    const int64_t row = mine ? t : t0 + 16 * k + __builtin_ctz(bits);
+    const int piece = 16 / ES * g;             // of this lane's pieces, from the first column of each
+    constexpr int APART = 64 / PIECES;         // columns from piece to piece
+    const char* base = static_cast<const char*>(p.base) + (row * p.ld_base + n0 + piece) * ES;
+    char* out = static_cast<char*>(p.Y) + (row * p.ldy + n0 + piece) * ES;
+    const int left = in ? 0 : (int)(p.cols - n0 - piece);              // columns from the lane's first on
+    row_u32x4 bv[in ? UNITS : 1][PIECES];
+    // at: column from the block's first on
+    auto load_base_piece = [&](int at) -> row_u32x4 {
+      if (!p.base) return row_u32x4{};
+      if constexpr (in) {
+        return reinterpret_cast<const Any16<ES>*>(base + at * ES)->v;
+      } else if constexpr (OB) {
+        return load_part<true>(reinterpret_cast<const uint16_t*>(base) - piece, at + piece, p.cols - n0);
+      } else {
+        row_u32x4 v;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+        for (int e = 0; e < 4; ++e) v[e] = reinterpret_cast<const uint32_t*>(base)[at + e < left ? at + e : -piece];
+        return v;
+      }
+    };
+    if constexpr (in) {
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) bv[u][q] = load_base_piece(64 * u + APART * q);
+    }
+    bf16x8 vf[NC][TERMS];
+    if constexpr (product) {
+      constexpr int AHEAD = NC < 2 ? NC : 2;   // chunks whose loads are on their way at a time
+#pragma unroll
+      for (int c = 0; c < NC; c += AHEAD) {
+        float v[AHEAD][8];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) load_ranks(p.V + row * p.ldv, 32 * (c + i) + 8 * g, p.rank, v[i]);
+        loads_first();
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) split_terms<TERMS>(v[i], vf[c + i]);
+      }
+    }
+    auto unit = [&](int u, const row_u32x4 (&b)[PIECES]) {
+      f32x4 y[4];
+#pragma unroll
+      for (int q = 0; q < PIECES; ++q) {
         if constexpr (OB) {
-          to_float<true>(load8<true>(reinterpret_cast<const uint16_t*>(p.base) + row * p.ld_base, n0 + 16 * g + 8 * h, p.cols), y + 8 * h);
-        } else {
 #pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            const int64_t n = n0 + 16 * (2 * h + (q >> 2)) + 4 * g + (q & 3);
-            y[8 * h + q] = n < p.cols ? reinterpret_cast<const float*>(p.base)[row * p.ld_base + n] : 0.f;
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t w = b[q][e >> 1];
+            y[2 * q + (e >> 2)][e & 3] = (e & 1) ? bf16_high(w) : bf16_low(w);
           }
+        } else {
+          y[q] = __builtin_bit_cast(f32x4, b[q]);
         }
       }
-    } else {
+      if constexpr (product) {
+        f32x4 acc[4] = {};
 #pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] = 0.f;
-    }
-    uint32_t pending = all;
-    while (pending) {
-      const int a = __builtin_amdgcn_readlane(id, __builtin_ctz(pending));
-      pending &= ~(uint32_t)__ballot(id == a);
-      const uint16_t* w = p.W + (int64_t)a * p.stride_w;
-      f32x4 acc[4] = {};
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        if (32 * c >= p.rank) break;
-        bf16x8 wf[4];
-        if constexpr (NK) {
+        for (int c = 0; c < NC; ++c) {
+          if (NC > 2 && 32 * c >= p.rank) break;
+          bf16x8 wf[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const int64_t n = n0 + up_column<OB>(j, col);
-            wf[j] = n < p.cols ? load_bf16x8(w + n * p.ldw, 32 * c + 8 * g, p.rank) : bf16x8{};
+            if constexpr (NK)
+              wf[j] = *(lds_bf16x8*)(uintptr_t)(lds0 + (uint32_t)((64 * u + up_column<OB>(j, col)) * PITCH + 64 * c + 16 * g));
+            else
+              wf[j] = read_transposed(lds0 + (uint32_t)((32 * c + 8 * g + (col >> 2)) * PITCH + 2 * (64 * u + up_column<OB>(j, 4 * (col & 3)))), PITCH);
           }
-        } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = 8 * i + (lane >> 3), cc = 8 * (lane & 7);
-            const row_u32x4 v = 32 * c + r < p.rank && n0 + cc < p.cols
-                                    ? load8<true>(w + (int64_t)(32 * c + r) * p.ldw, n0 + cc, p.cols).w[0] : row_u32x4{};
-            lds_write16(own + (uint32_t)(r * PITCH + 2 * cc), v);
-          }
-          wait_lds_all();
+          for (int k2 = 0; k2 < TERMS; ++k2)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            wf[j] = read_transposed(own + (uint32_t)((8 * g + (col >> 2)) * PITCH + 2 * up_column<OB>(j, 4 * (col & 3))), PITCH);
-          wait_lds_all();
+            for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j], vf[c][k2], acc[j], 0, 0, 0);
         }
 #pragma unroll
-        for (int k = 0; k < TERMS; ++k)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j], vf[c][k], acc[j], 0, 0, 0);
+          for (int e = 0; e < 4; ++e) y[j][e] += acc[j][e];
       }
-      const bool mine = id == a;
+      if (mine) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+        for (int q = 0; q < PIECES; ++q) {
+          const int at = 64 * u + APART * q;
+          Raw8<true> o;
+          if constexpr (OB) {
+            const f32x4 lo = y[2 * q], hi = y[2 * q + 1];
+            o.w[0] = row_u32x4{bf16_pair(lo[0], lo[1]), bf16_pair(lo[2], lo[3]), bf16_pair(hi[0], hi[1]), bf16_pair(hi[2], hi[3])};
+          } else {
+            o.w[0] = __builtin_bit_cast(row_u32x4, y[q]);
+          }
+          if constexpr (in) store16<false>(out + at * ES, o.w[0]);
+          else if constexpr (OB) store8<true, false>(out, at, left, o);
+          else
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[4 * j + e] = mine ? y[4 * j + e] + acc[j][e] : y[4 * j + e];
+            for (int e = 0; e < 4; ++e)
+              if (at + e < left) reinterpret_cast<uint32_t*>(out)[at + e] = o.w[0][e];
+        }
+      }
+    };
+    if constexpr (in) {
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) {
+        loads_first();                         // (and one unit after the other, for registers)
+        unit(u, bv[u]);
+      }
+    } else {
+#pragma unroll 1
+      for (int u = 0; u < UNITS && n0 + 64 * u < p.cols; ++u) {
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) bv[0][q] = load_base_piece(64 * u + APART * q);
+        unit(u, bv[0]);
+      }
     }
-    if (live) {
-      if constexpr (OB) {
+  };
+  auto tiles = [&](const uint64_t (&rows)[Q], auto product) {
+    // (tiles 4 q .. 4 q + 3, one a wave: 16 bits of each)
+    uint64_t own = 0;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          store8<true, false>(reinterpret_cast<uint16_t*>(p.Y) + row * p.ldy, n0 + 16 * g + 8 * h, p.cols, from_float<true>(y + 8 * h));
+    for (int q = 0; q < Q; ++q) own |= (rows[q] >> (16 * wave) & 0xFFFFu) << (16 * q);
+#pragma unroll 1
+    for (int k = wave; own; k += 4, own >>= 16) {
+      const uint32_t bits = (uint32_t)own & 0xFFFFu;
+      if (!bits) continue;
+      if (inside) tile(k, bits, product, std::true_type{});
+      else tile(k, bits, product, std::false_type{});
+    }
+  };
+
+  for (;;) {
+    int a = -1;
+#pragma unroll
+    for (int q = Q - 1; q >= 0; --q)
+      if (pending[q]) a = __builtin_amdgcn_readlane(id[q], __builtin_ctzll(pending[q]));
+    if (a < 0 || p.rank == 0) break;
+    uint64_t match[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      match[q] = __ballot(id[q] == a);
+      pending[q] &= ~match[q];
+    }
+    const uint16_t* w = p.W + (int64_t)a * p.stride_w;
+    // 16-byte pieces of the block's weights, consecutive ones a lane after the other
+    constexpr int LINE = NK ? NC * 4 : CB / 8, COUNT = (NK ? CB : 32 * NC) * LINE / 256;
+    row_u32x4 piece[COUNT];
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+      const int line = (tid + 256 * i) / LINE, at = 8 * ((tid + 256 * i) % LINE);
+      if constexpr (NK) {
+        if (whole) piece[i] = load_any(w + (n0 + line) * p.ldw + (at < p.rank ? at : 0));
+        else piece[i] = load_part<true>(w + (n0 + line < p.cols ? n0 + line : p.cols - 1) * p.ldw, at, p.rank);
       } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int64_t n = n0 + 16 * (e >> 2) + 4 * g + (e & 3);
-          if (n < p.cols) reinterpret_cast<float*>(p.Y)[row * p.ldy + n] = y[e];
-        }
+        if (inside) piece[i] = load_any(w + (int64_t)(line < p.rank ? line : 0) * p.ldw + n0 + at);
+        else piece[i] = load_part<true>(w + (int64_t)(line < p.rank ? line : 0) * p.ldw, n0 + at, p.cols);
       }
     }
+    loads_first();
+    __syncthreads();                           // the last turn's readers are done
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+      const int line = (tid + 256 * i) / LINE, at = 8 * ((tid + 256 * i) % LINE);
+      lds_write16(lds0 + (uint32_t)(line * PITCH + 2 * at), keep_if((NK ? at : line) < p.rank, piece[i]));
+    }
+    __syncthreads();
+    tiles(match, std::true_type{});
   }
+  if (p.rank == 0) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) none[q] |= pending[q];
+  }
+  tiles(none, std::false_type{});
 }
 
 // ---- gradient of the weights -------------------------------------------------------------------
 
-constexpr int kGradWaves = 8, kGradColumns = 64;
+constexpr int kGradWaves = 4, kGradColumns = 64 * kGradWaves;
+constexpr int kGradList = 2048;        // chunks of 32 rows that are looked through at a time
 
-// A workgroup takes an adapter, 64 columns of Z and 16 FR ranks; its waves deal the rows out in chunks of
-// 32, leave out chunks without a row of the adapter, and add up through LDS in the order of the
-// waves.  In a chunk, rows of other adapters are zeros in both operands.
+// A workgroup takes an adapter, 256 columns of Z, 64 a wave, 16 FR ranks and a part of the adapter's rows.  It
+// lists the chunks of 32 rows that hold rows of the adapter and takes its part of the list: a chunk's V is
+// taken apart once for all waves, into one of two slots, while the next chunk's loads are in flight.  In a chunk,
+// rows of other adapters are zeros in both operands.
 template <int FR, bool NK, bool OB>
 __global__ __launch_bounds__(kGradWaves * 64) void lora_wgrad_kernel(LoraParams p) {
-  constexpr int TERMS = 3, FC = kGradColumns / 16;
-  constexpr int ZP = kGradColumns * 2 + 16, VP = 16 * FR * 2 + 16;       // bytes from row to row
-  constexpr int WAVE = 32 * ZP + TERMS * 32 * VP;
-  constexpr int SUMS = 16 * FC * (16 * FR + 4) * 4;                       // bytes of a wave's sums
-  __shared__ __attribute__((aligned(16))) unsigned char smem[kGradWaves * WAVE > SUMS ? kGradWaves * WAVE : SUMS];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int WAVES = kGradWaves, TERMS = 3;
+  constexpr int ZP = 64 * 2 + 16, VP = 16 * FR * 2 + 16;                 // bytes from row to row
+  constexpr int VSLOT = TERMS * 32 * VP;
+  constexpr int VL = (32 * 2 * FR + WAVES * 64 - 1) / (WAVES * 64);      // pieces of 8 ranks of a thread
+  __shared__ __attribute__((aligned(16))) unsigned char smem[WAVES * 32 * ZP + 2 * VSLOT];
+  __shared__ uint16_t list[kGradList];
+  __shared__ int counts[WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, g = lane >> 4;
-  const int64_t c0 = (int64_t)blockIdx.x * kGradColumns;
-  const int r0 = blockIdx.y * 16 * FR, a = p.first_adapter + (int)blockIdx.z;
-  const uint32_t z_own = lds_addr(smem) + (uint32_t)(wave * WAVE), v_own = z_own + 32 * ZP;
-  f32x4 acc[FC][FR] = {};
-  for (int64_t t0 = (int64_t)wave * 32; t0 < p.rows; t0 += kGradWaves * 32) {
-    const uint32_t mine = (uint32_t)__ballot(lane < 32 && adapter_of(p, t0 + lane) == a);
-    if (!mine) continue;
+  const int64_t c0 = (int64_t)blockIdx.x * kGradColumns + 64 * wave;
+  const int r0 = (int)(blockIdx.y / p.splits) * 16 * FR, split = (int)(blockIdx.y % p.splits);
+  const int a = p.first_adapter + (int)blockIdx.z;
+  const uint32_t z_own = lds_addr(smem) + (uint32_t)(wave * 32 * ZP), v_all = lds_addr(smem) + WAVES * 32 * ZP;
+  const bool whole = c0 + 64 <= p.cols, live = c0 < p.cols;
+  f32x4 acc[4][FR] = {};
+
+  struct Chunk {
+    uint32_t mine;             // rows of the adapter
+    row_u32x4 z[4];
+    float v[VL][8];
+  };
+  // lane: row 8 i + l / 8 and 8 columns of load i of Z; thread: row and 8 ranks of piece i of V
+  const int zc = 8 * (lane & 7);
+  auto load = [&](int64_t t0, Chunk& k) {
+    k.mine = (uint32_t)__ballot(lane < 32 && adapter_of(p, t0 + lane) == a);
+    if (live) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t t = t0 + 8 * i + (lane >> 3) < p.rows ? t0 + 8 * i + (lane >> 3) : p.rows - 1;
+        if (whole) k.z[i] = load_any(p.X + t * p.ldx + c0 + zc);
+        else k.z[i] = load_part<true>(p.X + t * p.ldx, c0 + zc, p.cols);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VL; ++i) {
+      const int at = tid + i * (WAVES * 64);
+      if (at < 32 * 2 * FR) {
+        const int64_t t = t0 + at / (2 * FR) < p.rows ? t0 + at / (2 * FR) : p.rows - 1;
+        load_ranks(p.V + t * p.ldv, r0 + 8 * (at % (2 * FR)), p.rank, k.v[i]);
+      }
+    }
+  };
+  auto use = [&](const Chunk& k, int slot) {
+    const uint32_t v_at = v_all + (uint32_t)(slot * VSLOT);
+    wait_lds_all();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int t = 8 * i + (lane >> 3), c = 8 * (lane & 7);
-      const row_u32x4 v = (mine >> t & 1) && c0 + c < p.cols ? load8<true>(p.X + (t0 + t) * p.ldx, c0 + c, p.cols).w[0] : row_u32x4{};
-      lds_write16(z_own + (uint32_t)(t * ZP + 2 * c), v);
+      const int t = 8 * i + (lane >> 3);
+      lds_write16(z_own + (uint32_t)(t * ZP + 2 * zc), keep_if(k.mine >> t & 1, k.z[i]));
     }
 #pragma unroll
-    for (int i = lane; i < 32 * 2 * FR; i += 64) {
-      const int t = i / (2 * FR), r = 8 * (i % (2 * FR));
-      float v[8];
+    for (int i = 0; i < VL; ++i) {
+      const int at = tid + i * (WAVES * 64);
+      if (at < 32 * 2 * FR) {
+        const int t = at / (2 * FR), r = 8 * (at % (2 * FR));
+        bf16x8 terms[TERMS];
+        split_terms<TERMS>(k.v[i], terms);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (mine >> t & 1) && r0 + r + e < p.rank ? p.V[(t0 + t) * p.ldv + r0 + r + e] : 0.f;
-      bf16x8 terms[TERMS];
-      split_terms<TERMS>(v, terms);
-#pragma unroll
-      for (int k = 0; k < TERMS; ++k)
-        lds_write16(v_own + (uint32_t)(k * 32 * VP + t * VP + 2 * r), __builtin_bit_cast(u32x4, terms[k]));
+        for (int q = 0; q < TERMS; ++q)
+          lds_write16(v_at + (uint32_t)(q * 32 * VP + t * VP + 2 * r), keep_if(k.mine >> t & 1, __builtin_bit_cast(row_u32x4, terms[q])));
+      }
     }
     wait_lds_all();
+    __builtin_amdgcn_s_barrier();              // (the slot's last readers passed the barrier before this one)
+    if (!live) return;
     const uint32_t lane_row = (uint32_t)(8 * g + (col >> 2));
-    bf16x8 zf[FC];
+    bf16x8 zf[4];
 #pragma unroll
-    for (int c = 0; c < FC; ++c) zf[c] = read_transposed(z_own + lane_row * ZP + (uint32_t)(32 * c + 8 * (col & 3)), ZP);
+    for (int c = 0; c < 4; ++c) zf[c] = read_transposed(z_own + lane_row * ZP + (uint32_t)(32 * c + 8 * (col & 3)), ZP);
 #pragma unroll
-    for (int k = 0; k < TERMS; ++k)
+    for (int q = 0; q < TERMS; ++q)
 #pragma unroll
       for (int f = 0; f < FR; ++f) {
-        const bf16x8 vf = read_transposed(v_own + (uint32_t)(k * 32 * VP) + lane_row * VP + (uint32_t)(32 * f + 8 * (col & 3)), VP);
+        const bf16x8 vf = read_transposed(v_at + (uint32_t)(q * 32 * VP) + lane_row * VP + (uint32_t)(32 * f + 8 * (col & 3)), VP);
 #pragma unroll
-        for (int c = 0; c < FC; ++c)
+        for (int c = 0; c < 4; ++c)
           acc[c][f] = NK ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, zf[c], acc[c][f], 0, 0, 0)
                          : __builtin_amdgcn_mfma_f32_16x16x32_bf16(zf[c], vf, acc[c][f], 0, 0, 0);
       }
-    wait_lds_all();
-  }
-  // Sums of the waves, one after the other.  NK: a lane holds column l % 16 and 4 ranks of a fragment,
-  // else rank l % 16 and 4 columns.
-  float* sums = reinterpret_cast<float*>(smem);
-  constexpr int SP = 16 * FR + 4;
-  for (int w = 0; w < kGradWaves; ++w) {
-    __syncthreads();
-    if (wave == w) {
+  };
+
+  const int64_t chunks = (p.rows + 31) >> 5;
+  for (int64_t from = 0; from < chunks; from += kGradList) {
+    // the list: a thread looks through a chunk's ids, 64 chunks a wave at a time
+    const int n = (int)(chunks - from < kGradList ? chunks - from : kGradList);
+    int total = 0;
+    for (int b = 0; b < n; b += WAVES * 64) {
+      const int c = b + tid;
+      bool any = false;
+      if (c < n) {
+        const int64_t t = (from + c) * 32;
+        if (t + 32 <= p.rows) {
+          row_u32x4 v[8];
 #pragma unroll
-      for (int c = 0; c < FC; ++c)
+          for (int i = 0; i < 8; ++i) v[i] = reinterpret_cast<const Any16<4>*>(p.ids + t + 4 * i)->v;
+          loads_first();
 #pragma unroll
-        for (int f = 0; f < FR; ++f)
+          for (int i = 0; i < 8; ++i) any |= v[i][0] == (uint32_t)a || v[i][1] == (uint32_t)a || v[i][2] == (uint32_t)a || v[i][3] == (uint32_t)a;
+        } else {
+          for (int i = 0; t + i < p.rows; ++i) any |= p.ids[t + i] == a;
+        }
+      }
+      const uint64_t m = __ballot(any);
+      if (lane == 0) counts[wave] = __popcll(m);
+      __syncthreads();
+      int at = total;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float& s = NK ? sums[(16 * c + col) * SP + 16 * f + 4 * g + e] : sums[(16 * c + 4 * g + e) * SP + 16 * f + col];
-            s = w == 0 ? acc[c][f][e] : s + acc[c][f][e];
-          }
+      for (int w = 0; w < WAVES; ++w) {
+        at += w < wave ? counts[w] : 0;
+        total += counts[w];
+      }
+      if (any) list[at + __popcll(m & ((1ull << lane) - 1))] = (uint16_t)c;
+      __syncthreads();
     }
+    total = __builtin_amdgcn_readfirstlane(total);
+    const int lo = (int)((int64_t)total * split / p.splits), hi = (int)((int64_t)total * (split + 1) / p.splits);
+    if (lo < hi) {
+      Chunk k;
+      load((from + __builtin_amdgcn_readfirstlane(list[lo])) * 32, k);
+      for (int i = lo; i < hi; ++i) {
+        Chunk next = k;
+        if (i + 1 < hi) load((from + __builtin_amdgcn_readfirstlane(list[i + 1])) * 32, next);
+        loads_first();
+        use(k, (i - lo) & 1);
+        k = next;
+      }
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  for (int i = tid; i < kGradColumns * 16 * FR; i += kGradWaves * 64) {
-    const int c = NK ? i / (16 * FR) : i % kGradColumns, r = NK ? i % (16 * FR) : i / kGradColumns;
-    if (c0 + c >= p.cols || r0 + r >= p.rank) continue;
-    const int64_t at = (int64_t)a * p.stride_y + (NK ? (c0 + c) * p.ldy + r0 + r : (int64_t)(r0 + r) * p.ldy + c0 + c);
-    if constexpr (OB) reinterpret_cast<__bf16*>(p.Y)[at] = (__bf16)sums[c * SP + r];
-    else reinterpret_cast<float*>(p.Y)[at] = sums[c * SP + r];
+  if (!live) return;
+  // NK: a lane holds column l % 16 and 4 ranks of a fragment, else rank l % 16 and 4 columns
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int f = 0; f < FR; ++f)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int64_t n = c0 + 16 * c + (NK ? col : 4 * g + e);
+        const int r = r0 + 16 * f + (NK ? 4 * g + e : col);
+        if (n >= p.cols || r >= p.rank) continue;
+        if (p.splits > 1) {
+          const int64_t plane = ((int64_t)split * p.adapters + a) * p.all_cols * p.rank;
+          p.sums[plane + (NK ? (p.first_col + n) * p.rank + r : r * p.all_cols + p.first_col + n)] = acc[c][f][e];
+        } else {
+          const int64_t at = (int64_t)a * p.stride_y + (NK ? n * p.ldy + r : r * p.ldy + n);
+          if constexpr (OB) reinterpret_cast<__bf16*>(p.Y)[at] = (__bf16)acc[c][f][e];
+          else reinterpret_cast<float*>(p.Y)[at] = acc[c][f][e];
+        }
+      }
+}
+
+// G from the sums of the parts of the rows, in their order.
+template <bool NK, bool OB>
+__global__ __launch_bounds__(256) void lora_grad_sum(LoraParams p) {
+  const int64_t each = p.all_cols * p.rank, n = each * p.adapters;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t a = i / each, at = i % each;
+    const int64_t c = NK ? at / p.rank : at % p.all_cols, r = NK ? at % p.rank : at / p.all_cols;
+    float v = p.sums[i];
+    for (int k = 1; k < p.splits; ++k) v += p.sums[k * n + i];
+    const int64_t to = a * p.stride_y + (NK ? c * p.ldy + r : r * p.ldy + c);
+    if constexpr (OB) reinterpret_cast<__bf16*>(p.Y)[to] = (__bf16)v;
+    else reinterpret_cast<float*>(p.Y)[to] = v;
+  }
+}
+
+int lanes_for(int rank, int most) {
+  int lanes = 1;
+  while (lanes < most && 8 * lanes < rank) lanes *= 2;
+  return lanes;
+}
+
+hipError_t launch_row_down(const LoraParams& p, bool nk, hipStream_t stream) {
+  if (nk) {
+    const bool one = p.rows * p.rank <= 2048;
+    const int64_t jobs = p.rows * (one ? p.rank : (p.rank + 3) / 4);
+    return launch_kernel(one ? lora_row_down_nk<1> : lora_row_down_nk<4>, dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, stream, p);
+  }
+  const dim3 grid((unsigned)p.rows), block(kRowWaves * 64);
+  switch (lanes_for(p.rank, 32)) {
+    case 1: return launch_kernel(lora_row_down_kn<1>, grid, block, 0, stream, p);
+    case 2: return launch_kernel(lora_row_down_kn<2>, grid, block, 0, stream, p);
+    case 4: return launch_kernel(lora_row_down_kn<4>, grid, block, 0, stream, p);
+    case 8: return launch_kernel(lora_row_down_kn<8>, grid, block, 0, stream, p);
+    case 16: return launch_kernel(lora_row_down_kn<16>, grid, block, 0, stream, p);
+    default: return launch_kernel(lora_row_down_kn<32>, grid, block, 0, stream, p);
+  }
+}
+
+template <bool OB>
+hipError_t launch_row_up(const LoraParams& p, bool nk, hipStream_t stream) {
+  const dim3 block(256);
+  if (!nk) return launch_kernel(lora_row_up_kn<OB>, dim3((unsigned)((p.cols + 2047) / 2048), (unsigned)p.rows), block, 0, stream, p);
+  const int lanes = lanes_for(p.rank, 8);
+  const dim3 grid((unsigned)((p.cols + 1024 / lanes - 1) / (1024 / lanes)), (unsigned)p.rows);
+  switch (lanes) {
+    case 1: return launch_kernel(lora_row_up_nk<1, OB>, grid, block, 0, stream, p);
+    case 2: return launch_kernel(lora_row_up_nk<2, OB>, grid, block, 0, stream, p);
+    case 4: return launch_kernel(lora_row_up_nk<4, OB>, grid, block, 0, stream, p);
+    default: return launch_kernel(lora_row_up_nk<8, OB>, grid, block, 0, stream, p);
   }
 }
 
 }  // namespace
 
-hipError_t launch_lora_down(const LoraParams& p, bool nk, int num_cus, hipStream_t stream) {
-  const int fr = p.rank <= 16 ? 1 : p.rank <= 32 ? 2 : 4;
-  const dim3 grid((unsigned)((p.rows + 15) / 16), (unsigned)((p.rank + 16 * fr - 1) / (16 * fr))), block(kDownWaves * 64);
-  if (fr == 1) return launch_kernel(nk ? lora_down_kernel<1, true> : lora_down_kernel<1, false>, grid, block, 0, stream, p);
-  if (fr == 2) return launch_kernel(nk ? lora_down_kernel<2, true> : lora_down_kernel<2, false>, grid, block, 0, stream, p);
-  return launch_kernel(nk ? lora_down_kernel<4, true> : lora_down_kernel<4, false>, grid, block, 0, stream, p);
+// Rows are taken one by one, each reading its adapter's weights (from the L2 for the most part).
+bool lora_by_rows(int64_t rows, int64_t cols, int rank) { return rows * rank * cols <= (int64_t)32 << 20 && rows <= 4096; }
+
+hipError_t launch_lora_down(const LoraParams& p, bool nk, hipStream_t stream) {
+  return lora_by_rows(p.rows, p.cols, p.rank) ? launch_row_down(p, nk, stream) : launch_lora_down_tiles(p, nk, stream);
+}
+
+template <int NC, bool NK, bool OB>
+static hipError_t up_launch(const LoraParams& p, int num_cus, hipStream_t stream) {
+  // 256 rows to a workgroup read the weights least often; 64 where there would be few workgroups
+  const int64_t across = (p.cols + up_columns<NC>() - 1) / up_columns<NC>();
+  if (across * ((p.rows + 255) / 256) >= 2 * num_cus)
+    return launch_kernel(lora_up_kernel<4, NC, NK, OB>, dim3((unsigned)across, (unsigned)((p.rows + 255) / 256)), dim3(256), 0, stream, p);
+  return launch_kernel(lora_up_kernel<1, NC, NK, OB>, dim3((unsigned)across, (unsigned)((p.rows + 63) / 64)), dim3(256), 0, stream, p);
 }
 
 template <bool NK, bool OB>
-static hipError_t up_launch(const LoraParams& p, hipStream_t stream) {
-  const dim3 grid((unsigned)((p.rows + 63) / 64), (unsigned)((p.cols + kUpUnits * kUpColumns - 1) / (kUpUnits * kUpColumns))), block(256);
-  if (p.rank <= 32) return launch_kernel(lora_up_kernel<1, NK, OB>, grid, block, 0, stream, p);
-  if (p.rank <= 64) return launch_kernel(lora_up_kernel<2, NK, OB>, grid, block, 0, stream, p);
-  if (p.rank <= 128) return launch_kernel(lora_up_kernel<4, NK, OB>, grid, block, 0, stream, p);
-  return launch_kernel(lora_up_kernel<8, NK, OB>, grid, block, 0, stream, p);
+static hipError_t up_rank(const LoraParams& p, int num_cus, hipStream_t stream) {
+  if (p.rank <= 32) return up_launch<1, NK, OB>(p, num_cus, stream);
+  if (p.rank <= 64) return up_launch<2, NK, OB>(p, num_cus, stream);
+  if (p.rank <= 128) return up_launch<4, NK, OB>(p, num_cus, stream);
+  return up_launch<8, NK, OB>(p, num_cus, stream);
 }
 
 hipError_t launch_lora_up(const LoraParams& p, bool nk, bool bf16, int num_cus, hipStream_t stream) {
-  return nk ? (bf16 ? up_launch<true, true>(p, stream) : up_launch<true, false>(p, stream))
-            : (bf16 ? up_launch<false, true>(p, stream) : up_launch<false, false>(p, stream));
+  if (lora_by_rows(p.rows, p.cols, p.rank)) return bf16 ? launch_row_up<true>(p, nk, stream) : launch_row_up<false>(p, nk, stream);
+  return nk ? (bf16 ? up_rank<true, true>(p, num_cus, stream) : up_rank<true, false>(p, num_cus, stream))
+            : (bf16 ? up_rank<false, true>(p, num_cus, stream) : up_rank<false, false>(p, num_cus, stream));
+}
+
+int lora_wgrad_splits(int64_t rows, int64_t cols, int rank, int adapters, int num_cus) {
+  // parts of the rows, so that one adapter's workgroups fill the chip; each at least a chunk for every wave
+  const int fr = rank <= 64 ? (rank + 15) / 16 : 4;
+  const int64_t groups = (cols + kGradColumns - 1) / kGradColumns * ((rank + 16 * fr - 1) / (16 * fr));
+  // (as if the rows were dealt out evenly: 4 chunks to a workgroup)
+  const int64_t chunks = (rows + 31) / 32;
+  int64_t splits = groups > 0 ? 2 * (int64_t)num_cus / (groups * adapters) : 1;
+  if (splits > chunks / (4 * (int64_t)adapters)) splits = chunks / (4 * (int64_t)adapters);
+  if (splits > 16) splits = 16;
+  return splits < 1 ? 1 : (int)splits;
 }
 
 template <bool NK, bool OB>
 static hipError_t wgrad_launch(const LoraParams& all, hipStream_t stream) {
-  const int fr = all.rank <= 16 ? 1 : all.rank <= 32 ? 2 : 4;
-  const int64_t across = (all.cols + kGradColumns - 1) / kGradColumns, ranks = (all.rank + 16 * fr - 1) / (16 * fr);
+  const int fr = all.rank <= 64 ? (all.rank + 15) / 16 : 4;
+  const int64_t across = (all.cols + kGradColumns - 1) / kGradColumns;
+  const int64_t ranks = (all.rank + 16 * fr - 1) / (16 * fr) * all.splits;
   // launches of less than 2^31 threads
+  const int64_t threads = kGradWaves * 64;
   LoraParams p = all;
-  const int64_t width = across < (1 << 20) ? across : 1 << 20;
-  int64_t deep = ((int64_t)1 << 31) / (width * ranks * kGradWaves * 64);
+  p.all_cols = all.cols;
+  const int64_t width = across < (1 << 14) ? across : 1 << 14;
+  int64_t deep = ((int64_t)1 << 31) / (width * ranks * threads);
   deep = deep < 1 ? 1 : deep > 32768 ? 32768 : deep;
   for (int64_t first = 0; first < all.adapters; first += deep)
     for (int64_t c = 0; c < across; c += width) {
       p.first_adapter = (int)first;
-      p.X = all.X + c * kGradColumns;
-      p.cols = all.cols - c * kGradColumns < width * kGradColumns ? all.cols - c * kGradColumns : width * kGradColumns;
-      p.Y = static_cast<char*>(all.Y) + c * kGradColumns * (NK ? all.ldy : 1) * (OB ? 2 : 4);
+      p.first_col = c * kGradColumns;
+      p.X = all.X + p.first_col;
+      p.cols = all.cols - p.first_col < width * kGradColumns ? all.cols - p.first_col : width * kGradColumns;
+      p.Y = static_cast<char*>(all.Y) + p.first_col * (NK ? all.ldy : 1) * (OB ? 2 : 4);
       const dim3 grid((unsigned)((p.cols + kGradColumns - 1) / kGradColumns), (unsigned)ranks,
                       (unsigned)(all.adapters - first < deep ? all.adapters - first : deep));
-      const dim3 block(kGradWaves * 64);
       const hipError_t e = launch_kernel(fr == 1   ? lora_wgrad_kernel<1, NK, OB>
                                          : fr == 2 ? lora_wgrad_kernel<2, NK, OB>
-                                                   : lora_wgrad_kernel<4, NK, OB>, grid, block, 0, stream, p);
+                                         : fr == 3 ? lora_wgrad_kernel<3, NK, OB>
+                                                   : lora_wgrad_kernel<4, NK, OB>, grid, dim3((unsigned)threads), 0, stream, p);
       if (e != hipSuccess) return e;
     }
-  return hipSuccess;
+  if (all.splits < 2) return hipSuccess;
+  p.Y = all.Y;
+  const int64_t n = all.cols * all.rank * all.adapters, blocks = (n + 255) / 256;
+  return launch_kernel(lora_grad_sum<NK, OB>, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, stream, p);
 }
 
-hipError_t launch_lora_wgrad(const LoraParams& p, bool nk, bool bf16, int num_cus, hipStream_t stream) {
+hipError_t launch_lora_wgrad(const LoraParams& p, bool nk, bool bf16, hipStream_t stream) {
   return nk ? (bf16 ? wgrad_launch<true, true>(p, stream) : wgrad_launch<true, false>(p, stream))
             : (bf16 ? wgrad_launch<false, true>(p, stream) : wgrad_launch<false, false>(p, stream));
 }

@@ -28,9 +28,18 @@ struct LoraParams {
   int64_t ld_base;
   void* Y;
   int64_t ldy, stride_y;     // stride_y: gradient, between adapters
+  // gradient: parts of the rows; their sums (splits > 1), [splits][adapters], each as G; this launch's first
+  // column.  down: ranges of K, their sums (splits > 1) [splits][rows][rank]
+  int splits;
+  float* sums;
+  int64_t all_cols, first_col;
 };
-hipError_t launch_lora_down(const LoraParams& p, bool nk, int num_cus, hipStream_t stream);
+int lora_wgrad_splits(int64_t rows, int64_t cols, int rank, int adapters, int num_cus);
+bool lora_by_rows(int64_t rows, int64_t cols, int rank);
+int lora_down_splits(int64_t rows, int64_t cols, int rank, int num_cus);
+hipError_t launch_lora_down(const LoraParams& p, bool nk, hipStream_t stream);
+hipError_t launch_lora_down_tiles(const LoraParams& p, bool nk, hipStream_t stream);
 hipError_t launch_lora_up(const LoraParams& p, bool nk, bool bf16, int num_cus, hipStream_t stream);
-hipError_t launch_lora_wgrad(const LoraParams& p, bool nk, bool bf16, int num_cus, hipStream_t stream);
+hipError_t launch_lora_wgrad(const LoraParams& p, bool nk, bool bf16, hipStream_t stream);
 
 }  // namespace sfc

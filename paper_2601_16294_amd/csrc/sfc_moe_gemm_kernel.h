@@ -15,7 +15,7 @@
 // wave has read the stage, and its two units take the loads that come next.
 //   * an operand along K is kept [row][64], 16-byte chunk c of row r at chunk c ^ ((r >> 1) & 7), and
 //     read 16 bytes a lane; one along M or N is kept [64][columns], chunk c of row k at chunk
-//     c ^ b_swz(k), and read by the transposing LDS load.  Both swizzles keep the banks apart;
+//     c ^ moe_swz(k), and read by the transposing LDS load.  Both swizzles keep the banks apart;
 //   * rows past the segment and K past its end are loaded as zeros (lanes past the
 //     descriptor's range).  A chunk that the end of a row cuts is left out of the loads of the last
 //     stage and written to LDS element by element, so nothing outside the matrices is used, nor read
@@ -32,6 +32,10 @@ namespace sfc {
 constexpr uint32_t kMoeRange = 0xFFFFFF00u;       // descriptors' range: byte offsets below it are loaded
 constexpr uint32_t kMoeOut = 0xFFFFFFF0u;         // a lane that loads zeros
 
+// Chunk c of row k of an operand along M or N lies at chunk c ^ moe_swz(k) (rows of 8 chunks at least).
+template <int BX>
+__device__ __forceinline__ int moe_swz(int k) { return b_swz(k) & (BX / 8 - 1); }
+
 template <int BM, int BN>
 struct MoeTile {
   static constexpr int WTM = BM / 2, WTN = BN / 2;           // a wave's part
@@ -39,7 +43,7 @@ struct MoeTile {
   static constexpr int UNIT = BM * 128;                      // bytes of an operand's stage
   static constexpr int L = BM / 32;                          // loads of 1 KiB per wave and unit
   static constexpr int LDS = 5 * UNIT;
-  static constexpr int PER_CU = BM == 256 ? 1 : 2;
+  static constexpr int PER_CU = BM == 256 ? 1 : BM == 128 ? 2 : 4;
   // epilogue: a wave's strip of 16 rows, fp32, rows 16 bytes apart from a multiple of 256
   static constexpr int RS = WTN * 4 + 16;
   static_assert(BM == BN, "square blocks");
@@ -101,7 +105,7 @@ struct MoeLoads {
     } else {
       const int e = (wave * L + j) * 512 + lane * 8;
       row = e / BX;
-      chunk = ((e % BX) >> 3) ^ b_swz(row);
+      chunk = ((e % BX) >> 3) ^ moe_swz<BX>(row);
     }
   }
 
@@ -158,7 +162,7 @@ struct MoeLoads {
         if (e < n) w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
     }
     const uint32_t at = ALONG_K ? (uint32_t)(tid * 128 + ((c ^ ((tid >> 1) & 7)) << 4))
-                                : (uint32_t)(tid * BX * 2 + ((c ^ b_swz(tid)) << 4));
+                                : (uint32_t)(tid * BX * 2 + ((c ^ moe_swz<BX>(tid)) << 4));
     lds_write16(unit + at, u32x4{w[0], w[1], w[2], w[3]});
   }
 };
@@ -169,7 +173,13 @@ struct MoeReads {
   static constexpr int PARTS = ALONG_K ? 1 : 2;              // LDS loads of a fragment
   uint32_t at;                                               // of fragment 0, step 0 (byte offset in the unit)
   __device__ __forceinline__ void init(int first, int lane) {
-    at = ALONG_K ? (uint32_t)(2 * a_frag_off(first, lane, 0)) : (uint32_t)(2 * b_frag_off<BX>(first, lane, 0, 0));
+    if constexpr (ALONG_K) {
+      at = (uint32_t)(2 * a_frag_off(first, lane, 0));
+    } else {
+      // lane (g = l / 16, j = l % 16) points at row 8 g + j / 4 and 4 columns; it gets column j of 4 rows
+      const int k = 8 * (lane >> 4) + ((lane & 15) >> 2), n = first + 4 * (lane & 3);
+      at = (uint32_t)(2 * (k * BX + (((n >> 3) ^ moe_swz<BX>(k)) << 3) + (n & 7)));
+    }
   }
   __device__ __forceinline__ void read(uint32_t unit, int step, int i, int part, bf16x8& f) const {
     if constexpr (ALONG_K) {
@@ -240,15 +250,15 @@ __device__ __forceinline__ void moe_store(const MoeGemmParams& p, const MoeTask&
   }
 }
 
-template <int BM, int BN, MoeLayout LAYOUT, bool GATHER, bool OB, bool PAST>
-__device__ __forceinline__ void moe_block(const MoeGemmParams& p, const MoeTask& t, uint32_t lds0, int wave, int lane) {
+// acc = the block's sums; every wave is done with the ring when it returns.
+template <int BM, int BN, MoeLayout LAYOUT, bool GATHER>
+__device__ __forceinline__ void moe_accumulate(const MoeTask& t, uint32_t lds0, int wave, int lane, f32x4 (&acc)[BM / 32][BN / 32]) {
   using T = MoeTile<BM, BN>;
   constexpr bool AK = LAYOUT != kMoeTN, BK = LAYOUT == kMoeNK;
   constexpr int L = T::L, FM = T::FM, FN = T::FN, NM = FM * FN;
   using LA = MoeLoads<BM, AK, GATHER>;
   using LB = MoeLoads<BN, BK, false>;
   const int wm = wave >> 1, wn = wave & 1;
-  f32x4 acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -390,6 +400,12 @@ __device__ __forceinline__ void moe_block(const MoeGemmParams& p, const MoeTask&
   // (loads of stages past the end write zeros to the ring)
   wait_vmem_at_most<0>();
   __syncthreads();                // every wave is done with the ring
+}
+
+template <int BM, int BN, MoeLayout LAYOUT, bool GATHER, bool OB, bool PAST>
+__device__ __forceinline__ void moe_block(const MoeGemmParams& p, const MoeTask& t, uint32_t lds0, int wave, int lane) {
+  f32x4 acc[BM / 32][BN / 32];
+  moe_accumulate<BM, BN, LAYOUT, GATHER>(t, lds0, wave, lane, acc);
   const int mv = t.a.valid, nv = t.b.valid;
   if (mv == BM && nv == BN) moe_store<BM, BN, OB, true, PAST>(p, t, mv, nv, acc, lds0, wave, lane);
   else moe_store<BM, BN, OB, false, PAST>(p, t, mv, nv, acc, lds0, wave, lane);

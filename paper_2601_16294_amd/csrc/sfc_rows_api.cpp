@@ -40,17 +40,34 @@ double moe_tile_us(bool large, double tasks, double stages, bool out_f32, int nu
 int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 
 // Launches a part at a time: rows first .. first + count - 1 and columns col .. col + width - 1, so
-// that a launch has less than 2^32 threads (at most 32 for a row, and 8 for a column of 64 rows).
+// that a launch has less than 2^32 threads (at most 512 for a row, and 4 for a row and column).
 template <class F>
 hipError_t lora_parts(int64_t rows, int64_t cols, F launch) {
   const int64_t width = least(cols, (int64_t)1 << 20);
-  const int64_t height = width > (1 << 12) ? (int64_t)1 << 17 : sfc::kLaunchRows;
+  const int64_t height = width > (1 << 12) ? (int64_t)1 << 17 : (int64_t)1 << 21;
   for (int64_t first = 0; first < rows; first += height)
     for (int64_t col = 0; col < cols; col += width) {
       const hipError_t e = launch(first, least(height, rows - first), col, least(width, cols - col));
       if (e != hipSuccess) return e;
     }
   return hipSuccess;
+}
+
+// Bytes of the sums that the adapters' down calls keep of ranges of K, the most that one of its launches needs.
+size_t down_sums(int64_t rows, int64_t K, int64_t rank, int cus) {
+  size_t most = 0;
+  (void)lora_parts(rows, 1, [&](int64_t, int64_t count, int64_t, int64_t) {
+    const int splits = sfc::lora_down_splits(count, K, (int)rank, cus);
+    const size_t need = splits > 1 ? (size_t)splits * (size_t)count * (size_t)rank * 4u : 0;
+    most = need > most ? need : most;
+    return hipSuccess;
+  });
+  return most;
+}
+
+// Bytes of the sums of an adapters' weight gradient over parts of the rows.
+size_t lora_sums(int splits, int64_t columns, int64_t rank, int adapters) {
+  return splits > 1 ? (size_t)splits * (size_t)adapters * (size_t)columns * (size_t)rank * 4u : 0;
 }
 
 }  // namespace
@@ -117,16 +134,32 @@ int sfc_moe_wgrad_ex(int64_t M, int64_t N, int64_t rows, int experts, const void
   return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "experts' weight gradient");
 }
 
+size_t sfc_lora_down_ws_size(int64_t rows, int64_t K, int64_t rank, int adapters) {
+  if (sfc::check_lora_sizes(rows, K, rank, adapters, sfc::kMaxRank, SFC_B_NK).code != SFC_OK || rows == 0 || rank == 0) return 0;
+  std::lock_guard<std::mutex> lock(sfc::host_mutex());
+  int cus = 0;
+  if (sfc::host_num_cus(&cus) != SFC_OK) return 0;
+  return down_sums(rows, K, rank, cus);
+}
+
 int sfc_lora_down(int64_t rows, int64_t K, int64_t rank, int adapters, const void* X, int64_t ldx, const void* A, int64_t lda,
-                  int64_t stride_a, int layout, const int32_t* ids, const float* scales, float* V, int64_t ldv, void* stream) {
-  const Checked c = sfc::check_lora_down(rows, K, rank, adapters, sfc::kMaxRank, X, ldx, A, lda, stride_a, layout, ids, scales,
-                                         V, ldv);
+                  int64_t stride_a, int layout, const int32_t* ids, const float* scales, float* V, int64_t ldv, void* ws,
+                  size_t ws_bytes, void* stream) {
+  Checked c = sfc::check_lora_down(rows, K, rank, adapters, sfc::kMaxRank, X, ldx, A, lda, stride_a, layout, ids, scales,
+                                   V, ldv);
+  if (c.code == SFC_OK) c = sfc::check_workspace(ws);
   if (c.code != SFC_OK) return reject(c);
   if (rows == 0 || rank == 0) return SFC_OK;
   std::lock_guard<std::mutex> lock(sfc::host_mutex());
   int cus = 0;
-  const int rc = sfc::host_num_cus(&cus);
+  int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
+  const size_t need = down_sums(rows, K, rank, cus);
+  if (ws && ws_bytes < need) return sfc::host_error(SFC_ERR_WORKSPACE, "workspace smaller than sfc_lora_down_ws_size()");
+  if (need && !ws) {
+    rc = sfc::host_workspace(as_stream(stream), need, &ws);
+    if (rc != SFC_OK) return rc;
+  }
   const hipError_t e = lora_parts(rows, 1, [&](int64_t first, int64_t count, int64_t, int64_t) {
     sfc::LoraParams p = {};
     p.rows = count;
@@ -142,7 +175,9 @@ int sfc_lora_down(int64_t rows, int64_t K, int64_t rank, int adapters, const voi
     p.scales = scales;
     p.V = V + first * ldv;
     p.ldv = ldv;
-    return sfc::launch_lora_down(p, layout == SFC_B_NK, cus, as_stream(stream));
+    p.splits = sfc::lora_down_splits(count, K, (int)rank, cus);
+    p.sums = static_cast<float*>(ws);
+    return sfc::launch_lora_down(p, layout == SFC_B_NK, as_stream(stream));
   });
   return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "adapters, down");
 }
@@ -180,18 +215,36 @@ int sfc_lora_up(int64_t rows, int64_t N, int64_t rank, int adapters, const float
   return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "adapters, up");
 }
 
+size_t sfc_lora_wgrad_ws_size(int64_t rows, int64_t columns, int64_t rank, int adapters) {
+  if (sfc::check_lora_sizes(rows, columns, rank, adapters, sfc::kMaxRank, SFC_B_NK).code != SFC_OK || columns == 0 || rank == 0)
+    return 0;
+  std::lock_guard<std::mutex> lock(sfc::host_mutex());
+  int cus = 0;
+  if (sfc::host_num_cus(&cus) != SFC_OK) return 0;
+  return lora_sums(sfc::lora_wgrad_splits(rows, columns, (int)rank, adapters, cus), columns, rank, adapters);
+}
+
 int sfc_lora_wgrad(int64_t rows, int64_t columns, int64_t rank, int adapters, const void* Z, int64_t ldz, const float* V,
                    int64_t ldv, const int32_t* ids, void* G, int64_t ldg, int64_t stride_g, int layout, int out_type,
-                   void* stream) {
-  const Checked c = sfc::check_lora_wgrad(rows, columns, rank, adapters, sfc::kMaxRank, Z, ldz, V, ldv, ids, G, ldg, stride_g,
-                                          layout, out_type);
+                   void* ws, size_t ws_bytes, void* stream) {
+  Checked c = sfc::check_lora_wgrad(rows, columns, rank, adapters, sfc::kMaxRank, Z, ldz, V, ldv, ids, G, ldg, stride_g,
+                                    layout, out_type);
+  if (c.code == SFC_OK) c = sfc::check_workspace(ws);
   if (c.code != SFC_OK) return reject(c);
   if (columns == 0 || rank == 0) return SFC_OK;
   std::lock_guard<std::mutex> lock(sfc::host_mutex());
   int cus = 0;
-  const int rc = sfc::host_num_cus(&cus);
+  int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
   sfc::LoraParams p = {};
+  p.splits = sfc::lora_wgrad_splits(rows, columns, (int)rank, adapters, cus);
+  const size_t need = lora_sums(p.splits, columns, rank, adapters);
+  if (ws && ws_bytes < need) return sfc::host_error(SFC_ERR_WORKSPACE, "workspace smaller than sfc_lora_wgrad_ws_size()");
+  if (need && !ws) {
+    rc = sfc::host_workspace(as_stream(stream), need, &ws);
+    if (rc != SFC_OK) return rc;
+  }
+  p.sums = static_cast<float*>(ws);
   p.rows = rows;
   p.cols = columns;
   p.rank = (int)rank;
@@ -204,7 +257,7 @@ int sfc_lora_wgrad(int64_t rows, int64_t columns, int64_t rank, int adapters, co
   p.Y = G;
   p.ldy = ldg;
   p.stride_y = stride_g;
-  const hipError_t e = sfc::launch_lora_wgrad(p, layout == SFC_B_NK, out_type == SFC_OUT_BF16, cus, as_stream(stream));
+  const hipError_t e = sfc::launch_lora_wgrad(p, layout == SFC_B_NK, out_type == SFC_OUT_BF16, as_stream(stream));
   return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "adapters, weight gradient");
 }
 

@@ -96,7 +96,9 @@ inline Checked check_lora_down(int64_t rows, int64_t K, int64_t rank, int adapte
   SFC_RETURN_IF(check_lora_sizes(rows, K, rank, adapters, most_rank, layout));
   if (rows == 0 || rank == 0) return ok();
   SFC_RETURN_IF(check_rows(V, rows, rank, ldv, SFC_OUT_F32, "V is NULL", "ldv < rank"));
-  SFC_RETURN_IF(check_rows(X, rows, K, ldx, SFC_OUT_BF16, "X is NULL", "ldx < K"));
+  SFC_RETURN_IF(check_bf16(X, rows, K, ldx, "X is NULL", "ldx < K"));
+  if (K > 0 && lda >= kRowsMaxLd)
+    return fail(SFC_ERR_UNSUPPORTED, "leading dimensions of bf16 operands must be below 2^22");
   SFC_RETURN_IF(check_lora_weights(A, rank, K, lda, stride_a, adapters, layout));
   SFC_RETURN_IF(check_weights(scales));
   return check_index(ids, "ids is NULL");

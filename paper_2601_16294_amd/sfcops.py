@@ -29,7 +29,7 @@ except ImportError as e:
 __all__ = ["SfcError", "mx4_empty", "sfc_mx4_quant", "sfc_mx4_dequant", "sfc_gemm_mx4_ex", "sfc_mx4_linear",
            "sfc_gemm_mx4_ws_size", "sfc_mx4_linear_ws_size", "sfc_moe_sort", "sfc_moe_sort_rows", "sfc_moe_dispatch", "sfc_moe_combine", "sfc_moe_combine_grad",
            "sfc_moe_gemm_mx4_ex", "sfc_moe_wgrad_mx4_ex", "SFC_B_NK", "SFC_B_KN", "sfc_moe_gemm_ex", "sfc_moe_wgrad_ex",
-           "sfc_lora_down", "sfc_lora_up", "sfc_lora_wgrad"]
+           "sfc_lora_down", "sfc_lora_up", "sfc_lora_wgrad", "sfc_lora_down_ws_size", "sfc_lora_wgrad_ws_size"]
 
 # layouts of weights (sfcgemm.h): N x K as a linear layer holds them, or K x N
 SFC_B_NK, SFC_B_KN = 0, 1
@@ -56,15 +56,17 @@ def _declare() -> None:
     lib.sfc_moe_gemm_ex.argtypes = [i64, i64, i64, i32] + rows + [p, i64, i32, p, i64, i64, i32, p] + rows + [i32, p]
     lib.sfc_moe_wgrad_ex.argtypes = [i64, i64, i64, i32] + rows + rows + [p] + rows + [i64, i32, p]
     stack = [p, i64, i64, i32]                   # weights, leading dimension, stride, layout
-    lib.sfc_lora_down.argtypes = [i64, i64, i64, i32] + rows + stack + [p, p] + rows + [p]
+    lib.sfc_lora_down.argtypes = [i64, i64, i64, i32] + rows + stack + [p, p] + rows + [p, sz, p]
     lib.sfc_lora_up.argtypes = [i64, i64, i64, i32] + rows + stack + [p] + rows + rows + [i32, p]
-    lib.sfc_lora_wgrad.argtypes = [i64, i64, i64, i32] + rows + rows + [p, p, i64, i64, i32, i32, p]
+    lib.sfc_lora_wgrad.argtypes = [i64, i64, i64, i32] + rows + rows + [p, p, i64, i64, i32, i32, p, sz, p]
+    lib.sfc_lora_down_ws_size.argtypes = lib.sfc_lora_wgrad_ws_size.argtypes = [i64, i64, i64, i32]
     for name in __all__:
         if name.startswith("sfc_") and name != "sfc_moe_sort_rows" and not name.endswith("_size"):
             getattr(lib, name).restype = i32
     for name in ("sfc_gemm_mx4_ws_ex", "sfc_mx4_linear_ws"):
         getattr(lib, name).restype = i32
-    for name in ("sfc_gemm_mx4_ws_size", "sfc_mx4_linear_ws_size", "sfc_moe_sort_ws_size"):
+    for name in ("sfc_gemm_mx4_ws_size", "sfc_mx4_linear_ws_size", "sfc_moe_sort_ws_size", "sfc_lora_down_ws_size",
+                 "sfc_lora_wgrad_ws_size"):
         getattr(lib, name).restype = sz
 
 
@@ -486,19 +488,26 @@ def _f32(t, name, what, shape=None):
     return p, ld
 
 
-def sfc_lora_down(X, A, ids, V, scales=None, layout: int = SFC_B_NK, stream=None) -> None:
+def sfc_lora_down_ws_size(rows: int, K: int, rank: int, adapters: int) -> int:
+    """Bytes of the workspace that sfc_lora_down takes (0: none)."""
+    return int(lib.sfc_lora_down_ws_size(rows, K, rank, adapters))
+
+
+def sfc_lora_down(X, A, ids, V, scales=None, layout: int = SFC_B_NK, stream=None, workspace=None) -> None:
     """V (rows, rank), float32, = scales[ids] * X (rows, K) times the transposed A of the row's adapter; zeros where
     ids (int32, one to a row) names none.  A is (adapters, rank, K) with SFC_B_NK or (adapters, K, rank) with
-    SFC_B_KN; X and A bfloat16, scales float32 or None (1)."""
+    SFC_B_KN; X and A bfloat16, scales float32 or None (1).  workspace: None (library memory of the stream) or a
+    tensor of sfc_lora_down_ws_size() bytes; graphs that are replayed at once need workspaces of their own."""
     what = "sfc_lora_down"
     px, ldx = _bf16(X, "X", what)
     rows, K = X.shape
     pa, lda, stride = _weights_of(A, "A", what, layout, K)
     n, rank = A.shape[0], A.shape[1 if layout == SFC_B_NK else 2]
     pv, ldv = _f32(V, "V", what, (rows, rank))
+    ws, ws_bytes = (None, 0) if workspace is None else _memory(workspace, what)
     _check(lib.sfc_lora_down(rows, K, rank, _int(n, "the number of adapters", what), px, ldx, pa, lda, stride, layout,
                              _ints(ids, "ids", what, rows), None if scales is None else _vector(scales, "scales", what, _F32, n),
-                             pv, ldv, _stream(stream)), what)
+                             pv, ldv, ws, ws_bytes, _stream(stream)), what)
 
 
 def sfc_lora_up(V, B, ids, Y, base=None, layout: int = SFC_B_NK, stream=None) -> None:
@@ -520,10 +529,16 @@ def sfc_lora_up(V, B, ids, Y, base=None, layout: int = SFC_B_NK, stream=None) ->
                            _ints(ids, "ids", what, rows), p0, ld0, py, ldy, kind, _stream(stream)), what)
 
 
-def sfc_lora_wgrad(Z, V, ids, G, layout: int = SFC_B_NK, stream=None) -> None:
+def sfc_lora_wgrad_ws_size(rows: int, columns: int, rank: int, adapters: int) -> int:
+    """Bytes of the workspace that sfc_lora_wgrad takes (0: none)."""
+    return int(lib.sfc_lora_wgrad_ws_size(rows, columns, rank, adapters))
+
+
+def sfc_lora_wgrad(Z, V, ids, G, layout: int = SFC_B_NK, stream=None, workspace=None) -> None:
     """G[a] = the sum over the rows t of adapter a of Z[t]^T V[t], G (adapters, columns, rank) with SFC_B_NK, or of
     V[t]^T Z[t], G (adapters, rank, columns) with SFC_B_KN; Z (rows, columns) bfloat16, V (rows, rank) float32, G
-    float32 or bfloat16."""
+    float32 or bfloat16.  workspace: None (library memory of the stream) or a tensor of sfc_lora_wgrad_ws_size()
+    bytes; graphs that are replayed at once need workspaces of their own."""
     what = "sfc_lora_wgrad"
     pz, ldz = _bf16(Z, "Z", what)
     rows, cols = Z.shape
@@ -535,5 +550,6 @@ def sfc_lora_wgrad(Z, V, ids, G, layout: int = SFC_B_NK, stream=None) -> None:
         raise ValueError(f"{what}: layout must be SFC_B_NK or SFC_B_KN")
     pg, ldg, stride, kind = _stack(G, "G", what, (-1, cols, rank) if layout == SFC_B_NK else (-1, rank, cols))
     n = G.shape[0]
+    ws, ws_bytes = (None, 0) if workspace is None else _memory(workspace, what)
     _check(lib.sfc_lora_wgrad(rows, cols, rank, _int(n, "the number of adapters", what), pz, ldz, pv, ldv,
-                              _ints(ids, "ids", what, rows), pg, ldg, stride, layout, kind, _stream(stream)), what)
+                              _ints(ids, "ids", what, rows), pg, ldg, stride, layout, kind, ws, ws_bytes, _stream(stream)), what)

@@ -59,6 +59,9 @@ def same(got, want):
 # (rows, columns, rank, adapters)
 SHAPES = [(1, 1, 1, 1), (1, 4096, 16, 3), (5, 33, 7, 2), (16, 64, 16, 16), (32, 1000, 16, 8), (17, 130, 33, 4), (100, 70, 64, 1),
           (64, 65, 12, 5), (333, 257, 100, 3), (70, 515, 128, 2), (40, 96, 256, 3), (1000, 300, 8, 6), (2049, 640, 24, 9)]
+# (too large to be taken row by row)
+SHAPES += [(2100, 1030, 16, 5), (1100, 1100, 31, 9), (1000, 900, 40, 2), (530, 1000, 64, 3), (700, 515, 100, 2), (530, 600, 128, 3),
+           (300, 520, 256, 4), (4200, 1030, 8, 6), (9000, 64, 64, 3)]
 
 
 @pytest.mark.parametrize("rows,cols,rank,adapters", SHAPES)
@@ -71,8 +74,13 @@ def test_down(so, rows, cols, rank, adapters, kind, nk, pad, shift):
     a = small_ints((adapters, rank, cols) if nk else (adapters, cols, rank), 2, pad, shift, gap=3)
     scales = torch.exp2(torch.arange(adapters, device="cuda").float() % 5 - 2) if pad else None
     v = framed((rows, rank), F32, pad, shift)
-    so.sfc_lora_down(x, a, ids, v, scales=scales, layout=so.SFC_B_NK if nk else so.SFC_B_KN)
+    lay = so.SFC_B_NK if nk else so.SFC_B_KN
+    so.sfc_lora_down(x, a, ids, v, scales=scales, layout=lay)
     assert same(v, down(x, a, ids, scales, nk))
+    need = so.sfc_lora_down_ws_size(rows, cols, rank, adapters)
+    ws, again = framed((1, max(need // 4, 4)), F32), torch.empty_like(v)
+    so.sfc_lora_down(x, a, ids, again, scales=scales, layout=lay, workspace=ws)
+    assert torch.equal(again, v) and (need == 0) == bool(torch.isnan(ws).all())
     assert untouched_outside(v)
 
 
@@ -113,7 +121,13 @@ def test_weight_gradient(so, rows, cols, rank, adapters, kind, nk, dtype, pad, s
     v = framed((rows, rank), F32, pad, shift)
     v.copy_(torch.randint(-500, 501, (rows, rank), generator=g).float())
     out = framed((adapters, cols, rank) if nk else (adapters, rank, cols), dtype, pad, shift, gap=2)
-    so.sfc_lora_wgrad(z, v, ids, out, layout=so.SFC_B_NK if nk else so.SFC_B_KN)
+    lay = so.SFC_B_NK if nk else so.SFC_B_KN
+    so.sfc_lora_wgrad(z, v, ids, out, layout=lay)
+    need = so.sfc_lora_wgrad_ws_size(rows, cols, rank, adapters)
+    ws = framed((1, max(need // 4, 4)), F32)
+    again = torch.empty_like(out)
+    so.sfc_lora_wgrad(z, v, ids, again, layout=lay, workspace=ws)
+    assert torch.equal(again, out) and (need == 0) == bool(torch.isnan(ws).all())
     for a in range(adapters):
         t = torch.nonzero(ids == a)[:, 0]
         w = z[t].double().t() @ v[t].double()
