@@ -28,6 +28,13 @@ __device__ __forceinline__ bf16x8 as_bf16x8(const row_u32x4& v) { return __built
 
 // 8 elements at p, or (CHECKED) those of a row's from column c on that lie before `cols`, and zeros.
 __device__ __forceinline__ row_u32x4 load_any(const uint16_t* p) { return reinterpret_cast<const Any16<2>*>(p)->v; }
+// Element i + n of v as element i, zeros behind.
+__device__ __forceinline__ row_u32x4 moved_down(const row_u32x4& v, int64_t n) {
+  const uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+  const int s = n < 4 ? 16 * (int)n : n < 8 ? 16 * (int)n - 64 : 0;
+  const uint64_t low = n >= 8 ? 0 : n >= 4 ? hi >> s : s ? lo >> s | hi << (64 - s) : lo, high = n >= 4 ? 0 : hi >> s;
+  return row_u32x4{(uint32_t)low, (uint32_t)(low >> 32), (uint32_t)high, (uint32_t)(high >> 32)};
+}
 template <bool CHECKED>
 __device__ __forceinline__ row_u32x4 load_part(const uint16_t* row, int64_t c, int64_t cols) {
   if constexpr (!CHECKED) {
@@ -37,12 +44,7 @@ __device__ __forceinline__ row_u32x4 load_part(const uint16_t* row, int64_t c, i
   } else {
     // the 8 elements that end with the row, moved down (no branch: a load waits for no other)
     const int64_t at = c + 8 <= cols ? c : cols - 8;
-    const row_u32x4 v = load_any(row + at);
-    const int64_t off = c - at;
-    const uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
-    const int s = off < 4 ? 16 * (int)off : off < 8 ? 16 * (int)off - 64 : 0;
-    const uint64_t low = off >= 8 ? 0 : off >= 4 ? hi >> s : s ? lo >> s | hi << (64 - s) : lo, high = off >= 4 ? 0 : hi >> s;
-    return row_u32x4{(uint32_t)low, (uint32_t)(low >> 32), (uint32_t)high, (uint32_t)(high >> 32)};
+    return moved_down(load_any(row + at), c - at);
   }
 }
 __device__ __forceinline__ row_u32x4 keep_if(bool on, const row_u32x4& v) {
@@ -572,87 +574,222 @@ __global__ __launch_bounds__(256, (NC == 1 ? 3 : 2)) void lora_up_kernel(LoraPar
 
 constexpr int kGradWaves = 4, kGradColumns = 64 * kGradWaves;
 constexpr int kGradList = 2048;        // chunks of 32 rows that are looked through at a time
+constexpr int kGradAdapters = 1024;    // most adapters whose rows are dealt out in parts
 
-// A workgroup takes an adapter, 256 columns of Z, 64 a wave, 16 FR ranks and a part of the adapter's rows.  It
-// lists the chunks of 32 rows that hold rows of the adapter and takes its part of the list: a chunk's V is
-// taken apart once for all waves, into one of two slots, while the next chunk's loads are in flight.  In a chunk,
-// rows of other adapters are zeros in both operands.
-template <int FR, bool NK, bool OB>
+// Parts of an adapter with `count` of `total` rows: `extra` of them are dealt out over all adapters by their
+// rows; less than two are one, which needs no sum.
+__device__ __forceinline__ int grad_parts(int64_t count, int64_t total, int extra) {
+  const int n = total > 0 ? (int)(count * extra / total) : 0;
+  return n > 1 ? n : 1;
+}
+
+__device__ __forceinline__ void store4(float* to, const f32x4& v, int64_t inside) {
+  if (inside >= 4) {
+    reinterpret_cast<Any16<4>*>(to)->v = __builtin_bit_cast(row_u32x4, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < inside) to[e] = v[e];
+  }
+}
+
+// A workgroup takes 256 columns of Z, 64 a wave, 16 FR ranks, an adapter and a part of its rows.  Parts go by
+// the adapters' numbers of rows, which every workgroup counts for itself, so that an adapter with most of the
+// rows keeps the chip busy too; the workgroup then lists the chunks of 32 rows that hold rows of its
+// adapter and takes its part of the list.  A chunk's V is taken apart once for all waves; chunks lie in one of two
+// slots of LDS, the next one written while one is computed with, three more on their way.  In a
+// chunk, rows of other adapters are zeros in both operands.
+// NARROW: rows of Z or V of fewer than 8 elements, which are loaded one by one.
+template <int FR, bool NARROW, bool NK, bool OB>
 __global__ __launch_bounds__(kGradWaves * 64) void lora_wgrad_kernel(LoraParams p) {
   constexpr int WAVES = kGradWaves, TERMS = 3;
   constexpr int ZP = 64 * 2 + 16, VP = 16 * FR * 2 + 16;                 // bytes from row to row
   constexpr int VSLOT = TERMS * 32 * VP;
   constexpr int VL = (32 * 2 * FR + WAVES * 64 - 1) / (WAVES * 64);      // pieces of 8 ranks of a thread
-  __shared__ __attribute__((aligned(16))) unsigned char smem[WAVES * 32 * ZP + 2 * VSLOT];
+  constexpr int SLOT = WAVES * 32 * ZP + VSLOT;                          // a chunk's Z and V
+  __shared__ __attribute__((aligned(16))) unsigned char smem[2 * SLOT];
   __shared__ uint16_t list[kGradList];
-  __shared__ int counts[WAVES];
+  __shared__ int found[WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, g = lane >> 4;
   const int64_t c0 = (int64_t)blockIdx.x * kGradColumns + 64 * wave;
-  const int r0 = (int)(blockIdx.y / p.splits) * 16 * FR, split = (int)(blockIdx.y % p.splits);
-  const int a = p.first_adapter + (int)blockIdx.z;
+  const int r0 = (int)blockIdx.y * 16 * FR;
   const uint32_t z_own = lds_addr(smem) + (uint32_t)(wave * 32 * ZP), v_all = lds_addr(smem) + WAVES * 32 * ZP;
   const bool whole = c0 + 64 <= p.cols, live = c0 < p.cols;
   f32x4 acc[4][FR] = {};
 
+  const int64_t chunks = (p.rows + 31) >> 5;
+  // What a chunk's rows belong to: the adapter that all of them have, -1 for none, -2 for several.  With
+  // `counts`, adds up the adapters' rows there.
+  int* const kinds = reinterpret_cast<int*>(smem);                       // of kGradList chunks from `from` on
+  int* const counts = kinds + kGradList;                                 // of kGradAdapters
+  auto look_through = [&](int64_t from, int n, bool count) {
+    for (int c = tid; c < n; c += WAVES * 64) {
+      const int64_t t = (from + c) * 32;
+      int ids[32];
+      if (t + 32 <= p.rows) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const row_u32x4 v = reinterpret_cast<const Any16<4>*>(p.ids + t + 4 * i)->v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) ids[4 * i + e] = (int)v[e];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) ids[i] = t + i < p.rows ? p.ids[t + i] : -1;
+      }
+      loads_first();
+#pragma unroll
+      for (int i = 0; i < 32; ++i) ids[i] = ids[i] >= 0 && ids[i] < p.adapters ? ids[i] : -1;
+      bool one = true;
+#pragma unroll
+      for (int i = 1; i < 32; ++i) one = one && ids[i] == ids[0];
+      kinds[c] = one ? ids[0] : -2;
+      if (count && one) {
+        if (ids[0] >= 0) atomicAdd(&counts[ids[0]], 32);
+      } else if (count) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (ids[i] >= 0) atomicAdd(&counts[ids[i]], 1);
+      }
+    }
+  };
+  // this workgroup's adapter, which part of how many, and the first of them among all parts that are summed
+  int a = p.first_adapter + (int)blockIdx.z, part = 0, parts = 1, first_part = 0;
+  if (p.splits > 1 && p.adapters == 1) {
+    part = a;
+    parts = p.splits;
+    a = 0;
+    if (tid == 0 && part == 0 && blockIdx.x == 0 && blockIdx.y == 0) {
+      p.parts[0] = 0;
+      p.parts[1] = parts;
+    }
+  } else if (p.splits > 1) {
+    for (int i = tid; i < p.adapters; i += WAVES * 64) counts[i] = 0;
+    __syncthreads();
+    for (int64_t from = 0; from < chunks; from += kGradList)
+      look_through(from, (int)(chunks - from < kGradList ? chunks - from : kGradList), true);
+    __syncthreads();
+    int64_t total = 0;
+    for (int i = lane; i < p.adapters; i += 64) total += counts[i];
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) total += __shfl_xor(total, d);
+    // adapters in order, 64 at a time, until their parts pass this workgroup's number
+    int before = 0, summed = 0;
+    a = -1;
+    for (int base = 0; base < p.adapters; base += 64) {
+      const int own = base + lane < p.adapters ? grad_parts(counts[base + lane], total, p.splits) : 0;
+      int end = own, sums = own > 1 ? own : 0;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int e = __shfl_up(end, d), q = __shfl_up(sums, d);
+        end += lane >= d ? e : 0;
+        sums += lane >= d ? q : 0;
+      }
+      if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && wave == 0 && base + lane < p.adapters) {
+        p.parts[2 * (base + lane)] = summed + sums - (own > 1 ? own : 0);
+        p.parts[2 * (base + lane) + 1] = own;
+      }
+      const uint64_t past = __ballot(before + end > (int)blockIdx.z);
+      if (past && a < 0) {
+        const int l = __ffsll((unsigned long long)past) - 1;
+        a = base + l;
+        parts = __shfl(own, l);
+        part = (int)blockIdx.z - (before + __shfl(end, l) - parts);
+        first_part = summed + __shfl(sums, l) - (parts > 1 ? parts : 0);
+      }
+      before += __shfl(end, 63);
+      summed += __shfl(sums, 63);
+    }
+    a = __builtin_amdgcn_readfirstlane(a);
+    parts = __builtin_amdgcn_readfirstlane(parts);
+    part = __builtin_amdgcn_readfirstlane(part);
+    first_part = __builtin_amdgcn_readfirstlane(first_part);
+    __syncthreads();
+    if (a < 0) return;                         // more workgroups than parts
+  }
+
+  constexpr int DEEP = 3;                      // chunks whose loads are on their way
   struct Chunk {
-    uint32_t mine;             // rows of the adapter
+    int id;                    // of row l % 32
     row_u32x4 z[4];
     float v[VL][8];
   };
-  // lane: row 8 i + l / 8 and 8 columns of load i of Z; thread: row and 8 ranks of piece i of V
+  // lane: row 8 i + l / 8 and 8 columns of load i of Z; thread: row and 8 ranks of piece i of V.  Pieces that
+  // the end of a row cuts are the 8 elements that end with it, moved down before they are written; nothing in
+  // `load` depends on a branch, so that a chunk waits for its own loads alone.
   const int zc = 8 * (lane & 7);
+  const int64_t z_at = c0 + zc + 8 <= p.cols ? c0 + zc : p.cols - 8;
+  auto v_place = [&](int i, int& t, int& r) {
+    const int at = tid + i * (WAVES * 64) < 32 * 2 * FR ? tid + i * (WAVES * 64) : 32 * 2 * FR - 1;
+    t = at / (2 * FR);
+    r = r0 + 8 * (at % (2 * FR));
+  };
   auto load = [&](int64_t t0, Chunk& k) {
-    k.mine = (uint32_t)__ballot(lane < 32 && adapter_of(p, t0 + lane) == a);
-    if (live) {
+    k.id = p.ids[t0 + (lane & 31) < p.rows ? t0 + (lane & 31) : p.rows - 1];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t t = t0 + 8 * i + (lane >> 3) < p.rows ? t0 + 8 * i + (lane >> 3) : p.rows - 1;
-        if (whole) k.z[i] = load_any(p.X + t * p.ldx + c0 + zc);
-        else k.z[i] = load_part<true>(p.X + t * p.ldx, c0 + zc, p.cols);
-      }
+    for (int i = 0; i < 4; ++i) {
+      const int64_t t = t0 + 8 * i + (lane >> 3) < p.rows ? t0 + 8 * i + (lane >> 3) : p.rows - 1;
+      if constexpr (NARROW) k.z[i] = load_part<true>(p.X + t * p.ldx, c0 + zc, p.cols);
+      else k.z[i] = load_any(p.X + t * p.ldx + z_at);
     }
 #pragma unroll
     for (int i = 0; i < VL; ++i) {
-      const int at = tid + i * (WAVES * 64);
-      if (at < 32 * 2 * FR) {
-        const int64_t t = t0 + at / (2 * FR) < p.rows ? t0 + at / (2 * FR) : p.rows - 1;
-        load_ranks(p.V + t * p.ldv, r0 + 8 * (at % (2 * FR)), p.rank, k.v[i]);
+      int tv, r;
+      v_place(i, tv, r);
+      const int64_t t = t0 + tv < p.rows ? t0 + tv : p.rows - 1;
+      if constexpr (NARROW) {
+        load_ranks(p.V + t * p.ldv, r, p.rank, k.v[i]);
+      } else {
+        const float* q = p.V + t * p.ldv + (r + 8 <= p.rank ? r : p.rank - 8);
+        const row_u32x4 lo = reinterpret_cast<const Any16<4>*>(q)->v, hi = reinterpret_cast<const Any16<4>*>(q + 4)->v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) k.v[i][e] = __builtin_bit_cast(float, (uint32_t)(e < 4 ? lo[e] : hi[e - 4]));
       }
     }
   };
-  auto use = [&](const Chunk& k, int slot) {
-    const uint32_t v_at = v_all + (uint32_t)(slot * VSLOT);
-    wait_lds_all();
+  auto write = [&](const Chunk& k, int64_t t0, uint32_t slot) {
+    const uint32_t mine = (uint32_t)__ballot(k.id == a && t0 + (lane & 31) < p.rows);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int t = 8 * i + (lane >> 3);
-      lds_write16(z_own + (uint32_t)(t * ZP + 2 * zc), keep_if(k.mine >> t & 1, k.z[i]));
+      const row_u32x4 z = NARROW || whole ? k.z[i] : moved_down(k.z[i], c0 + zc - z_at);
+      lds_write16(z_own + slot + (uint32_t)(t * ZP + 2 * zc), keep_if(mine >> t & 1, z));
     }
 #pragma unroll
     for (int i = 0; i < VL; ++i) {
-      const int at = tid + i * (WAVES * 64);
-      if (at < 32 * 2 * FR) {
-        const int t = at / (2 * FR), r = 8 * (at % (2 * FR));
-        bf16x8 terms[TERMS];
-        split_terms<TERMS>(k.v[i], terms);
+      int t, r;
+      v_place(i, t, r);
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = k.v[i][e];
+      if (!NARROW && r0 + 16 * FR > p.rank) {
+        const int n = r + 8 <= p.rank ? 0 : r - (p.rank - 8);
+#pragma unroll
+        for (int d = 4; d >= 1; d >>= 1)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = (n & d) || n >= 8 ? (e + d < 8 && n < 8 ? v[e + d] : 0.f) : v[e];
+      }
+      bf16x8 terms[TERMS];
+      split_terms<TERMS>(v, terms);
+      if (tid + i * (WAVES * 64) < 32 * 2 * FR) {
 #pragma unroll
         for (int q = 0; q < TERMS; ++q)
-          lds_write16(v_at + (uint32_t)(q * 32 * VP + t * VP + 2 * r), keep_if(k.mine >> t & 1, __builtin_bit_cast(row_u32x4, terms[q])));
+          lds_write16(v_all + slot + (uint32_t)(q * 32 * VP + t * VP + 2 * (r - r0)),
+                      keep_if(mine >> t & 1, __builtin_bit_cast(row_u32x4, terms[q])));
       }
     }
-    wait_lds_all();
-    __builtin_amdgcn_s_barrier();              // (the slot's last readers passed the barrier before this one)
-    if (!live) return;
+  };
+  auto compute = [&](uint32_t slot) {
     const uint32_t lane_row = (uint32_t)(8 * g + (col >> 2));
     bf16x8 zf[4];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) zf[c] = read_transposed(z_own + lane_row * ZP + (uint32_t)(32 * c + 8 * (col & 3)), ZP);
+    for (int c = 0; c < 4; ++c) zf[c] = read_transposed(z_own + slot + lane_row * ZP + (uint32_t)(32 * c + 8 * (col & 3)), ZP);
 #pragma unroll
     for (int q = 0; q < TERMS; ++q)
 #pragma unroll
       for (int f = 0; f < FR; ++f) {
-        const bf16x8 vf = read_transposed(v_at + (uint32_t)(q * 32 * VP) + lane_row * VP + (uint32_t)(32 * f + 8 * (col & 3)), VP);
+        const bf16x8 vf = read_transposed(v_all + slot + (uint32_t)(q * 32 * VP) + lane_row * VP + (uint32_t)(32 * f + 8 * (col & 3)), VP);
 #pragma unroll
         for (int c = 0; c < 4; ++c)
           acc[c][f] = NK ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, zf[c], acc[c][f], 0, 0, 0)
@@ -660,89 +797,106 @@ __global__ __launch_bounds__(kGradWaves * 64) void lora_wgrad_kernel(LoraParams 
       }
   };
 
-  const int64_t chunks = (p.rows + 31) >> 5;
   for (int64_t from = 0; from < chunks; from += kGradList) {
-    // the list: a thread looks through a chunk's ids, 64 chunks a wave at a time
     const int n = (int)(chunks - from < kGradList ? chunks - from : kGradList);
+    if (p.splits == 1 || p.adapters == 1 || chunks > kGradList) look_through(from, n, false);
+    __syncthreads();
+    // the list: a thread to a chunk, 64 chunks a wave at a time
     int total = 0;
     for (int b = 0; b < n; b += WAVES * 64) {
       const int c = b + tid;
-      bool any = false;
-      if (c < n) {
-        const int64_t t = (from + c) * 32;
-        if (t + 32 <= p.rows) {
-          row_u32x4 v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = reinterpret_cast<const Any16<4>*>(p.ids + t + 4 * i)->v;
-          loads_first();
-#pragma unroll
-          for (int i = 0; i < 8; ++i) any |= v[i][0] == (uint32_t)a || v[i][1] == (uint32_t)a || v[i][2] == (uint32_t)a || v[i][3] == (uint32_t)a;
-        } else {
-          for (int i = 0; t + i < p.rows; ++i) any |= p.ids[t + i] == a;
-        }
-      }
+      bool any = c < n && kinds[c] == a;
+      if (c < n && kinds[c] == -2)
+        for (int i = 0; i < 32; ++i) any |= adapter_of(p, (from + c) * 32 + i) == a;
       const uint64_t m = __ballot(any);
-      if (lane == 0) counts[wave] = __popcll(m);
+      if (lane == 0) found[wave] = __popcll(m);
       __syncthreads();
       int at = total;
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) {
-        at += w < wave ? counts[w] : 0;
-        total += counts[w];
+        at += w < wave ? found[w] : 0;
+        total += found[w];
       }
       if (any) list[at + __popcll(m & ((1ull << lane) - 1))] = (uint16_t)c;
       __syncthreads();
     }
     total = __builtin_amdgcn_readfirstlane(total);
-    const int lo = (int)((int64_t)total * split / p.splits), hi = (int)((int64_t)total * (split + 1) / p.splits);
-    if (lo < hi) {
-      Chunk k;
-      load((from + __builtin_amdgcn_readfirstlane(list[lo])) * 32, k);
-      for (int i = lo; i < hi; ++i) {
-        Chunk next = k;
-        if (i + 1 < hi) load((from + __builtin_amdgcn_readfirstlane(list[i + 1])) * 32, next);
-        loads_first();
-        use(k, (i - lo) & 1);
-        k = next;
+    const int lo = (int)((int64_t)total * part / parts), hi = (int)((int64_t)total * (part + 1) / parts);
+    if (lo == hi) continue;                    // (for the whole workgroup; the list is not used again)
+    Chunk k[DEEP];
+    auto first_row = [&](int i) { return (from + __builtin_amdgcn_readfirstlane(list[i < hi ? i : hi - 1])) * 32; };
+    auto fetch = [&](int i, Chunk& c) {
+      load(first_row(i), c);
+      loads_first();
+    };
+#pragma unroll
+    for (int d = 0; d < DEEP; ++d) fetch(lo + d, k[d]);
+    write(k[0], first_row(lo), 0);
+    fetch(lo + DEEP, k[0]);
+    wait_lds_all();
+    __builtin_amdgcn_s_barrier();
+    uint32_t slot = 0;
+    for (int i = lo; i < hi; i += DEEP)
+#pragma unroll
+      for (int d = 0; d < DEEP; ++d) {
+        if (i + d >= hi) break;
+        // the next chunk goes into the other slot while this one is computed with (behind the last one: once more)
+        write(k[(d + 1) % DEEP], first_row(i + d + 1), SLOT - slot);
+        fetch(i + d + 1 + DEEP, k[(d + 1) % DEEP]);
+        compute(slot);
+        slot = SLOT - slot;
+        wait_lds_all();
+        __builtin_amdgcn_s_barrier();
       }
-    }
     __syncthreads();
   }
   if (!live) return;
   // NK: a lane holds column l % 16 and 4 ranks of a fragment, else rank l % 16 and 4 columns
+  const int64_t line = NK ? p.rank : p.all_cols;                         // of the sums of a part
 #pragma unroll
   for (int c = 0; c < 4; ++c)
 #pragma unroll
-    for (int f = 0; f < FR; ++f)
+    for (int f = 0; f < FR; ++f) {
+      const int64_t n = c0 + 16 * c + (NK ? col : 4 * g);
+      const int r = r0 + 16 * f + (NK ? 4 * g : col);
+      if (n >= p.cols || r >= p.rank) continue;
+      const int64_t inside = NK ? p.rank - r : p.cols - n;               // of the 4
+      const f32x4 v = acc[c][f];
+      if (parts > 1) {
+        float* to = p.sums + (int64_t)(first_part + part) * p.all_cols * p.rank + (NK ? (p.first_col + n) * line + r : r * line + p.first_col + n);
+        store4(to, v, inside);
+      } else {
+        const int64_t at = (int64_t)a * p.stride_y + (NK ? n * p.ldy + r : r * p.ldy + n);
+        if constexpr (OB) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int64_t n = c0 + 16 * c + (NK ? col : 4 * g + e);
-        const int r = r0 + 16 * f + (NK ? 4 * g + e : col);
-        if (n >= p.cols || r >= p.rank) continue;
-        if (p.splits > 1) {
-          const int64_t plane = ((int64_t)split * p.adapters + a) * p.all_cols * p.rank;
-          p.sums[plane + (NK ? (p.first_col + n) * p.rank + r : r * p.all_cols + p.first_col + n)] = acc[c][f][e];
+          for (int e = 0; e < 4; ++e)
+            if (e < inside) reinterpret_cast<__bf16*>(p.Y)[at + e] = (__bf16)v[e];
         } else {
-          const int64_t at = (int64_t)a * p.stride_y + (NK ? n * p.ldy + r : r * p.ldy + n);
-          if constexpr (OB) reinterpret_cast<__bf16*>(p.Y)[at] = (__bf16)acc[c][f][e];
-          else reinterpret_cast<float*>(p.Y)[at] = acc[c][f][e];
+          store4(reinterpret_cast<float*>(p.Y) + at, v, inside);
         }
       }
+    }
 }
 
-// G from the sums of the parts of the rows, in their order.
-template <bool NK, bool OB>
-__global__ __launch_bounds__(256) void lora_grad_sum(LoraParams p) {
-  const int64_t each = p.all_cols * p.rank, n = each * p.adapters;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t a = i / each, at = i % each;
-    const int64_t c = NK ? at / p.rank : at % p.all_cols, r = NK ? at % p.rank : at / p.all_cols;
-    float v = p.sums[i];
-    for (int k = 1; k < p.splits; ++k) v += p.sums[k * n + i];
-    const int64_t to = a * p.stride_y + (NK ? c * p.ldy + r : r * p.ldy + c);
-    if constexpr (OB) reinterpret_cast<__bf16*>(p.Y)[to] = (__bf16)v;
-    else reinterpret_cast<float*>(p.Y)[to] = v;
+// G of an adapter from the sums of its parts, in their order; a thread takes an element.
+template <bool OB>
+__global__ __launch_bounds__(256) void lora_grad_sum(LoraParams p, int64_t lines, int64_t line) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = lines * line;
+  const int first = p.parts[2 * blockIdx.y], parts = p.parts[2 * blockIdx.y + 1];
+  if (i >= n || parts < 2) return;
+  const float* s = p.sums + first * n + i;
+  float v = 0.f;
+  for (int k = 0; k < parts; k += 8) {
+    float part[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) part[u] = s[(k + u < parts ? k + u : parts - 1) * n];
+    loads_first();
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v = k + u < parts ? v + part[u] : v;
   }
+  const int64_t row = (uint32_t)i / (uint32_t)line, to = blockIdx.y * p.stride_y + row * p.ldy + (i - row * line);
+  if constexpr (OB) reinterpret_cast<__bf16*>(p.Y)[to] = (__bf16)v;
+  else reinterpret_cast<float*>(p.Y)[to] = v;
 }
 
 int lanes_for(int rank, int most) {
@@ -815,26 +969,43 @@ hipError_t launch_lora_up(const LoraParams& p, bool nk, bool bf16, int num_cus, 
 }
 
 int lora_wgrad_splits(int64_t rows, int64_t cols, int rank, int adapters, int num_cus) {
-  // parts of the rows, so that one adapter's workgroups fill the chip; each at least a chunk for every wave
-  const int fr = rank <= 64 ? (rank + 15) / 16 : 4;
+  if (adapters > kGradAdapters) return 1;
+  // parts of the rows, so that the workgroups of one adapter that has them all fill the chip twice; each of 8
+  // chunks at least.  Their sums are written and read back: 16 MB at most.  (2^31: one launch.)
+  const int fr = cols < 8 ? 1 : rank <= 64 ? (rank + 15) / 16 : 4;
   const int64_t groups = (cols + kGradColumns - 1) / kGradColumns * ((rank + 16 * fr - 1) / (16 * fr));
-  // (as if the rows were dealt out evenly: 4 chunks to a workgroup)
-  const int64_t chunks = (rows + 31) / 32;
-  int64_t splits = groups > 0 ? 2 * (int64_t)num_cus / (groups * adapters) : 1;
-  if (splits > chunks / (4 * (int64_t)adapters)) splits = chunks / (4 * (int64_t)adapters);
-  if (splits > 16) splits = 16;
-  return splits < 1 ? 1 : (int)splits;
+  const int64_t chunks = (rows + 31) / 32, each = cols * rank;
+  if (each < 1 || groups * (adapters + 32) > (int64_t)1 << 22) return 1;
+  int64_t splits = 3 * (int64_t)num_cus / groups;
+  if (splits > chunks / 8) splits = chunks / 8;
+  if (splits > 32) splits = 32;
+  if (splits > ((int64_t)4 << 20) / each) splits = ((int64_t)4 << 20) / each;
+  return splits < 2 ? 1 : (int)splits;
 }
 
 template <bool NK, bool OB>
 static hipError_t wgrad_launch(const LoraParams& all, hipStream_t stream) {
-  const int fr = all.rank <= 64 ? (all.rank + 15) / 16 : 4;
+  const bool narrow = all.cols < 8 || all.rank < 8;
+  const int fr = narrow ? 1 : all.rank <= 64 ? (all.rank + 15) / 16 : 4;
+  const auto kernel = narrow    ? lora_wgrad_kernel<1, true, NK, OB>
+                      : fr == 1 ? lora_wgrad_kernel<1, false, NK, OB>
+                      : fr == 2 ? lora_wgrad_kernel<2, false, NK, OB>
+                      : fr == 3 ? lora_wgrad_kernel<3, false, NK, OB>
+                                : lora_wgrad_kernel<4, false, NK, OB>;
   const int64_t across = (all.cols + kGradColumns - 1) / kGradColumns;
-  const int64_t ranks = (all.rank + 16 * fr - 1) / (16 * fr) * all.splits;
-  // launches of less than 2^31 threads
-  const int64_t threads = kGradWaves * 64;
+  const int64_t ranks = (all.rank + 16 * fr - 1) / (16 * fr), threads = kGradWaves * 64;
   LoraParams p = all;
   p.all_cols = all.cols;
+  if (all.splits > 1) {
+    // (an adapter has a part at least, and all of them together `splits` more at most)
+    const int64_t most = all.adapters == 1 ? all.splits : all.adapters + all.splits;
+    hipError_t e = launch_kernel(kernel, dim3((unsigned)across, (unsigned)ranks, (unsigned)most), dim3((unsigned)threads), 0, stream, p);
+    if (e != hipSuccess) return e;
+    const int64_t lines = NK ? all.cols : all.rank, line = NK ? all.rank : all.cols;
+    return launch_kernel(lora_grad_sum<OB>, dim3((unsigned)((lines * line + 255) / 256), (unsigned)all.adapters), dim3(256), 0,
+                         stream, p, lines, line);
+  }
+  // launches of less than 2^31 threads
   const int64_t width = across < (1 << 14) ? across : 1 << 14;
   int64_t deep = ((int64_t)1 << 31) / (width * ranks * threads);
   deep = deep < 1 ? 1 : deep > 32768 ? 32768 : deep;
@@ -847,16 +1018,10 @@ static hipError_t wgrad_launch(const LoraParams& all, hipStream_t stream) {
       p.Y = static_cast<char*>(all.Y) + p.first_col * (NK ? all.ldy : 1) * (OB ? 2 : 4);
       const dim3 grid((unsigned)((p.cols + kGradColumns - 1) / kGradColumns), (unsigned)ranks,
                       (unsigned)(all.adapters - first < deep ? all.adapters - first : deep));
-      const hipError_t e = launch_kernel(fr == 1   ? lora_wgrad_kernel<1, NK, OB>
-                                         : fr == 2 ? lora_wgrad_kernel<2, NK, OB>
-                                         : fr == 3 ? lora_wgrad_kernel<3, NK, OB>
-                                                   : lora_wgrad_kernel<4, NK, OB>, grid, dim3((unsigned)threads), 0, stream, p);
+      const hipError_t e = launch_kernel(kernel, grid, dim3((unsigned)threads), 0, stream, p);
       if (e != hipSuccess) return e;
     }
-  if (all.splits < 2) return hipSuccess;
-  p.Y = all.Y;
-  const int64_t n = all.cols * all.rank * all.adapters, blocks = (n + 255) / 256;
-  return launch_kernel(lora_grad_sum<NK, OB>, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, stream, p);
+  return hipSuccess;
 }
 
 hipError_t launch_lora_wgrad(const LoraParams& p, bool nk, bool bf16, hipStream_t stream) {

@@ -70,19 +70,27 @@ __global__ __launch_bounds__(256, 4) void lora_down_kernel(LoraParams p) {
   }
 }
 
-// V from the sums of the ranges of K, in their order.
+// V from the sums of the ranges of K, in their order: a workgroup takes 256 / LANES rows, LANES threads a row.
+template <int LANES>
 __global__ __launch_bounds__(256) void lora_down_sum(LoraParams p) {
+  const int64_t t = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  if (t >= p.rows) return;
+  const int a = p.ids[t];
+  const bool live = a >= 0 && a < p.adapters;
+  const float scale = live && p.scales ? p.scales[a] : 1.f;
   const int64_t n = p.rows * p.rank;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t t = i / p.rank;
-    const int a = p.ids[t];
+  for (int r = threadIdx.x % LANES; r < p.rank; r += LANES) {
+    const float* s = p.sums + t * p.rank + r;
     float v = 0.f;
-    if (a >= 0 && a < p.adapters) {
-      v = p.sums[i];
-      for (int k = 1; k < p.splits; ++k) v += p.sums[k * n + i];
-      v *= p.scales ? p.scales[a] : 1.f;
+    for (int k = 0; k < p.splits; k += 8) {
+      float part[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) part[u] = s[(k + u < p.splits ? k + u : p.splits - 1) * n];
+      __builtin_amdgcn_sched_barrier(0);       // (all loads are on their way first)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v = k + u < p.splits ? v + part[u] : v;
     }
-    p.V[t * p.ldv + (i - t * p.rank)] = v;
+    p.V[t * p.ldv + r] = live ? scale * v : 0.f;
   }
 }
 
@@ -101,8 +109,8 @@ hipError_t launch_lora_down_tiles(const LoraParams& p, bool nk, hipStream_t stre
   const dim3 grid((unsigned)((p.rows + kTile - 1) / kTile), (unsigned)p.splits, (unsigned)(kSlots * ((p.rank + kTile - 1) / kTile)));
   hipError_t e = launch_kernel(nk ? lora_down_kernel<true> : lora_down_kernel<false>, grid, dim3(256), 0, stream, p);
   if (e != hipSuccess || p.splits == 1) return e;
-  const int64_t blocks = (p.rows * p.rank + 255) / 256;
-  return launch_kernel(lora_down_sum, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream, p);
+  if (p.rank <= 16) return launch_kernel(lora_down_sum<16>, dim3((unsigned)((p.rows + 15) / 16)), dim3(256), 0, stream, p);
+  return launch_kernel(lora_down_sum<64>, dim3((unsigned)((p.rows + 3) / 4)), dim3(256), 0, stream, p);
 }
 
 }  // namespace sfc

@@ -28,10 +28,12 @@ struct LoraParams {
   int64_t ld_base;
   void* Y;
   int64_t ldy, stride_y;     // stride_y: gradient, between adapters
-  // gradient: parts of the rows; their sums (splits > 1), [splits][adapters], each as G; this launch's first
-  // column.  down: ranges of K, their sums (splits > 1) [splits][rows][rank]
+  // down: ranges of K, their sums (splits > 1) [splits][rows][rank].  gradient: parts of the rows that are
+  // dealt out over the adapters (splits > 1), the sums of those that are not alone, each as G, and for every
+  // adapter the first of its parts among them and their number; this launch's first column
   int splits;
   float* sums;
+  int32_t* parts;
   int64_t all_cols, first_col;
 };
 int lora_wgrad_splits(int64_t rows, int64_t cols, int rank, int adapters, int num_cus);

@@ -65,9 +65,10 @@ size_t down_sums(int64_t rows, int64_t K, int64_t rank, int cus) {
   return most;
 }
 
-// Bytes of the sums of an adapters' weight gradient over parts of the rows.
+// Bytes that an adapters' weight gradient over parts of the rows keeps: two numbers for every adapter, then the sums.
+size_t lora_table(int adapters) { return (size_t)((adapters * (int64_t)8 + 15) / 16 * 16); }
 size_t lora_sums(int splits, int64_t columns, int64_t rank, int adapters) {
-  return splits > 1 ? (size_t)splits * (size_t)adapters * (size_t)columns * (size_t)rank * 4u : 0;
+  return splits > 1 ? lora_table(adapters) + (size_t)splits * (size_t)columns * (size_t)rank * 4u : 0;
 }
 
 }  // namespace
@@ -244,7 +245,10 @@ int sfc_lora_wgrad(int64_t rows, int64_t columns, int64_t rank, int adapters, co
     rc = sfc::host_workspace(as_stream(stream), need, &ws);
     if (rc != SFC_OK) return rc;
   }
-  p.sums = static_cast<float*>(ws);
+  if (p.splits > 1) {
+    p.parts = static_cast<int32_t*>(ws);
+    p.sums = reinterpret_cast<float*>(static_cast<char*>(ws) + lora_table(adapters));
+  }
   p.rows = rows;
   p.cols = columns;
   p.rank = (int)rank;
