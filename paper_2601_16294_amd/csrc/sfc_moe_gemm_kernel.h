@@ -409,7 +409,9 @@ __device__ __forceinline__ void moe_block(const MoeGemmParams& p, const MoeTask&
   const int mv = t.a.valid, nv = t.b.valid;
   if (mv == BM && nv == BN) moe_store<BM, BN, OB, true, PAST>(p, t, mv, nv, acc, lds0, wave, lane);
   else moe_store<BM, BN, OB, false, PAST>(p, t, mv, nv, acc, lds0, wave, lane);
-  __syncthreads();                // the ring may be filled again
+  // the ring may be filled again (the stores need not have arrived for that)
+  wait_lds_all();
+  __builtin_amdgcn_s_barrier();
 }
 
 // Blocks of rows of all experts in turn, in supertiles of up to 8 of them by all blocks of columns
@@ -423,21 +425,54 @@ __global__ __launch_bounds__(256, (MoeTile<BM, BN>::PER_CU)) void moe_gemm_kerne
   const uint32_t lds0 = lds_addr(smem);
   const int P = gridDim.x, rank = xcd_rank(blockIdx.x, P);
   constexpr int ES = OB ? 2 : 4;
-  // Tasks of this workgroup: its rank of every full round, and in the last, partial one its rank among as
-  // many workgroups as there are tasks left (the first ones: spread over all chiplets).
-  auto next_task = [&](int64_t task, int64_t total) {
-    const int64_t from = task < 0 ? 0 : (task / P + 1) * P;       // the round's first task
-    if (from + P <= total) return from + rank;
-    const int left = (int)(total - from);
-    return (int)blockIdx.x < left ? from + xcd_rank(blockIdx.x, left) : (int64_t)-1;
+  // Calls block(task) for this workgroup's tasks: its rank of every full round, and in the last, partial one its
+  // rank among as many workgroups as there are tasks left (the first ones: spread over all chiplets).  A last round
+  // that is at most half full is taken in quarters of blocks, quarter(task, q): 256x256 blocks of 64 stages, 1088
+  // on 256 CUs, XX us instead of XX.
+  constexpr bool QUARTERS = BM > 64;
+  auto each_task = [&](int64_t total, auto block, auto quarter) {
+    const int64_t full = total / P * P;
+    const int left = (int)(total - full);
+    const bool quarters = QUARTERS && 2 * left <= P;
+    const int64_t last = !quarters && (int)blockIdx.x < left ? full + xcd_rank(blockIdx.x, left) : -1;
+    for (int64_t task = full > 0 ? rank : last; task >= 0; task = task + P < full ? task + P : task < full ? last : -1) block(task);
+    if (!quarters) return;
+    for (int i = blockIdx.x; i < 4 * left; i += P) {
+      // (quarters of a task run on one chiplet: its ranks are consecutive)
+      const int r = 4 * left <= P ? xcd_rank(i, 4 * left) : i < P ? xcd_rank(i, P) : P + xcd_rank(i - P, 4 * left - P);
+      quarter(full + r / 4, r % 4);
+    }
+  };
+  // the quarter q of a block: rows and columns it starts at, in the block
+  auto cut = [&](MoeTask& t, int q) {
+    const int m = (q >> 1) * (BM / 2), n = (q & 1) * (BN / 2);
+    t.a.valid = t.a.valid - m < BM / 2 ? t.a.valid - m : BM / 2;
+    t.b.valid = t.b.valid - n < BN / 2 ? t.b.valid - n : BN / 2;
+    if constexpr (GATHER) t.a.order += m;
+    else t.a.base += (uint64_t)(LAYOUT == kMoeTN ? m : m * p.lda) * 2;
+    t.b.base += (uint64_t)(LAYOUT == kMoeNK ? n * p.ldb : n) * 2;
+    t.C += (m * p.ldc + n) * ES;
+    return t.a.valid > 0 && t.b.valid > 0;
   };
   MoeTask t = {};
   t.a.ld = p.lda;
   t.b.ld = p.ldb;
+  auto run = [&](int64_t total, auto place) {
+    each_task(total,
+              [&](int64_t task) {
+                place(task);
+                moe_block<BM, BN, LAYOUT, GATHER, OB, PAST>(p, t, lds0, wave, lane);
+              },
+              [&](int64_t task, int q) {
+                place(task);
+                if constexpr (QUARTERS)
+                  if (cut(t, q)) moe_block<BM / 2, BN / 2, LAYOUT, GATHER, OB, PAST>(p, t, lds0, wave, lane);
+              });
+  };
   if constexpr (LAYOUT == kMoeTN) {
     const Segments seg = {p.offsets, p.experts, p.K};
     const int64_t cells = (int64_t)p.gm * p.gn, total = cells * p.experts;
-    for (int64_t task = next_task(-1, total); task >= 0; task = next_task(task, total)) {
+    auto place = [&](int64_t task) {
       const int e = (int)(task / cells);
       const int cell = load_scalar_i32(p.table + (task - (int64_t)e * cells));
       const int64_t m0 = (int64_t)(cell / p.gn) * BM, n0 = (int64_t)(cell % p.gn) * BN;
@@ -449,8 +484,8 @@ __global__ __launch_bounds__(256, (MoeTile<BM, BN>::PER_CU)) void moe_gemm_kerne
       t.b.valid = p.N - n0 < BN ? (int)(p.N - n0) : BN;
       t.depth = hi - lo;
       t.C = reinterpret_cast<char*>(p.C) + ((int64_t)e * p.stride_c + m0 * p.ldc + n0) * ES;
-      moe_block<BM, BN, LAYOUT, false, OB, PAST>(p, t, lds0, wave, lane);
-    }
+    };
+    run(total, place);
   } else {
     const Segments seg = {p.offsets, p.experts, p.M};
     int used;
@@ -458,7 +493,7 @@ __global__ __launch_bounds__(256, (MoeTile<BM, BN>::PER_CU)) void moe_gemm_kerne
     t.a.rows = p.a_rows;
     t.a.topk = p.topk;
     t.depth = p.K;
-    for (int64_t task = next_task(-1, total); task >= 0; task = next_task(task, total)) {
+    auto place = [&](int64_t task) {
       int first = 0, gm = 0;
       const int e = __builtin_amdgcn_readfirstlane(seg.find<BM>((int)(task / p.gn), lane, first, gm));
       int64_t lo, hi;
@@ -475,8 +510,8 @@ __global__ __launch_bounds__(256, (MoeTile<BM, BN>::PER_CU)) void moe_gemm_kerne
       t.a.valid = hi - m0 < BM ? (int)(hi - m0) : BM;
       t.b.valid = p.N - n0 < BN ? (int)(p.N - n0) : BN;
       t.C = reinterpret_cast<char*>(p.C) + (m0 * p.ldc + n0) * ES;
-      moe_block<BM, BN, LAYOUT, GATHER, OB, PAST>(p, t, lds0, wave, lane);
-    }
+    };
+    run(total, place);
     // rows of no expert
     for (int64_t r = (int64_t)used + blockIdx.x; r < p.M; r += P)
       for (int64_t c = tid; c < p.N; c += 256) {

@@ -29,8 +29,11 @@ struct MoeGemmParams {
   int gm, gn;
   bool past;                 // C goes past the caches
 };
-// Blocks of 256 x 256, one workgroup to a CU, or of 128 x 128, two.
+// Blocks of 256 x 256, one workgroup to a CU, of 128 x 128, two, or of 64 x 64, four.
 hipError_t launch_moe_256x256(const MoeGemmParams& p, MoeLayout layout, bool out_bf16, int grid, hipStream_t stream);
+hipError_t launch_moe_64x64(const MoeGemmParams& p, MoeLayout layout, bool out_bf16, int grid, hipStream_t stream);
 hipError_t launch_moe_128x128(const MoeGemmParams& p, MoeLayout layout, bool out_bf16, int grid, hipStream_t stream);
+// Few rows of each expert, kMoeNK: 16 * fn rows of an expert's weights past 16 * fm of its rows (fn = 1 for fm = 1 alone).
+hipError_t launch_moe_rows(const MoeGemmParams& p, int fm, int fn, bool out_bf16, hipStream_t stream);
 
 }  // namespace sfc

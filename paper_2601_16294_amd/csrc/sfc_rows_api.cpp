@@ -21,23 +21,60 @@ int reject(const Checked& c) { return sfc::host_error(c.code, c.msg); }
 hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 const uint16_t* bf16(const void* p) { return static_cast<const uint16_t*>(p); }
 
+int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
+
 // Whether a C of so many elements goes past the caches: from 32 MB on, as for the 4-bit products.
 bool past_caches(int64_t elements, int out_type) { return elements * sfc::type_size(out_type) >= (int64_t)32 << 20; }
 
-// Microseconds of `tasks` blocks over `stages` 64-deep stages.
-double moe_tile_us(bool large, double tasks, double stages, bool out_f32, int num_cus) {
-  const double slots = large ? num_cus : 2 * num_cus;
+// Microseconds of `tasks` blocks of b x b over `stages` 64-deep stages on the tile kernels, fitted to timings of
+// random operands (rows from 2 to 16384 over 1 to 64 experts, sides 512 to 14336, weight gradients too;
+// mostly within 20 %): what a full round of blocks takes, and a last, partial one, with its stores.
+double moe_tile_us(int b, double tasks, double stages, bool out_f32, int num_cus) {
+  const double slots = (b == 256 ? 1.0 : b == 128 ? 2.0 : 4.0) * num_cus;
   const double full = (double)(int64_t)(tasks / slots), part = tasks / slots - full;
-  double us = full * (large ? 1.4 * stages + (out_f32 ? 11.0 : 5.5) : 0.9 * stages + (out_f32 ? 4.5 : 2.5));
-  if (part > 0) {
-    if (large) us += (1.1 + 0.3 * part) * stages + 2.0 + (out_f32 ? 9.0 : 3.5) * part;
-    else if (part <= 0.5) us += (0.45 + 0.15 * part) * stages + 0.4 + (out_f32 ? 4.5 : 2.2) * part;
-    else us += (0.25 + 0.65 * part) * stages + (out_f32 ? 4.0 : 2.5);
+  if (b == 256) return full * (1.5 * stages + (out_f32 ? 14 : 9)) + (part > 0 ? (1.3 + 0.2 * part) * stages + 3 + (out_f32 ? 11 : 6) * part : 0);
+  if (b == 128) {
+    const double last = part <= 0.5 ? (0.58 + 0.3 * part) * stages + 3.5 : (0.3 + 0.75 * part) * stages + (out_f32 ? 5 : 3);
+    return full * (1.02 * stages + (out_f32 ? 7 : 4)) + (part > 0 ? last : 0);
   }
-  return us;
+  return full * (1.1 * stages + 4) + (part > 0 ? (0.45 + 0.65 * part) * stages + 2 : 0);
 }
 
-int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
+// The block shape of the least estimated time; tasks(b) is the number of b x b blocks.
+template <class F>
+int moe_block_of(F tasks, double stages, bool out_f32, int num_cus) {
+  int best = 256;
+  double us = moe_tile_us(256, tasks(256), stages, out_f32, num_cus);
+  for (int b = 128; b >= 64; b /= 2) {
+    const double t = moe_tile_us(b, tasks(b), stages, out_f32, num_cus);
+    if (t < us) {
+      us = t;
+      best = b;
+    }
+  }
+  return best;
+}
+
+hipError_t moe_tiles(int b, const sfc::MoeGemmParams& p, sfc::MoeLayout layout, bool ob, int64_t tasks, int num_cus, hipStream_t stream) {
+  const int64_t slots = (b == 256 ? 1 : b == 128 ? 2 : 4) * (int64_t)num_cus;
+  const int grid = (int)(tasks < slots ? tasks : slots);
+  return b == 256   ? sfc::launch_moe_256x256(p, layout, ob, grid, stream)
+         : b == 128 ? sfc::launch_moe_128x128(p, layout, ob, grid, stream)
+                    : sfc::launch_moe_64x64(p, layout, ob, grid, stream);
+}
+
+// Whether an experts' product runs on the kernel that streams the weights past 16 fm rows at a time (fm > 0), us
+// there / on the best blocks.  Rows of 16-byte pieces: 8 an expert on average (8 experts 4096x4096, 2 rows
+// 17 / 34, 32 rows 42 / 50, 64 rows 47 / 52, 128 rows 71 / 53; 64 experts 2048x4096, 128 rows 140 / 182, 512 rows 195 /
+// 229), or few in all and too few blocks to fill the chip (1 expert, 64 rows 25 / 34).  Others, whose loads
+// straddle lines: less than a row to an expert (8 experts 4096x4095, 2 rows 33 / 42, 32 rows 160 / 60).
+int moe_few_rows(int64_t rows, int64_t N, int experts, bool aligned, int num_cus) {
+  if (sfc::ceil_div(N, 16) * 512 * experts >= (int64_t)1 << 31) return 0;
+  if (!aligned) return 2 * rows <= experts ? 1 : 0;
+  if (rows <= 8 * (int64_t)experts) return 1;
+  if (rows <= 64 && sfc::ceil_div(N, 32) * experts <= num_cus) return rows <= 32 ? 2 : 4;
+  return 0;
+}
 
 // Launches a part at a time: rows first .. first + count - 1 and columns col .. col + width - 1, so
 // that a launch has less than 2^32 threads (at most 512 for a row, and 4 for a row and column).
@@ -89,17 +126,19 @@ int sfc_moe_gemm_ex(int64_t rows, int64_t N, int64_t K, int experts, const void*
   sfc::MoeGemmParams p = {rows, N, K, bf16(A), lda, order, a_rows, order ? topk : 1, bf16(B), ldb, stride_b, C, ldc, 0,
                           offsets, experts, nullptr, 0, 0, past_caches(rows * N, out_type)};
   const bool ob = out_type == SFC_OUT_BF16;
-  const double stages = (double)sfc::ceil_div(K > 0 ? K : 1, 64);
-  // blocks of rows: every expert's last one is on average half full
-  auto tasks = [&](int64_t b) { return ((double)rows / (double)b + 0.5 * experts) * (double)sfc::ceil_div(N, b); };
-  const bool big = moe_tile_us(true, tasks(256), stages, !ob, cus) < moe_tile_us(false, tasks(128), stages, !ob, cus);
-  const int b = big ? 256 : 128;
-  p.gn = (int)sfc::ceil_div(N, b);
-  const int64_t most = (sfc::ceil_div(rows, b) + experts) * p.gn, slots = big ? cus : 2 * cus;
-  const int grid = (int)(most < slots ? most : slots);
-  const sfc::MoeLayout layout = b_layout == SFC_B_NK ? sfc::kMoeNK : sfc::kMoeKN;
-  const hipError_t e = big ? sfc::launch_moe_256x256(p, layout, ob, grid, as_stream(stream))
-                           : sfc::launch_moe_128x128(p, layout, ob, grid, as_stream(stream));
+  const bool aligned = ((uintptr_t)A | (uintptr_t)B) % 16 == 0 && (lda | ldb | stride_b) % 8 == 0;
+  const int fm = b_layout == SFC_B_NK ? moe_few_rows(rows, N, experts, aligned, cus) : 0;
+  hipError_t e;
+  if (fm) {
+    e = sfc::launch_moe_rows(p, fm, fm == 1 ? 1 : 2, ob, as_stream(stream));
+  } else {
+    // rows of an expert that has some fill a block at least, and part of a last one
+    const double used = (double)least(rows, experts), each = (double)rows / used;
+    auto tasks = [&](int b) { return used * (each > 0.5 * b ? each / b + 0.5 : 1.0) * (double)sfc::ceil_div(N, b); };
+    const int b = moe_block_of(tasks, (double)sfc::ceil_div(K > 0 ? K : 1, 64), !ob, cus);
+    p.gn = (int)sfc::ceil_div(N, b);
+    e = moe_tiles(b, p, b_layout == SFC_B_NK ? sfc::kMoeNK : sfc::kMoeKN, ob, (sfc::ceil_div(rows, b) + experts) * p.gn, cus, as_stream(stream));
+  }
   return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "experts' product");
 }
 
@@ -118,20 +157,13 @@ int sfc_moe_wgrad_ex(int64_t M, int64_t N, int64_t rows, int experts, const void
   sfc::MoeGemmParams p = {M, N, rows, bf16(A), lda, nullptr, 0, 1, bf16(B), ldb, 0, C, ldc, stride_c,
                           offsets, experts, nullptr, 0, 0, past_caches(M * N * experts, out_type)};
   const bool ob = out_type == SFC_OUT_BF16;
-  const double stages = (double)sfc::ceil_div(rows > 0 ? rows : 1, 64 * (int64_t)experts);
-  auto us = [&](int64_t b) {
-    return moe_tile_us(b == 256, (double)(sfc::ceil_div(M, b) * sfc::ceil_div(N, b) * experts), stages, !ob, cus);
-  };
-  const bool big = us(256) < us(128);
-  const int b = big ? 256 : 128;
+  auto tasks = [&](int b) { return (double)(sfc::ceil_div(M, b) * sfc::ceil_div(N, b)) * experts; };
+  const int b = moe_block_of(tasks, (double)sfc::ceil_div(rows > 0 ? rows : 1, 64 * (int64_t)experts), !ob, cus);
   p.gm = (int)sfc::ceil_div(M, b);
   p.gn = (int)sfc::ceil_div(N, b);
   rc = sfc::host_table(p.gm, p.gn, st, &p.table);
   if (rc != SFC_OK) return rc;
-  const int64_t tasks = (int64_t)p.gm * p.gn * experts, slots = big ? cus : 2 * cus;
-  const int grid = (int)(tasks < slots ? tasks : slots);
-  const hipError_t e = big ? sfc::launch_moe_256x256(p, sfc::kMoeTN, ob, grid, st)
-                           : sfc::launch_moe_128x128(p, sfc::kMoeTN, ob, grid, st);
+  const hipError_t e = moe_tiles(b, p, sfc::kMoeTN, ob, (int64_t)p.gm * p.gn * experts, cus, st);
   return e == hipSuccess ? SFC_OK : sfc::host_hip_error(e, "experts' weight gradient");
 }
 

@@ -52,7 +52,7 @@ inline Checked check_moe_gemm(int64_t rows, int64_t N, int64_t K, int experts, i
   SFC_RETURN_IF(check_bf16(B, nk ? N : K, nk ? K : N, ldb, "B is NULL", "rows of B are longer than ldb"));
   if (K > 0 && experts > 1 && stride_b < 0) return fail(SFC_ERR_INVALID_ARG, "the experts' stride must be >= 0");
   // a block of rows may be partly filled for every expert
-  if ((ceil_div(rows, 128) + experts) * ceil_div(N, 16) >= kMaxDim)
+  if ((ceil_div(rows, 64) + experts) * ceil_div(N, 64) >= kMaxDim)
     return fail(SFC_ERR_UNSUPPORTED, "too many output blocks");
   return ok();
 }
@@ -69,7 +69,8 @@ inline Checked check_moe_wgrad(int64_t M, int64_t N, int64_t rows, int experts, 
   SFC_RETURN_IF(check_index(offsets, "offsets is NULL"));
   SFC_RETURN_IF(check_bf16(A, rows, M, lda, "A is NULL", "lda < M"));
   SFC_RETURN_IF(check_bf16(B, rows, N, ldb, "B is NULL", "ldb < N"));
-  return check_blocks(M, N, experts);
+  if (ceil_div(M, 64) * ceil_div(N, 64) >= kMaxDim / experts) return fail(SFC_ERR_UNSUPPORTED, "too many output blocks");
+  return ok();
 }
 
 // Sizes shared by the adapters' calls.
