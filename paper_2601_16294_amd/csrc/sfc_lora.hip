@@ -360,9 +360,11 @@ __global__ __launch_bounds__(256) void lora_row_up_kn(LoraParams p) {
 
 // ---- up, in tiles --------------------------------------------------------------------------------
 
-// Ranks in NC chunks of 32; columns of a workgroup, so that its weights take 20 to 36 KB of LDS.
-template <int NC>
-constexpr int up_columns() { return NC <= 2 ? 256 : NC == 4 ? 128 : 64; }
+// Ranks in NC chunks of 32; columns of a workgroup.  Wide blocks read V least often, narrow ones take fewer
+// registers (us at 64 / 128 / 256 columns: bf16 4096x14336 rank 64 74 / 65 / 61, 8192x4096 rank 16 28 / 25 / 27, fp32
+// 1003x5003 rank 12 17 / 14 / 26).
+template <int NC, bool OB>
+constexpr int up_columns() { return NC == 2 && OB ? 256 : NC <= 4 ? 128 : 64; }
 
 // Column of 64 that lane n of fragment j computes, so that a lane, which ends with 4 columns of every
 // fragment, has 16 bytes of a row at a time, and 4 lanes 64: bf16 8 columns of two fragments, fp32 4 of one.
@@ -377,7 +379,7 @@ __device__ __forceinline__ int up_column(int j, int n) {
 // workgroups: those in flight cover whole rows.
 template <int Q, int NC, bool NK, bool OB>
 __global__ __launch_bounds__(256, (NC == 1 ? 3 : 2)) void lora_up_kernel(LoraParams p) {
-  constexpr int TERMS = OB ? 2 : 3, ES = OB ? 2 : 4, CB = up_columns<NC>(), UNITS = CB / 64;
+  constexpr int TERMS = OB ? 2 : 3, ES = OB ? 2 : 4, CB = up_columns<NC, OB>(), UNITS = CB / 64;
   constexpr int PITCH = NK ? NC * 64 + 16 : CB * 2 + 16;     // NK: [column][rank], else [rank][column]
   constexpr int PIECES = OB ? 2 : 4;           // 16-byte pieces of 64 columns of a row that a lane has
   __shared__ __attribute__((aligned(16))) unsigned char smem[NK ? CB * PITCH : 32 * NC * PITCH];
@@ -948,7 +950,7 @@ hipError_t launch_lora_down(const LoraParams& p, bool nk, hipStream_t stream) {
 template <int NC, bool NK, bool OB>
 static hipError_t up_launch(const LoraParams& p, int num_cus, hipStream_t stream) {
   // 256 rows to a workgroup read the weights least often; 64 where there would be few workgroups
-  const int64_t across = (p.cols + up_columns<NC>() - 1) / up_columns<NC>();
+  const int64_t across = (p.cols + up_columns<NC, OB>() - 1) / up_columns<NC, OB>();
   if (across * ((p.rows + 255) / 256) >= 2 * num_cus)
     return launch_kernel(lora_up_kernel<4, NC, NK, OB>, dim3((unsigned)across, (unsigned)((p.rows + 255) / 256)), dim3(256), 0, stream, p);
   return launch_kernel(lora_up_kernel<1, NC, NK, OB>, dim3((unsigned)across, (unsigned)((p.rows + 63) / 64)), dim3(256), 0, stream, p);
@@ -970,14 +972,15 @@ hipError_t launch_lora_up(const LoraParams& p, bool nk, bool bf16, int num_cus, 
 
 int lora_wgrad_splits(int64_t rows, int64_t cols, int rank, int adapters, int num_cus) {
   if (adapters > kGradAdapters) return 1;
-  // parts of the rows, so that the workgroups of one adapter that has them all fill the chip twice; each of 8
-  // chunks at least.  Their sums are written and read back: 16 MB at most.  (2^31: one launch.)
+  // parts of the rows, so that the workgroups of one adapter that has them all fill the chip twice; each of 4
+  // chunks at least (8 where there are few: a sum takes longer than 8 chunks).  Their sums are written and read back: 16 MB at most.  (2^31: one launch.)
   const int fr = cols < 8 ? 1 : rank <= 64 ? (rank + 15) / 16 : 4;
   const int64_t groups = (cols + kGradColumns - 1) / kGradColumns * ((rank + 16 * fr - 1) / (16 * fr));
   const int64_t chunks = (rows + 31) / 32, each = cols * rank;
   if (each < 1 || groups * (adapters + 32) > (int64_t)1 << 22) return 1;
   int64_t splits = 3 * (int64_t)num_cus / groups;
-  if (splits > chunks / 8) splits = chunks / 8;
+  const int64_t most = chunks >= 32 ? chunks / 4 : chunks / 8;
+  if (splits > most) splits = most;
   if (splits > 32) splits = 32;
   if (splits > ((int64_t)4 << 20) / each) splits = ((int64_t)4 << 20) / each;
   return splits < 2 ? 1 : (int)splits;
