@@ -60,8 +60,9 @@ def same(got, want):
 SHAPES = [(1, 1, 1, 1), (1, 4096, 16, 3), (5, 33, 7, 2), (16, 64, 16, 16), (32, 1000, 16, 8), (17, 130, 33, 4), (100, 70, 64, 1),
           (64, 65, 12, 5), (333, 257, 100, 3), (70, 515, 128, 2), (40, 96, 256, 3), (1000, 300, 8, 6), (2049, 640, 24, 9)]
 # (too large to be taken row by row)
-SHAPES += [(2100, 1030, 16, 5), (1100, 1100, 31, 9), (1000, 900, 40, 2), (530, 1000, 64, 3), (700, 515, 100, 2), (530, 600, 128, 3),
-           (300, 520, 256, 4), (4200, 1030, 8, 6), (9000, 64, 64, 3)]
+TILES = [(5000, 1030, 16, 5), (2500, 1030, 31, 9), (2100, 1100, 40, 2), (1300, 1000, 64, 3), (1500, 515, 100, 2), (1000, 600, 128, 3),
+         (600, 520, 256, 4), (9700, 1030, 8, 6), (20000, 64, 64, 3), (8000, 800, 12, 3), (250, 2200, 256, 3)]
+SHAPES += TILES
 
 
 @pytest.mark.parametrize("rows,cols,rank,adapters", SHAPES)
