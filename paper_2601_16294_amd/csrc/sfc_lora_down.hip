@@ -98,10 +98,13 @@ __global__ __launch_bounds__(256) void lora_down_sum(LoraParams p) {
 
 int lora_down_splits(int64_t rows, int64_t cols, int rank, int num_cus) {
   if (lora_by_rows(rows, cols, rank)) return 1;
-  // two workgroups to a CU, and 8 stages of K at least for each
+  // a workgroup to a CU, or 4 ranges while that is two to a CU at most, each of 4 stages at least (us with 1 / 2 / 4 / 8
+  // ranges of K = 4096: 4096 rows, rank 64 35 / 25 / 20 / 28; 8192, rank 16, K x rank 31 / 24 / 22 / 31; 16384, rank 64 38 /
+  // 44 / 52 / 69)
   const int64_t tiles = (rows + kTile - 1) / kTile * ((rank + kTile - 1) / kTile), stages = (cols + 63) / 64;
-  int64_t splits = 2 * (int64_t)num_cus / tiles;
-  if (splits > stages / 8) splits = stages / 8;
+  int64_t splits = num_cus / tiles > 4 ? num_cus / tiles : 4;
+  if (splits > 2 * num_cus / tiles) splits = 2 * num_cus / tiles;
+  if (splits > stages / 4) splits = stages / 4;
   return splits < 1 ? 1 : splits > 16 ? 16 : (int)splits;
 }
 
