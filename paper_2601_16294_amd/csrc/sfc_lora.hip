@@ -978,13 +978,15 @@ hipError_t launch_lora_up(const LoraParams& p, bool nk, bool bf16, int num_cus, 
 
 int lora_wgrad_splits(int64_t rows, int64_t cols, int rank, int adapters, int num_cus) {
   if (adapters > kGradAdapters) return 1;
-  // parts of the rows, so that the workgroups of one adapter that has them all fill the chip twice; each of 4
-  // chunks at least (8 where there are few: a sum takes longer than 8 chunks).  Their sums are written and read back: 16 MB at most.  (2^31: one launch.)
+  // parts of the rows, so that all workgroups, two to a CU, are in flight at once; each of 4 chunks at least (8
+  // where there are few: a sum takes longer than 8 chunks).  Their sums are written and read back: 16 MB at
+  // most.  (2^22: one launch.)
   const int fr = cols < 8 ? 1 : rank <= 64 ? (rank + 15) / 16 : 4;
   const int64_t groups = (cols + kGradColumns - 1) / kGradColumns * ((rank + 16 * fr - 1) / (16 * fr));
   const int64_t chunks = (rows + 31) / 32, each = cols * rank;
   if (each < 1 || groups * (adapters + 32) > (int64_t)1 << 22) return 1;
-  int64_t splits = 3 * (int64_t)num_cus / groups;
+  int64_t splits = 2 * (int64_t)num_cus / groups - adapters;
+  if (splits < num_cus / groups) splits = num_cus / groups;
   const int64_t most = chunks >= 32 ? chunks / 4 : chunks / 8;
   if (splits > most) splits = most;
   if (splits > 32) splits = 32;
