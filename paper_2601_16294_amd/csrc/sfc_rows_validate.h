@@ -25,7 +25,8 @@ inline Checked check_bf16(const void* p, int64_t rows, int64_t cols, int64_t ld,
 inline Checked check_stack(int64_t rows, int64_t cols, int64_t ld, int64_t count, int64_t stride, const char* overlap_text) {
   if (count < 2) return ok();
   if (stride < 0) return fail(SFC_ERR_INVALID_ARG, "strides must be >= 0");
-  if (stride < (rows - 1) * ld + cols && (stride < cols || ld < (count - 1) * stride + cols))
+  const __int128 matrix = (__int128)(rows - 1) * ld + cols, row = (__int128)(count - 1) * stride + cols;
+  if (stride < matrix && (stride < cols || ld < row))
     return fail(SFC_ERR_INVALID_ARG, overlap_text);
   return ok();
 }
@@ -46,7 +47,7 @@ inline Checked check_moe_gemm(int64_t rows, int64_t N, int64_t K, int experts, i
   SFC_RETURN_IF(check_index(offsets, "offsets is NULL"));
   if (order) SFC_RETURN_IF(check_index(order, "order is NULL"));
   SFC_RETURN_IF(check_bf16(A, order ? a_rows : rows, K, lda, "A is NULL", "lda < K"));
-  if (order && a_rows * lda > kGatherMax)
+  if (order && K > 0 && a_rows * lda > kGatherMax)
     return fail(SFC_ERR_UNSUPPORTED, "rows taken through an order must lie within 2^31 elements");
   const bool nk = b_layout == SFC_B_NK;
   SFC_RETURN_IF(check_bf16(B, nk ? N : K, nk ? K : N, ldb, "B is NULL", "rows of B are longer than ldb"));
