@@ -577,7 +577,8 @@ int sfc_moe_wgrad_ex(int64_t M, int64_t N, int64_t rows, int experts,
  *     Y[t] = base[t] + V[t] * B[a]^T,   V[t] = scales[a] * X[t] * A[a]^T
  * with A[a] of rank x K and B[a] of N x rank, bf16, V fp32; ranks up to 256 (adapters of less are
  * filled up with zeros).  Rows in any order: runs of one adapter's rows (prompts) read its weights
- * least often.  A row sees its own adapter's weights only, so infinities and NaN stay with their adapter.
+ * least often.  A row sees its own adapter's weights only, so infinities and NaN stay with their adapter;
+ * the products with V of an infinite weight or Z are infinite or NaN (V is multiplied as a sum of bf16 terms).
  * The gradients, with U[t] = scales[a] * dY[t] * B[a]: dBase = dY; dX = U[t] * A[a] (added to the shared
  * projection's); dA[a] = sum of U[t]^T X[t], dB[a] = sum of dY[t]^T V[t] over the adapter's rows t; all
  * of them calls below with the weights' other layout.  X, dY and weights at element alignment.

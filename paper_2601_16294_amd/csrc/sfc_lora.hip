@@ -14,7 +14,8 @@
 // itself and reads its adapter's weights (from the L2 where another row has): no order of the rows is
 // slow.  Else a wave takes tiles of 16 rows on MFMAs.  They may belong to up to 16 adapters: it computes with one adapter
 // after the other and keeps the results of that adapter's rows, so no row sees another adapter's
-// weights, infinities and NaN among them.
+// weights, infinities and NaN among them.  (Its own adapter's infinite weight times a term of V that is 0, as the second of 1
+// is, is NaN where the formula has an infinity.)
 #include "sfc_gemm_kernel.h"
 #include "sfc_launch.h"
 #include "sfc_lora_params.h"
@@ -574,9 +575,7 @@ __global__ __launch_bounds__(256, (NC == 1 ? 3 : 2)) void lora_up_kernel(LoraPar
 
 // ---- gradient of the weights -------------------------------------------------------------------
 
-constexpr int kGradWaves = 4, kGradColumns = 64 * kGradWaves;
 constexpr int kGradList = 2048;        // chunks of 32 rows that are looked through at a time
-constexpr int kGradAdapters = 1024;    // most adapters whose rows are dealt out in parts
 
 // Parts of an adapter with `count` of `total` rows: `extra` of them are dealt out over all adapters by their
 // rows; less than two are one, which needs no sum.
@@ -940,15 +939,6 @@ hipError_t launch_row_up(const LoraParams& p, bool nk, hipStream_t stream) {
 
 }  // namespace
 
-// Whether rows are taken one by one, each reading its adapter's weights (from the L2 for the most part).  That takes
-// the same time in any order of the rows; the tiles are faster where rows come in runs and slower where they do not,
-// which the host does not know (us of up, bf16, one by one / tiles of 8 runs / tiles of 32 adapters at random: 64 rows x
-// 14336, rank 64 15 / 23 / 77; 256 x 14336, rank 16 15 / 7 / 46; 512 x 4096, rank 16 9 / 5 / 43; 2048 x 4096, rank 64 108 /
-// 11 / 94).  Up to 256 rows may be a decode step, a request each; more are taken for prompts.
-bool lora_by_rows(int64_t rows, int64_t cols, int rank) {
-  return rows * rank * cols <= (int64_t)(rows <= 64 ? 256 : rows <= 256 ? 128 : 32) << 20 && rows <= 4096;
-}
-
 hipError_t launch_lora_down(const LoraParams& p, bool nk, hipStream_t stream) {
   return lora_by_rows(p.rows, p.cols, p.rank) ? launch_row_down(p, nk, stream) : launch_lora_down_tiles(p, nk, stream);
 }
@@ -974,24 +964,6 @@ hipError_t launch_lora_up(const LoraParams& p, bool nk, bool bf16, int num_cus, 
   if (lora_by_rows(p.rows, p.cols, p.rank)) return bf16 ? launch_row_up<true>(p, nk, stream) : launch_row_up<false>(p, nk, stream);
   return nk ? (bf16 ? up_rank<true, true>(p, num_cus, stream) : up_rank<true, false>(p, num_cus, stream))
             : (bf16 ? up_rank<false, true>(p, num_cus, stream) : up_rank<false, false>(p, num_cus, stream));
-}
-
-int lora_wgrad_splits(int64_t rows, int64_t cols, int rank, int adapters, int num_cus) {
-  if (adapters > kGradAdapters) return 1;
-  // parts of the rows, so that all workgroups, two to a CU, are in flight at once; each of 4 chunks at least (8
-  // where there are few: a sum takes longer than 8 chunks).  Their sums are written and read back: 16 MB at
-  // most.  (2^22: one launch.)
-  const int fr = cols < 8 ? 1 : rank <= 64 ? (rank + 15) / 16 : 4;
-  const int64_t groups = (cols + kGradColumns - 1) / kGradColumns * ((rank + 16 * fr - 1) / (16 * fr));
-  const int64_t chunks = (rows + 31) / 32, each = cols * rank;
-  if (each < 1 || groups * (adapters + 32) > (int64_t)1 << 22) return 1;
-  int64_t splits = 2 * (int64_t)num_cus / groups - adapters;
-  if (splits < num_cus / groups) splits = num_cus / groups;
-  const int64_t most = chunks >= 32 ? chunks / 4 : chunks / 8;
-  if (splits > most) splits = most;
-  if (splits > 32) splits = 32;
-  if (splits > ((int64_t)4 << 20) / each) splits = ((int64_t)4 << 20) / each;
-  return splits < 2 ? 1 : (int)splits;
 }
 
 template <bool NK, bool OB>

@@ -15,7 +15,7 @@ namespace sfc {
 
 namespace {
 
-constexpr int kTile = 64, kSlots = 4;
+constexpr int kTile = kDownTile, kSlots = 4;
 
 template <bool NK>
 __global__ __launch_bounds__(256, 4) void lora_down_kernel(LoraParams p) {
@@ -95,18 +95,6 @@ __global__ __launch_bounds__(256) void lora_down_sum(LoraParams p) {
 }
 
 }  // namespace
-
-int lora_down_splits(int64_t rows, int64_t cols, int rank, int num_cus) {
-  if (lora_by_rows(rows, cols, rank)) return 1;
-  // a workgroup to a CU, or 4 ranges while that is two to a CU at most, each of 4 stages at least (us with 1 / 2 / 4 / 8
-  // ranges of K = 4096: 4096 rows, rank 64 35 / 25 / 20 / 28; 8192, rank 16, K x rank 31 / 24 / 22 / 31; 16384, rank 64 38 /
-  // 44 / 52 / 69)
-  const int64_t tiles = (rows + kTile - 1) / kTile * ((rank + kTile - 1) / kTile), stages = (cols + 63) / 64;
-  int64_t splits = num_cus / tiles > 4 ? num_cus / tiles : 4;
-  if (splits > 2 * num_cus / tiles) splits = 2 * num_cus / tiles;
-  if (splits > stages / 4) splits = stages / 4;
-  return splits < 1 ? 1 : splits > 16 ? 16 : (int)splits;
-}
 
 hipError_t launch_lora_down_tiles(const LoraParams& p, bool nk, hipStream_t stream) {
   const dim3 grid((unsigned)((p.rows + kTile - 1) / kTile), (unsigned)p.splits, (unsigned)(kSlots * ((p.rank + kTile - 1) / kTile)));

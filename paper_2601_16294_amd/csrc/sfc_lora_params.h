@@ -36,9 +36,51 @@ struct LoraParams {
   int32_t* parts;
   int64_t all_cols, first_col;
 };
-int lora_wgrad_splits(int64_t rows, int64_t cols, int rank, int adapters, int num_cus);
-bool lora_by_rows(int64_t rows, int64_t cols, int rank);
-int lora_down_splits(int64_t rows, int64_t cols, int rank, int num_cus);
+constexpr int kDownTile = 64;                            // rows and ranks of a tile of down
+constexpr int kGradWaves = 4, kGradColumns = 64 * kGradWaves;
+constexpr int kGradAdapters = 1024;                      // most adapters whose rows are dealt out in parts
+
+// Whether rows are taken one by one, each reading its adapter's weights (from the L2 for the most part).  That takes
+// the same time in any order of the rows; the tiles are faster where rows come in runs and slower where they do not,
+// which the host does not know (us of up, bf16, one by one / tiles of 8 runs / tiles of 32 adapters at random: 64 rows x
+// 14336, rank 64 15 / 23 / 77; 256 x 14336, rank 16 15 / 7 / 46; 512 x 4096, rank 16 9 / 5 / 43; 2048 x 4096, rank 64 108 /
+// 11 / 94).  Up to 256 rows may be a decode step, a request each; more are taken for prompts.
+inline bool lora_by_rows(int64_t rows, int64_t cols, int rank) {
+  return rows <= 4096 && rows * rank * cols <= (int64_t)(rows <= 64 ? 256 : rows <= 256 ? 128 : 32) << 20;
+}
+
+// Ranges of K in the tiles of down.
+inline int lora_down_splits(int64_t rows, int64_t cols, int rank, int num_cus) {
+  if (lora_by_rows(rows, cols, rank)) return 1;
+  // a workgroup to a CU, or 4 ranges while that is two to a CU at most, each of 4 stages at least (us with 1 / 2 / 4 / 8
+  // ranges of K = 4096: 4096 rows, rank 64 35 / 25 / 20 / 28; 8192, rank 16, K x rank 31 / 24 / 22 / 31; 16384, rank 64 38 /
+  // 44 / 52 / 69)
+  const int64_t tiles = (rows + kDownTile - 1) / kDownTile * ((rank + kDownTile - 1) / kDownTile), stages = (cols + 63) / 64;
+  int64_t splits = num_cus / tiles > 4 ? num_cus / tiles : 4;
+  if (splits > 2 * num_cus / tiles) splits = 2 * num_cus / tiles;
+  if (splits > stages / 4) splits = stages / 4;
+  return splits < 1 ? 1 : splits > 16 ? 16 : (int)splits;
+}
+
+// Parts of the rows that the weight gradient deals out over the adapters.
+inline int lora_wgrad_splits(int64_t rows, int64_t cols, int rank, int adapters, int num_cus) {
+  if (adapters > kGradAdapters) return 1;
+  // parts of the rows, so that all workgroups, two to a CU, are in flight at once; each of 4 chunks at least (8
+  // where there are few: a sum takes longer than 8 chunks).  Their sums are written and read back: 16 MB at
+  // most.  (2^22: one launch.)
+  const int fr = cols < 8 ? 1 : rank <= 64 ? (rank + 15) / 16 : 4;
+  const int64_t groups = (cols + kGradColumns - 1) / kGradColumns * ((rank + 16 * fr - 1) / (16 * fr));
+  const int64_t chunks = (rows + 31) / 32, each = cols * rank;
+  if (each < 1 || groups * (adapters + 32) > (int64_t)1 << 22) return 1;
+  int64_t splits = 2 * (int64_t)num_cus / groups - adapters;
+  if (splits < num_cus / groups) splits = num_cus / groups;
+  const int64_t most = chunks >= 32 ? chunks / 4 : chunks / 8;
+  if (splits > most) splits = most;
+  if (splits > 32) splits = 32;
+  if (splits > ((int64_t)4 << 20) / each) splits = ((int64_t)4 << 20) / each;
+  return splits < 2 ? 1 : (int)splits;
+}
+
 hipError_t launch_lora_down(const LoraParams& p, bool nk, hipStream_t stream);
 hipError_t launch_lora_down_tiles(const LoraParams& p, bool nk, hipStream_t stream);
 hipError_t launch_lora_up(const LoraParams& p, bool nk, bool bf16, int num_cus, hipStream_t stream);

@@ -11,13 +11,21 @@ EXPERTS = [
     ([20, 30, 33], 70, 4129), ([70, 200, 0, 129], 200, 63), ([128, 128, 256], 257, 512), ([1, 2] * 32, 601, 288),
     ([0, 0, 0, 0], 70, 64), ([5, 300], 5, 200), ([9, 130], 3, 7), ([0, 2000, 1], 4096, 129), ([3, 2], 130, 0),
     ([1000, 3, 0, 1500], 7000, 1032), ([700, 0, 1111, 1256, 257, 1000, 511, 768], 4100, 1031), ([4096], 4096, 264),
+    ([3000, 5000], 8200, 70),
+]
+
+# (rows of every expert, N, K) with rows of 16-byte pieces: the kernels that stream the weights
+FEW = [
+    ([1], 1, 8), ([0, 3, 0, 8], 130, 264), ([1, 0, 16, 17, 5, 1, 0, 0], 600, 520), ([8] * 3, 100, 4104), ([24], 333, 1096), ([20], 32, 40),
+    ([32], 1000, 2056), ([33], 95, 4096), ([40, 0, 24], 257, 512), ([64], 4096, 1544), ([1, 50], 64, 64), ([0, 0], 40, 64),
 ]
 
 # (rows of every expert, M, N)
 DEPTHS = [
     ([1], 1, 1), ([32], 16, 16), ([0, 0, 64, 1, 31], 130, 70), ([33, 127, 2000], 200, 300), ([96, 0, 704, 200], 129, 257),
     ([4096], 100, 60), ([3, 66, 129], 5, 3), ([200, 7], 1, 9), ([65, 64, 63, 0, 1], 256, 256), ([0, 0], 33, 20),
-    ([300, 1, 0, 411], 2040, 2047), ([1000, 640], 4096, 1600),
+    ([300, 1, 0, 411], 2040, 2047), ([1000, 640], 4096, 1600), ([200, 100], 3100, 3000),
+    ([1500, 1100], 5000, 3403),
 ]
 
 

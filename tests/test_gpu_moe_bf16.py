@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 import torch
 
-from rows_cases import BF16, DEPTHS, EXPERTS, F32, close, framed, normals, offsets_of, small_ints, untouched_outside
+from rows_cases import BF16, DEPTHS, EXPERTS, F32, FEW, close, framed, normals, offsets_of, small_ints, untouched_outside
 
 pytestmark = pytest.mark.gpu
 
@@ -71,6 +71,29 @@ def test_product_of_rows_through_an_order(so, counts, N, K, nk, topk):
     a = torch.cat([x, torch.zeros((1, K), dtype=BF16, device="cuda")])[src]
     assert same(c, product(a, b, counts, nk))
     assert untouched_outside(c)
+
+
+@pytest.mark.parametrize("counts,N,K", FEW)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("topk", [0, 2])
+def test_few_rows(so, counts, N, K, dtype, topk):
+    """Operands of 16-byte pieces, a row behind the last segment, through an order (topk > 0) or not."""
+    rows, E, tokens = sum(counts), len(counts), 19
+    b = small_ints((E, N, K), 7, 8, 0, gap=16)
+    c = framed((rows + 1, N), dtype, 3, 1)
+    if topk:
+        x = small_ints((tokens, K), 8, 16)
+        rng = np.random.default_rng(rows + N)
+        order = rng.integers(-1, tokens * topk + 2, rows + 1).astype(np.int32)
+        src = torch.from_numpy(np.where((order >= 0) & (order // topk < tokens), order // topk, tokens).astype(np.int64)).cuda()
+        a = torch.cat([x, torch.zeros((1, K), dtype=BF16, device="cuda")])[src]
+        so.sfc_moe_gemm_ex(x, b, offsets_of(counts), c, order=torch.from_numpy(order).cuda(), topk=topk)
+    else:
+        a = small_ints((rows + 1, K), 8, 16)
+        so.sfc_moe_gemm_ex(a, b, offsets_of(counts), c)
+    if rows:
+        assert same(c[:rows], product(a, b, counts, True))
+    assert (c[rows:] == 0).all() and untouched_outside(c)
 
 
 @pytest.mark.parametrize("counts,M,N", DEPTHS)
