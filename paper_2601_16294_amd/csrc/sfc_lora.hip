@@ -361,6 +361,19 @@ __global__ __launch_bounds__(256) void lora_row_up_kn(LoraParams p) {
 
 // ---- up, in tiles --------------------------------------------------------------------------------
 
+// The first n of 8 bf16 elements, to a whole word's address.
+__device__ __forceinline__ void store_words(char* to, const row_u32x4& v, int n) {
+  typedef row_u32x4 word_u32x4 __attribute__((aligned(4)));
+  typedef uint32_t word_u32x2 __attribute__((ext_vector_type(2), aligned(4)));
+  if (n >= 8) {
+    *reinterpret_cast<word_u32x4*>(to) = v;
+  } else if (n > 0) {
+    if (n & 4) *reinterpret_cast<word_u32x2*>(to) = word_u32x2{v[0], v[1]};
+    if (n & 2) *reinterpret_cast<uint32_t*>(to + 2 * (n & 4)) = n & 4 ? v[2] : v[0];
+    if (n & 1) *reinterpret_cast<uint16_t*>(to + 2 * (n & 6)) = (uint16_t)(n & 4 ? (n & 2 ? v[3] : v[2]) : n & 2 ? v[1] : v[0]);
+  }
+}
+
 // Ranks in NC chunks of 32; columns of a workgroup.  Wide blocks read V least often, narrow ones take fewer
 // registers (us at 64 / 128 / 256 columns: bf16 4096x14336 rank 64 74 / 65 / 61, 8192x4096 rank 16 28 / 25 / 27, fp32
 // 1003x5003 rank 12 17 / 14 / 26).
@@ -390,6 +403,8 @@ __global__ __launch_bounds__(256, (NC == 1 ? 3 : 2)) void lora_up_kernel(LoraPar
   const uint32_t lds0 = lds_addr(smem);
   const bool inside = n0 + CB <= p.cols;       // the block lies inside the columns
   const bool whole = inside && p.rank % 8 == 0;
+  // rows of bf16 that start inside a word (16 bytes a lane at odd elements: 2001 rows x 4097, rank 40 24 us, 19 from the next word on)
+  const bool odd = OB && ((reinterpret_cast<uint64_t>(p.Y) | (uint64_t)(p.ldy * 2)) & 2);
   int id[Q];
   uint64_t pending[Q], none[Q];
 #pragma unroll
@@ -480,17 +495,45 @@ __global__ __launch_bounds__(256, (NC == 1 ? 3 : 2)) void lora_up_kernel(LoraPar
 #pragma unroll
           for (int e = 0; e < 4; ++e) y[j][e] += acc[j][e];
       }
+      Raw8<true> results[PIECES];
+#pragma unroll
+      for (int q = 0; q < PIECES; ++q) {
+        if constexpr (OB) {
+          const f32x4 lo = y[2 * q], hi = y[2 * q + 1];
+          results[q].w[0] = row_u32x4{bf16_pair(lo[0], lo[1]), bf16_pair(lo[2], lo[3]), bf16_pair(hi[0], hi[1]), bf16_pair(hi[2], hi[3])};
+        } else {
+          results[q].w[0] = __builtin_bit_cast(row_u32x4, y[q]);
+        }
+      }
+      if constexpr (OB) {
+        if (odd) {
+          // from the next word on: elements 1 .. 7 and the next lane's first; the unit's first element alone
+          const int first = (int)(reinterpret_cast<uint64_t>(out) >> 1) & 1;
+          const uint32_t w0 = results[0].w[0][0], w1 = results[1].w[0][0];
+          const uint32_t next[2] = {(uint32_t)__shfl((int)(g == 0 ? w1 : w0), (lane + 16) & 63),
+                                    (uint32_t)__shfl((int)w1, (lane + 16) & 63)};
+          if (!mine) return;
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const int at = 64 * u + APART * q, most = q == 1 && g == 3 ? 8 : 9;
+            const int end = in ? most : left - at < most ? left - at : most;
+            u32x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t w = results[q].w[0][e], up = e < 3 ? results[q].w[0][e + 1] : next[q];
+              o[e] = first ? w >> 16 | up << 16 : w;
+            }
+            store_words(out + 2 * (at + first), o, end - first);
+            if (first && q == 0 && g == 0 && end > 0) *reinterpret_cast<uint16_t*>(out + 2 * at) = (uint16_t)w0;
+          }
+          return;
+        }
+      }
       if (mine) {
 #pragma unroll
         for (int q = 0; q < PIECES; ++q) {
           const int at = 64 * u + APART * q;
-          Raw8<true> o;
-          if constexpr (OB) {
-            const f32x4 lo = y[2 * q], hi = y[2 * q + 1];
-            o.w[0] = row_u32x4{bf16_pair(lo[0], lo[1]), bf16_pair(lo[2], lo[3]), bf16_pair(hi[0], hi[1]), bf16_pair(hi[2], hi[3])};
-          } else {
-            o.w[0] = __builtin_bit_cast(row_u32x4, y[q]);
-          }
+          const Raw8<true>& o = results[q];
           if constexpr (in) store16<false>(out + at * ES, o.w[0]);
           else if constexpr (OB) store8<true, false>(out, at, left, o);
           else

@@ -23,8 +23,15 @@ const uint16_t* bf16(const void* p) { return static_cast<const uint16_t*>(p); }
 
 int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 
-// Whether a C of so many elements goes past the caches: from 32 MB on, as for the 4-bit products.
-bool past_caches(int64_t elements, int out_type) { return elements * sfc::type_size(out_type) >= (int64_t)32 << 20; }
+// Whether a C of so many elements goes past the caches: from 32 MB on, as for the 4-bit products.  Not where parts of lines are
+// stored and the depth of `stages` is soon computed, so that stores bound the call (weight gradients in fp32, us past the
+// caches / through them: 60 experts 1407x2047 from 17 rows each 286 / 205, 16 experts 1001x1503 from 250 45 / 36, 4 experts
+// 2001x4001 from 1000 89 / 80, but 8 experts 4095x4095 from 2048 602 / 633; products of 8000 rows x 4094, K = 1000 86 / 79,
+// K = 2046 135 / 155).
+bool past_caches(int64_t elements, int out_type, const void* C, int64_t ldc, int64_t stages) {
+  const int64_t size = sfc::type_size(out_type);
+  return elements * size >= (int64_t)32 << 20 && (stages > 16 || ((uintptr_t)C | (uintptr_t)(ldc * size)) % 16 == 0);
+}
 
 // Microseconds of `tasks` blocks of b x b over `stages` 64-deep stages on the tile kernels, fitted to timings of
 // random operands (rows from 2 to 16384 over 1 to 64 experts, sides 512 to 14336, weight gradients too;
@@ -124,7 +131,7 @@ int sfc_moe_gemm_ex(int64_t rows, int64_t N, int64_t K, int experts, const void*
   const int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
   sfc::MoeGemmParams p = {rows, N, K, bf16(A), lda, order, a_rows, order ? topk : 1, bf16(B), ldb, stride_b, C, ldc, 0,
-                          offsets, experts, nullptr, 0, 0, past_caches(rows * N, out_type)};
+                          offsets, experts, nullptr, 0, 0, past_caches(rows * N, out_type, C, ldc, sfc::ceil_div(K, 64))};
   const bool ob = out_type == SFC_OUT_BF16;
   const bool aligned = ((uintptr_t)A | (uintptr_t)B) % 16 == 0 && (lda | ldb | stride_b) % 8 == 0;
   const int fm = b_layout == SFC_B_NK ? moe_few_rows(rows, N, experts, aligned, cus) : 0;
@@ -155,7 +162,7 @@ int sfc_moe_wgrad_ex(int64_t M, int64_t N, int64_t rows, int experts, const void
   int rc = sfc::host_num_cus(&cus);
   if (rc != SFC_OK) return rc;
   sfc::MoeGemmParams p = {M, N, rows, bf16(A), lda, nullptr, 0, 1, bf16(B), ldb, 0, C, ldc, stride_c,
-                          offsets, experts, nullptr, 0, 0, past_caches(M * N * experts, out_type)};
+                          offsets, experts, nullptr, 0, 0, past_caches(M * N * experts, out_type, C, ldc, sfc::ceil_div(rows, 64 * (int64_t)experts))};
   const bool ob = out_type == SFC_OUT_BF16;
   auto tasks = [&](int b) { return (double)(sfc::ceil_div(M, b) * sfc::ceil_div(N, b)) * experts; };
   const int b = moe_block_of(tasks, (double)sfc::ceil_div(rows > 0 ? rows : 1, 64 * (int64_t)experts), !ob, cus);

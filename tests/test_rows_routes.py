@@ -138,17 +138,23 @@ def test_the_gpu_tests_reach_every_kernel(exe):
     assert {(64, False, "none"), (128, True, "quarters"), (256, True, "quarters"), (256, False, "none")} <= deep_ends
 
 
+def past(elements, ld, depth, out):
+    """Whether a result goes past the caches: 32 MB and more, in whole 16-byte pieces of rows or behind a long depth."""
+    size = 4 - 2 * out
+    return elements * size >= 32 << 20 and (ld * size % 16 == 0 or -(-depth // 64) > 16)
+
+
 @pytest.mark.parametrize("out", [0, 1])
-@pytest.mark.parametrize("rows,N,K,experts", [(1, 5, 9, 1), (300, 700, 64, 1024), (5000, 4100, 512, 8), (1 << 20, 14336, 4096, 8)])
+@pytest.mark.parametrize("rows,N,K,experts", [(5000, 4097, 1024, 8), (5000, 4097, 1025, 8), (1, 5, 9, 1), (300, 700, 64, 1024), (5000, 4100, 512, 8), (1 << 20, 14336, 4096, 8)])
 def test_experts_grid(exe, rows, N, K, experts, out):
     for layout in (0, 1):
         (name, e), = launches(one(exe, "experts", rows, N, K, experts, layout, out))
         if name == "tile":
-            assert e["layout"] == layout and e["bf16"] == out and e["gn"] == -(-N // e["b"]) and e["past"] == (rows * N * (4 - 2 * out) >= 32 << 20)
+            assert e["layout"] == layout and e["bf16"] == out and e["gn"] == -(-N // e["b"]) and e["past"] == past(rows * N, N, K, out)
             assert 1 <= e["grid"] <= 256 * {256: 1, 128: 2, 64: 4}[e["b"]]
     (_, e), = launches(one(exe, "depth", rows, N, K, experts, 0, out))
     assert e["layout"] == 2 and e["table"] and e["gm"] == -(-N // e["b"]) and e["gn"] == -(-K // e["b"])
-    assert 1 <= e["grid"] <= min(e["gm"] * e["gn"] * experts, 1024)
+    assert 1 <= e["grid"] <= min(e["gm"] * e["gn"] * experts, 1024) and e["past"] == past(N * K * experts, K, -(-rows // experts), out)
 
 
 def test_experts_without_work_take_no_launch(exe):
