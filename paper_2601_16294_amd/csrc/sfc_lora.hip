@@ -10,6 +10,9 @@
 // leave, the last one rounded: two are off by at most 2^-16 of it (bf16 results, which are rounded to 2^-8),
 // three hold every bit of it (fp32 results).
 //
+// Measured: up of 4096 rows x 14336, rank 64 58 us = 4.2 TB/s, of 8192 x 4096, rank 16 27 us = 5 TB/s; 32 rows x 4096 of 16
+// adapters, rank 16, 3.7 us down and 3.7 up, a launch and a chain of loads each.
+//
 // Two forms of down and up.  Where rows x rank x columns is small, as in decode steps, every row is taken by
 // itself and reads its adapter's weights (from the L2 where another row has): no order of the rows is
 // slow.  Else a wave takes tiles of 16 rows on MFMAs.  They may belong to up to 16 adapters: it computes with one adapter
@@ -387,9 +390,9 @@ __device__ __forceinline__ int up_column(int j, int n) {
   return OB ? 32 * (j >> 1) + 8 * (n >> 2) + 4 * (j & 1) + (n & 3) : 16 * j + n;
 }
 
-// A workgroup takes 64 Q rows, Q tiles for each of its 4 waves, and a block of columns, one adapter after the other: the block's weights of that
-// adapter go into LDS, and the waves take the tiles that hold rows of it, of which they load and store
-// these rows alone.  A last turn copies the rows of no adapter.  Column blocks run fastest over the
+// A workgroup takes 64 Q rows, Q tiles for each of its 4 waves, and a block of columns, one adapter after the other:
+// the block's weights of that adapter go into LDS, and the waves take the tiles that hold rows of it, of which they load and
+// store these rows alone.  A last turn copies the rows of no adapter.  Column blocks run fastest over the
 // workgroups: those in flight cover whole rows.
 template <int Q, int NC, bool NK, bool OB>
 __global__ __launch_bounds__(256, (NC == 1 ? 3 : 2)) void lora_up_kernel(LoraParams p) {
@@ -642,7 +645,9 @@ __device__ __forceinline__ void store4(float* to, const f32x4& v, int64_t inside
 // rows keeps the chip busy too; the workgroup then lists the chunks of 32 rows that hold rows of its
 // adapter and takes its part of the list.  A chunk's V is taken apart once for all waves; chunks lie in one of two
 // slots of LDS, the next one written while one is computed with, three more on their way.  In a
-// chunk, rows of other adapters are zeros in both operands.
+// chunk, rows of other adapters are zeros in both operands.  Bound: one read of Z for every 64 ranks, 13 us for 8192
+// rows x 4096, rank 16; with 4 adapters it takes 26 and the sum 4: the pass over the ids, the list and the first loads come before
+// a workgroup's 8 chunks (2001 rows x 4097, rank 40, 4 chunks each: 19).
 // NARROW: rows of Z or V of fewer than 8 elements, which are loaded one by one.
 template <int FR, bool NARROW, bool NK, bool OB>
 __global__ __launch_bounds__(kGradWaves * 64) void lora_wgrad_kernel(LoraParams p) {

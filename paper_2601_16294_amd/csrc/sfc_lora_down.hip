@@ -6,7 +6,8 @@
 // rows.  A rank of 16 or 64 is one block of columns, so without a split of K there would be 64
 // workgroups for 4096 rows: the sums of the ranges of K go to memory, and a second kernel adds them up in
 // order, scales them and clears rows of no adapter.  (Rows of one adapter leave the other slots
-// nothing to do; a tile where two meet takes no longer, for they run beside each other.)
+// nothing to do; a tile where two meet takes no longer, for they run beside each other.)  Bound: one read of X for every 64
+// ranks: 6.5 us for 4096 rows x 4096, where rank 64 takes 20: 16 stages, the sums' way through memory and a second launch, 4.
 #include "sfc_launch.h"
 #include "sfc_lora_params.h"
 #include "sfc_moe_gemm_kernel.h"

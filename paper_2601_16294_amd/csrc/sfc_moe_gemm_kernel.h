@@ -22,6 +22,14 @@
 //     where no row follows;
 //   * the MFMA takes B first, so a lane ends with one row of C and runs of 4 columns; the block
 //     leaves through LDS, a wave's 16-row strips at a time, as whole row segments.
+//
+// Bound: the MFMAs' rate, for segments long enough to fill blocks.  One segment of 8192^3, normal values: 1390 to 1425
+// TFLOP/s for kMoeNK and kMoeKN, 1330 for kMoeTN, with the MFMAs busy in 63, 60 and 58 % of the cycles at 2.16 GHz, no
+// bank conflicts, waves waiting in a fifth of the cycles (other places of the barrier and of the loads: within 1.5 %).
+// Stores take 5 to 6 % of a product, up to a fifth of a weight gradient in fp32.  4096 tokens, 2 of 8 experts
+// 14336x4096: 852 us = 1129 TFLOP/s, 12 % more with the empty rows of last blocks.  256x256 blocks read each
+// operand least often; 128x128 and 64x64, two and four workgroups to a CU, fill the chip where there are few rows or
+// columns: moe_tile_us() of the host layer estimates which takes least.
 #pragma once
 #include "sfc_gemm_kernel.h"
 #include "sfc_moe_params.h"
@@ -427,8 +435,8 @@ __global__ __launch_bounds__(256, (MoeTile<BM, BN>::PER_CU)) void moe_gemm_kerne
   constexpr int ES = OB ? 2 : 4;
   // Calls block(task) for this workgroup's tasks: its rank of every full round, and in the last, partial one its
   // rank among as many workgroups as there are tasks left (the first ones: spread over all chiplets).  A last round
-  // that is at most half full is taken in quarters of blocks, quarter(task, q): 256x256 blocks of 64 stages, 1088
-  // on 256 CUs, XX us instead of XX.
+  // that is at most half full is taken in quarters of blocks, quarter(task, q): 1088 blocks of 256x256 and 64 stages on
+  // 256 CUs take 473 us instead of 495.
   constexpr bool QUARTERS = BM > 64;
   auto each_task = [&](int64_t total, auto block, auto quarter) {
     const int64_t full = total / P * P;

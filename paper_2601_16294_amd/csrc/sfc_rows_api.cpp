@@ -23,14 +23,15 @@ const uint16_t* bf16(const void* p) { return static_cast<const uint16_t*>(p); }
 
 int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 
-// Whether a C of so many elements goes past the caches: from 32 MB on, as for the 4-bit products.  Not where parts of lines are
-// stored and the depth of `stages` is soon computed, so that stores bound the call (weight gradients in fp32, us past the
-// caches / through them: 60 experts 1407x2047 from 17 rows each 286 / 205, 16 experts 1001x1503 from 250 45 / 36, 4 experts
-// 2001x4001 from 1000 89 / 80, but 8 experts 4095x4095 from 2048 602 / 633; products of 8000 rows x 4094, K = 1000 86 / 79,
-// K = 2046 135 / 155).
+// Whether a C of so many elements goes past the caches: from 32 MB on, as for the 4-bit products.  Not the largest whose
+// rows are stored in parts of lines where the depth of `stages` is soon computed, so that stores bound the call (us past
+// the caches / through them, results in rotation: weight gradients in fp32 of 60 experts 1407x2047, 17 rows each, 691 MB 284 / 203,
+// of 64 experts 1999x999, 64 rows, 511 MB 195 / 181, 1001x1503, 250 rows, 385 MB 163 / 156, but of 16 experts, 96 MB 48 / 53,
+// and of 8 experts 4095x4095, 2048 rows, 537 MB 602 / 633).
 bool past_caches(int64_t elements, int out_type, const void* C, int64_t ldc, int64_t stages) {
-  const int64_t size = sfc::type_size(out_type);
-  return elements * size >= (int64_t)32 << 20 && (stages > 16 || ((uintptr_t)C | (uintptr_t)(ldc * size)) % 16 == 0);
+  const int64_t size = sfc::type_size(out_type), bytes = elements * size;
+  const bool whole = ((uintptr_t)C | (uintptr_t)(ldc * size)) % 16 == 0;
+  return bytes >= (int64_t)32 << 20 && (whole || stages > 16 || bytes < (int64_t)256 << 20);
 }
 
 // Microseconds of `tasks` blocks of b x b over `stages` 64-deep stages on the tile kernels, fitted to timings of

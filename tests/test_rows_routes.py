@@ -139,13 +139,13 @@ def test_the_gpu_tests_reach_every_kernel(exe):
 
 
 def past(elements, ld, depth, out):
-    """Whether a result goes past the caches: 32 MB and more, in whole 16-byte pieces of rows or behind a long depth."""
+    """Whether a result goes past the caches: 32 MB and more; 256 and more in whole 16-byte pieces of rows or behind a long depth."""
     size = 4 - 2 * out
-    return elements * size >= 32 << 20 and (ld * size % 16 == 0 or -(-depth // 64) > 16)
+    return elements * size >= 32 << 20 and (ld * size % 16 == 0 or -(-depth // 64) > 16 or elements * size < 256 << 20)
 
 
 @pytest.mark.parametrize("out", [0, 1])
-@pytest.mark.parametrize("rows,N,K,experts", [(5000, 4097, 1024, 8), (5000, 4097, 1025, 8), (1, 5, 9, 1), (300, 700, 64, 1024), (5000, 4100, 512, 8), (1 << 20, 14336, 4096, 8)])
+@pytest.mark.parametrize("rows,N,K,experts", [(5000, 4097, 1024, 8), (33000, 4097, 1024, 8), (33000, 4097, 1025, 8), (1000, 1407, 2047, 60), (1, 5, 9, 1), (300, 700, 64, 1024), (5000, 4100, 512, 8), (1 << 20, 14336, 4096, 8)])
 def test_experts_grid(exe, rows, N, K, experts, out):
     for layout in (0, 1):
         (name, e), = launches(one(exe, "experts", rows, N, K, experts, layout, out))
