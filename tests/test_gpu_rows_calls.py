@@ -346,3 +346,106 @@ def test_gradients_of_experts_against_differences(so, counts):
     for t, grad in ((x, dx), (w, dw)):
         places = [int(i) for i in rng.integers(0, t.numel(), 12)]
         assert differences(loss, t, places, 1.0) == [float(grad.reshape(-1)[i]) for i in places]
+
+
+# ---- calls that the documents allow and that are rare --------------------------------------------
+
+
+@pytest.mark.parametrize("rows,cols,rank,n", [(30, 77, 9, 3), (4096, 1100, 24, 4), (4096, 1100, 24, 1), (2500, 1031, 33, 9)])
+def test_rows_of_no_adapter(so, rows, cols, rank, n):
+    """None of a batch has one, whatever its V and its weights hold."""
+    nan = lambda *s, dtype=BF16: torch.full(s, float("nan"), dtype=dtype, device="cuda")  # noqa: E731
+    ids = torch.full((rows,), -1, dtype=I32, device="cuda")
+    ids[::3] = n
+    x, v = normals((rows, cols), 1), torch.full((rows, rank), 9.0, device="cuda")
+    so.sfc_lora_down(x, nan(n, rank, cols), ids, v, scales=nan(n, dtype=F32))
+    assert not v.any()
+    for dtype in (F32, BF16):
+        base, y = normals((rows, cols), 2, dtype=dtype), nan(rows, cols, dtype=dtype)
+        so.sfc_lora_up(nan(rows, rank, dtype=F32), nan(n, cols, rank), ids, y, base=base)
+        assert torch.equal(y, base)
+        so.sfc_lora_up(nan(rows, rank, dtype=F32), nan(n, cols, rank), ids, y)
+        assert not y.any()
+    g = nan(n, cols, rank, dtype=F32)
+    so.sfc_lora_wgrad(nan(rows, cols), nan(rows, rank, dtype=F32), ids, g)
+    assert not g.any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols,rank", [(30, 77, 9), (2500, 1031, 33), (5000, 514, 60), (2100, 1100, 40)])
+@pytest.mark.parametrize("layout", [0, 1])
+def test_up_in_place(so, rows, cols, rank, layout, dtype):
+    """The same bits as into other memory, at odd elements too."""
+    n = 3
+    v, ids = normals((rows, rank), 1, dtype=F32), random_ids(rows, n, 5)
+    b = normals((n, cols, rank) if layout == 0 else (n, rank, cols), 2)
+    for pad, shift in ((0, 0), (1, 0), (0, 1), (3, 1), (6, 0)):
+        base = normals((rows, cols), 3, ld_pad=pad, shift=shift, dtype=dtype)
+        y = torch.empty((rows, cols), dtype=dtype, device="cuda")
+        so.sfc_lora_up(v, b, ids, y, base=base, layout=layout)
+        so.sfc_lora_up(v, b, ids, base, base=base, layout=layout)
+        assert torch.equal(base, y)
+
+
+def test_weights_that_all_share(so):
+    """Experts and adapters of one matrix: a stride of 0 in the weights; gradients that would lie on each other are refused."""
+    x, w, off = small_ints((40, 64), 1), small_ints((72, 64), 2), offsets_of([10, 0, 25, 5])
+    y = torch.empty((40, 72), device="cuda")
+    so.sfc_moe_gemm_ex(x, w.expand(4, 72, 64), off, y)
+    assert torch.equal(y.double(), x.double() @ w.double().t())
+    with pytest.raises(so.SfcError, match="overlap"):
+        so.sfc_moe_wgrad_ex(y.to(BF16), x, off, torch.empty((72, 64), device="cuda").expand(4, 72, 64))
+    ids, v = torch.arange(40, dtype=I32, device="cuda") % 3, torch.empty((40, 72), device="cuda")
+    so.sfc_lora_down(x, w.expand(3, 72, 64), ids, v)
+    assert torch.equal(v, y)
+    with pytest.raises(so.SfcError, match="overlap"):
+        so.sfc_lora_wgrad(x, v, ids, torch.empty((64, 72), device="cuda").expand(3, 64, 72))
+
+
+@pytest.mark.parametrize("n,rows,cols,rank", [(1100, 3000, 40, 8), (33_000, 200, 16, 8), (1024, 20_000, 300, 5), (70_000, 50, 9, 3)])
+def test_many_adapters(so, n, rows, cols, rank):
+    """More than are counted in a workgroup, and more than a launch takes."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    ids = torch.randint(-1, n + 1, (rows,), generator=g, device="cuda", dtype=I32)
+    ids[:2], ids[2:4] = 0, n - 1
+    x, a, b = small_ints((rows, cols), 1), small_ints((n, rank, cols), 2), small_ints((n, cols, rank), 3)
+    v, y = torch.empty((rows, rank), device="cuda"), torch.empty((rows, cols), device="cuda")
+    so.sfc_lora_down(x, a, ids, v)
+    so.sfc_lora_up(v, b, ids, y)
+    live = ((ids >= 0) & (ids < n))[:, None]
+    at = ids.long().clamp(0, n - 1)
+    want_v = torch.where(live, torch.bmm(a[at].float(), x.float()[:, :, None])[..., 0], 0.0)
+    assert torch.equal(v, want_v)
+    assert torch.equal(y, torch.where(live, torch.bmm(b[at].float(), want_v[:, :, None])[..., 0], 0.0))
+    u = small_ints((rows, rank), 4).float()
+    for layout in (0, 1):
+        grad = torch.full((n, cols, rank) if layout == 0 else (n, rank, cols), 9.0, device="cuda")
+        so.sfc_lora_wgrad(x, u, ids, grad, layout=layout)
+        want = torch.zeros((n, cols, rank), device="cuda")
+        want.index_add_(0, at, torch.where(live[..., None], x.float()[:, :, None] * u[:, None, :], 0.0))
+        assert torch.equal(grad if layout == 0 else grad.transpose(1, 2), want)
+
+
+def test_most_experts(so):
+    counts = [(i * 7) % 5 for i in range(1024)]
+    rows, N, K = sum(counts), 70, 130
+    x, w, dy = small_ints((rows, K), 1), small_ints((1024, N, K), 2), small_ints((rows, N), 3)
+    off, y, dw = offsets_of(counts), torch.empty((rows, N), device="cuda"), torch.empty((1024, N, K), device="cuda")
+    so.sfc_moe_gemm_ex(x, w, off, y)
+    so.sfc_moe_wgrad_ex(dy, x, off, dw)
+    at = 0
+    for e, n in enumerate(counts):
+        s = slice(at, at + n)
+        assert torch.equal(y[s].double(), x[s].double() @ w[e].double().t()) and torch.equal(dw[e].double(), dy[s].double().t() @ x[s].double())
+        at += n
+
+
+def test_one_expert_with_all_rows(so):
+    """A batch of few rows on average whose router sends all of them to one of many experts."""
+    E, N, K, rows = 64, 200, 264, 500
+    x, w = small_ints((rows, K), 1), small_ints((E, N, K), 2)
+    for e in (0, 17, E - 1):
+        off = torch.tensor([0] * (e + 1) + [rows] * (E - e), dtype=I32, device="cuda")
+        y = torch.empty((rows, N), device="cuda")
+        so.sfc_moe_gemm_ex(x, w, off, y)
+        assert torch.equal(y.double(), x.double() @ w[e].double().t())
