@@ -30,7 +30,7 @@ namespace {
 
 __device__ __forceinline__ bf16x8 as_bf16x8(const row_u32x4& v) { return __builtin_bit_cast(bf16x8, v); }
 
-// 8 elements at p, or (CHECKED) those of a row's from column c on that lie before `cols`, and zeros.
+// 8 elements at p.
 __device__ __forceinline__ row_u32x4 load_any(const uint16_t* p) { return reinterpret_cast<const Any16<2>*>(p)->v; }
 // Element i + n of v as element i, zeros behind.
 __device__ __forceinline__ row_u32x4 moved_down(const row_u32x4& v, int64_t n) {
@@ -39,6 +39,7 @@ __device__ __forceinline__ row_u32x4 moved_down(const row_u32x4& v, int64_t n) {
   const uint64_t low = n >= 8 ? 0 : n >= 4 ? hi >> s : s ? lo >> s | hi << (64 - s) : lo, high = n >= 4 ? 0 : hi >> s;
   return row_u32x4{(uint32_t)low, (uint32_t)(low >> 32), (uint32_t)high, (uint32_t)(high >> 32)};
 }
+// 8 elements of a row from column c on; CHECKED: those that lie before `cols`, and zeros.
 template <bool CHECKED>
 __device__ __forceinline__ row_u32x4 load_part(const uint16_t* row, int64_t c, int64_t cols) {
   if constexpr (!CHECKED) {
@@ -956,6 +957,8 @@ int lanes_for(int rank, int most) {
 
 hipError_t launch_row_down(const LoraParams& p, bool nk, hipStream_t stream) {
   if (nk) {
+    // a rank to a wave while that takes few waves, else 4, which read X once (us, K = 4096, 1 / 4: 16 rows, rank 16 3.7 / 4.9, 128
+    // rows 4.3 / 5.0, 256 rows 5.2 / 5.3, 128 rows, rank 64 7.2 / 6.5)
     const bool one = p.rows * p.rank <= 2048;
     const int64_t jobs = p.rows * (one ? p.rank : (p.rank + 3) / 4);
     return launch_kernel(one ? lora_row_down_nk<1> : lora_row_down_nk<4>, dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, stream, p);
@@ -993,7 +996,8 @@ hipError_t launch_lora_down(const LoraParams& p, bool nk, hipStream_t stream) {
 
 template <int NC, bool NK, bool OB>
 static hipError_t up_launch(const LoraParams& p, int num_cus, hipStream_t stream) {
-  // 256 rows to a workgroup read the weights least often; 64 where there would be few workgroups
+  // 256 rows to a workgroup read the weights least often; 64 where there would be few workgroups (us, bf16, 8 runs, 64 / 256:
+  // 1024 rows x 4096, rank 64 7.7 / 16.5, 2048 11.9 / 17.4, 4096 21.9 / 21.7; 4096 x 14336 57 / 50; 8192 x 4096, rank 16 27 / 25)
   const int64_t across = (p.cols + up_columns<NC, OB>() - 1) / up_columns<NC, OB>();
   if (across * ((p.rows + 255) / 256) >= 2 * num_cus)
     return launch_kernel(lora_up_kernel<4, NC, NK, OB>, dim3((unsigned)across, (unsigned)((p.rows + 255) / 256)), dim3(256), 0, stream, p);
