@@ -1,4 +1,4 @@
-"""Python binding of the 4-bit (MX) and mixture-of-experts operators of libsfcgemm.so.
+"""Python binding of the 4-bit (MX), mixture-of-experts and low-rank adapter operators of libsfcgemm.so.
 
 Argument marshalling and checks only, as in ``sfcgemm``; names follow the C ABI
 (include/sfcgemm.h, where each operator's definition stands).  Outputs are tensors
@@ -12,6 +12,14 @@ rows of codes lie a multiple of 16 bytes apart, rows of scales a multiple of 4.
     xq = mx4_empty(M, K)
     sfc_mx4_quant(x, *xq)
     sfc_gemm_mx4_ex(*xq, *wq, y)            # y = x w^T
+
+Weights that depend on the row are stacked, bfloat16, as a linear layer holds them (SFC_B_NK) or the other way
+round (SFC_B_KN); a gradient reads the same memory with the other layout:
+
+    sfc_moe_gemm_ex(x, w, offsets, y)                       # y[p] = x[p] w[e]^T
+    sfc_moe_gemm_ex(dy, w, offsets, dx, layout=SFC_B_KN)    # dx[p] = dy[p] w[e]
+    sfc_lora_down(x, a, ids, v, scales)                     # v = s x a[id]^T
+    sfc_lora_up(v, b, ids, y, base=y)                       # y += v b[id]^T
 """
 from __future__ import annotations
 
