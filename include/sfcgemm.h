@@ -577,8 +577,8 @@ int sfc_moe_wgrad_ex(int64_t M, int64_t N, int64_t rows, int experts,
  *     Y[t] = base[t] + V[t] * B[a]^T,   V[t] = scales[a] * X[t] * A[a]^T
  * with A[a] of rank x K and B[a] of N x rank, bf16, V fp32; ranks up to 256 (adapters of less are
  * filled up with zeros).  Rows in any order: runs of one adapter's rows (prompts) read its weights
- * least often.  A row sees its own adapter's weights only, so infinities and NaN stay with their adapter;
- * the products with V of an infinite weight or Z are infinite or NaN (V is multiplied as a sum of bf16 terms).
+ * least often.  A row sees its own adapter's weights only, so infinities and NaN stay with their adapter, and are
+ * where the formulas have them, whatever the batch's size.
  * The gradients, with U[t] = scales[a] * dY[t] * B[a]: dBase = dY; dX = U[t] * A[a] (added to the shared
  * projection's); dA[a] = sum of U[t]^T X[t], dB[a] = sum of dY[t]^T V[t] over the adapter's rows t; all
  * of them calls below with the weights' other layout.  X, dY and weights at element alignment.
@@ -600,7 +600,7 @@ int sfc_lora_down(int64_t rows, int64_t K, int64_t rank, int adapters,
 
 /* sfc_lora_up -- Y (rows x N, `type`) as above: B as N x rank (SFC_B_NK) or rank x N (SFC_B_KN); base rows x N
  * of Y's type, NULL: 0, or Y itself; rows of no adapter are base's.  V's products with B are fp32, rounded once
- * with base; bf16 Y: V is taken to 16 bits (2^-16 of it). */
+ * with base; bf16 Y: V may be taken to 16 bits (2^-16 of it), in any case to 2^-134. */
 int sfc_lora_up(int64_t rows, int64_t N, int64_t rank, int adapters,
                 const float *V, int64_t ldv, const void *B, int64_t ldb, int64_t stride_b, int layout,
                 const int32_t *ids, const void *base, int64_t ld_base,

@@ -6,9 +6,9 @@
 //
 // with ranks of a few to a few hundred: X, base and Y are read and written once, and that
 // traffic is what bounds them; the products are small beside it.  V is fp32.  Where it meets bf16 weights in
-// MFMAs it is taken apart into bf16 terms of the same sign, each the leading 8 bits of what the ones before
+// MFMAs it is taken apart into bf16 terms, each the leading 8 bits of what the ones before
 // leave, the last one rounded: two are off by at most 2^-16 of it (bf16 results, which are rounded to 2^-8),
-// three hold every bit of it (fp32 results).
+// three hold every bit of it (fp32 results), down to 2^-134.
 //
 // Measured: up of 4096 rows x 14336, rank 64 58 us = 4.2 TB/s, of 8192 x 4096, rank 16 27 us = 5 TB/s; 32 rows x 4096 of 16
 // adapters, rank 16, 3.7 us down and 3.7 up, a launch and a chain of loads each.
@@ -17,8 +17,11 @@
 // itself and reads its adapter's weights (from the L2 where another row has): no order of the rows is
 // slow.  Else a wave takes tiles of 16 rows on MFMAs.  They may belong to up to 16 adapters: it computes with one adapter
 // after the other and keeps the results of that adapter's rows, so no row sees another adapter's
-// weights, infinities and NaN among them.  (Its own adapter's infinite weight times a term of V that is 0, as the second of 1
-// is, is NaN where the formula has an infinity.)
+// weights, infinities and NaN among them.
+//
+// An infinite weight (in the gradient: Z) times a term of V that is 0, as the second of 1 is, would be NaN where the formula has an
+// infinity.  The first term is 0 only where V is, so up adds up the others by themselves and puts a number in the place of a
+// NaN before the two meet; the gradient forms sums that end as NaN once more, from V as it is.
 #include "sfc_gemm_kernel.h"
 #include "sfc_launch.h"
 #include "sfc_lora_params.h"
@@ -66,48 +69,37 @@ __device__ __forceinline__ int adapter_of(const LoraParams& p, int64_t t) {
   return t < p.rows && a >= 0 && a < p.adapters ? a : -1;
 }
 
-// Leading bf16 terms of 8 fp32 values.  (Upper halves of two words in one: a byte permutation.)
-__device__ __forceinline__ uint32_t upper_halves(float lo, float hi) {
-  return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
-}
-__device__ __forceinline__ float less_upper(float v) {
-  return v - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) & 0xFFFF0000u);
+// bf16 terms of 8 fp32 values.  (Halves of two words in one: a byte permutation.)  The first is the value's leading 8
+// bits, the last of them set where a bit behind them is: so it is 0 only where the value is, a NaN stays one whatever its
+// payload, and what is left is less than its last bit.  An infinity leaves NaN.
+__device__ __forceinline__ uint32_t halves(float lo, float hi, uint32_t which) {
+  return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), which);
 }
 template <int TERMS>
 __device__ __forceinline__ void split_terms(const float (&v)[8], bf16x8 (&out)[TERMS]) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
   u32x4 w[TERMS];
-  float most = 0.f;                            // NaN once one value is, or is infinite
-#pragma unroll
-  for (int i = 0; i < 8; ++i) most = __builtin_fmaf(v[i], 0.f, most);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float lo = v[2 * i], hi = v[2 * i + 1];
+    const u16x2 behind = __builtin_elementwise_min(__builtin_bit_cast(u16x2, halves(lo, hi, 0x05040100u)), u16x2{1, 1});
+    w[0][i] = halves(lo, hi, 0x07060302u) | __builtin_bit_cast(uint32_t, behind);
+    lo -= bf16_low(w[0][i]);
+    hi -= bf16_high(w[0][i]);
 #pragma unroll
-    for (int k = 0; k + 1 < TERMS; ++k) {
-      w[k][i] = upper_halves(lo, hi);
-      lo = less_upper(lo);
-      hi = less_upper(hi);
+    for (int k = 1; k + 1 < TERMS; ++k) {
+      w[k][i] = halves(lo, hi, 0x07060302u);
+      lo -= bf16_low(w[k][i]);
+      hi -= bf16_high(w[k][i]);
     }
     w[TERMS - 1][i] = bf16_pair(lo, hi);
-  }
-  if (__ballot(most != most)) {
-    // an infinity or NaN is its first term alone (a NaN whose payload lies in the lower half has to stay one)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float x = v[2 * i + e];
-        if (__builtin_fabsf(x) < __builtin_inff()) continue;
-        const uint32_t keep = e ? 0x0000FFFFu : 0xFFFF0000u;
-        w[0][i] |= x != x ? 0x40u << (16 * e) : 0u;
-#pragma unroll
-        for (int k = 1; k < TERMS; ++k) w[k][i] &= keep;
-      }
-    }
   }
 #pragma unroll
   for (int k = 0; k < TERMS; ++k) out[k] = __builtin_bit_cast(bf16x8, w[k]);
 }
+
+// v, or the nearest number for an infinity, and some number for NaN.
+__device__ __forceinline__ float number(float v) { return __builtin_amdgcn_fmed3f(v, -__FLT_MAX__, __FLT_MAX__); }
 
 // Ranks r .. r + 7 of a row of V; zeros past the rank (which is at least 1).
 __device__ __forceinline__ void load_ranks(const float* row, int r, int rank, float (&v)[8]) {
@@ -477,22 +469,41 @@ __global__ __launch_bounds__(256, (NC == 1 ? 3 : 2)) void lora_up_kernel(LoraPar
         }
       }
       if constexpr (product) {
-        f32x4 acc[4] = {};
+        // The sums of all terms but the first, made numbers before they meet the first's.  Up to 2 chunks: these come on
+        // top of them, from the same weights in registers.  More would be read from LDS twice (8192x4096, rank 128,
+        // bf16 50 us), so the two sums have registers of their own (45 us).
+        constexpr bool FIRST = NC <= 2;
+        f32x4 acc[4] = {}, low[4] = {};
+        bf16x8 wf[FIRST ? NC : 1][4];
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           if (NC > 2 && 32 * c >= p.rank) break;
-          bf16x8 wf[4];
+          bf16x8 (&w)[4] = wf[FIRST ? c : 0];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             if constexpr (NK)
-              wf[j] = *(lds_bf16x8*)(uintptr_t)(lds0 + (uint32_t)((64 * u + up_column<OB>(j, col)) * PITCH + 64 * c + 16 * g));
+              w[j] = *(lds_bf16x8*)(uintptr_t)(lds0 + (uint32_t)((64 * u + up_column<OB>(j, col)) * PITCH + 64 * c + 16 * g));
             else
-              wf[j] = read_transposed(lds0 + (uint32_t)((32 * c + 8 * g + (col >> 2)) * PITCH + 2 * (64 * u + up_column<OB>(j, 4 * (col & 3)))), PITCH);
+              w[j] = read_transposed(lds0 + (uint32_t)((32 * c + 8 * g + (col >> 2)) * PITCH + 2 * (64 * u + up_column<OB>(j, 4 * (col & 3)))), PITCH);
           }
+          // (fp32 results of more chunks: 16 columns after the other, which takes fewer registers: rank 128 76 us, else 80)
+          constexpr int SOME = FIRST ? TERMS - 1 : TERMS;
 #pragma unroll
-          for (int k2 = 0; k2 < TERMS; ++k2)
+          for (int m = 0; m < 4 * SOME; ++m) {
+            const int j = OB || FIRST ? m % 4 : m / SOME, k2 = TERMS - SOME + (OB || FIRST ? m / 4 : m % SOME);
+            f32x4& to = k2 ? low[j] : acc[j];
+            to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[j], vf[c][k2], to, 0, 0, 0);
+          }
+        }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j], vf[c][k2], acc[j], 0, 0, 0);
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[j][e] = FIRST ? number(low[j][e]) : acc[j][e] + number(low[j][e]);
+        if constexpr (FIRST) {
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[c][j], vf[c][0], acc[j], 0, 0, 0);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -901,6 +912,54 @@ __global__ __launch_bounds__(kGradWaves * 64) void lora_wgrad_kernel(LoraParams 
     __syncthreads();
   }
   if (!live) return;
+  bool nan = false;
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int f = 0; f < FR; ++f)
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) nan |= __builtin_isunordered(acc[c][f][e], acc[c][f][e + 1]);
+  if (__ballot(nan)) {
+    // This wave's sums once more, from V as it is, over the same chunks: a lane takes its elements row by row.  Slow (8192
+    // rows x 4096, rank 16 27 -> 280 us), but only where Z or V hold NaN or infinities: other calls take up to 2 % longer for
+    // it, 3 to 5 if this were the loop above again.
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int f = 0; f < FR; ++f) acc[c][f] = f32x4{};
+    auto rows_of = [&](int64_t chunk) { return (uint32_t)__ballot(adapter_of(p, chunk * 32 + (lane & 31)) == a); };
+#pragma unroll 1
+    for (int64_t from = 0; from < chunks; from += kGradList) {
+      const int64_t end = from + kGradList < chunks ? from + kGradList : chunks;
+      int total = 0, i = 0;
+#pragma unroll 1
+      for (int64_t chunk = from; chunk < end; ++chunk) total += rows_of(chunk) != 0;
+      const int lo = (int)((int64_t)total * part / parts), hi = (int)((int64_t)total * (part + 1) / parts);
+#pragma unroll 1
+      for (int64_t chunk = from; chunk < end; ++chunk) {
+        uint32_t rows = rows_of(chunk);
+        if (!rows || i++ < lo || i > hi) continue;
+#pragma unroll 1
+        for (; rows; rows &= rows - 1) {
+          const int64_t t = chunk * 32 + __builtin_ctz(rows);
+          const uint16_t* z = p.X + t * p.ldx;
+          const float* v = p.V + t * p.ldv;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int64_t n = c0 + 16 * c + (NK ? col : 4 * g + e);
+              const float zf = bf16_low(z[n < p.cols ? n : p.cols - 1]);
+#pragma unroll
+              for (int f = 0; f < FR; ++f) {
+                const int r = r0 + 16 * f + (NK ? 4 * g + e : col);
+                acc[c][f][e] = __builtin_fmaf(zf, v[r < p.rank ? r : p.rank - 1], acc[c][f][e]);
+              }
+            }
+        }
+      }
+    }
+  }
   // NK: a lane holds column l % 16 and 4 ranks of a fragment, else rank l % 16 and 4 columns
   const int64_t line = NK ? p.rank : p.all_cols;                         // of the sums of a part
 #pragma unroll
