@@ -33,7 +33,8 @@ struct MoeGemmParams {
 hipError_t launch_moe_256x256(const MoeGemmParams& p, MoeLayout layout, bool out_bf16, int grid, hipStream_t stream);
 hipError_t launch_moe_64x64(const MoeGemmParams& p, MoeLayout layout, bool out_bf16, int grid, hipStream_t stream);
 hipError_t launch_moe_128x128(const MoeGemmParams& p, MoeLayout layout, bool out_bf16, int grid, hipStream_t stream);
-// Few rows of each expert, kMoeNK: 16 * fn rows of an expert's weights past 16 * fm of its rows (fn = 1 for fm = 1 alone).
+// Few rows of each expert, kMoeNK: 16 * fn rows of an expert's weights past 16 * fm of its rows (fm = fn = 1, or fm = 2 or 4
+// and fn = 2).
 hipError_t launch_moe_rows(const MoeGemmParams& p, int fm, int fn, bool out_bf16, hipStream_t stream);
 
 }  // namespace sfc

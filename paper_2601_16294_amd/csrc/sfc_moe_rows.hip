@@ -132,9 +132,10 @@ hipError_t launch(const MoeGemmParams& p, bool ob, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_moe_rows(const MoeGemmParams& p, int fm, int fn, bool out_bf16, hipStream_t stream) {
-  if (fm == 1) return fn == 1 ? launch<1, 1>(p, out_bf16, stream) : launch<1, 2>(p, out_bf16, stream);
-  if (fm == 2) return launch<2, 2>(p, out_bf16, stream);
-  return launch<4, 2>(p, out_bf16, stream);
+  if (fm == 1 && fn == 1) return launch<1, 1>(p, out_bf16, stream);
+  if (fm == 2 && fn == 2) return launch<2, 2>(p, out_bf16, stream);
+  if (fm == 4 && fn == 2) return launch<4, 2>(p, out_bf16, stream);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace sfc

@@ -3,6 +3,7 @@ needed."""
 import pytest
 
 import kernel_notes
+from test_rows_routes import exe, launches, one  # noqa: F401
 
 
 @pytest.fixture(scope="module")
@@ -17,3 +18,16 @@ def test_adapters_keep_their_values_in_registers(kernels):
     spilled = {n: (k[".vgpr_spill_count"], k[".private_segment_fixed_size"]) for n, k in mine.items()
                if k[".vgpr_spill_count"] or k[".private_segment_fixed_size"]}
     assert not spilled
+
+
+def test_few_rows_of_experts_have_no_kernel_that_no_call_takes(kernels, exe):
+    """What is compiled of the kernel that streams the experts' weights, against what the host layer asks for."""
+    asked = set()
+    for rows in (1, 2, 8, 16, 17, 32, 33, 64, 65, 512):
+        for experts in (1, 2, 8, 64, 1024):
+            for K in (4096, 4095):
+                for name, e in launches(one(exe, "experts", rows, 512, K, experts)):
+                    if name == "rows":
+                        asked.add((e["fm"], e["fn"]))
+    compiled = {tuple(int(i) for i in n[n.index("<") + 1:].split(", ")[:2]) for n in kernels if n.startswith("moe_rows_kernel<")}
+    assert compiled == asked
