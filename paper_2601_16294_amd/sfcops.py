@@ -496,9 +496,17 @@ def _f32(t, name, what, shape=None):
     return p, ld
 
 
+def _lora_sizes(what, rows, cols, rank, adapters):
+    """The sizes, if they fit the C ABI's (ctypes would cut them to 64 and 32 bits)."""
+    for v in (rows, cols, rank):
+        if not -(1 << 63) <= v < 1 << 63:
+            raise ValueError(f"{what}: sizes must be < 2^31 (got {v})")
+    return rows, cols, rank, _int(adapters, "the number of adapters", what)
+
+
 def sfc_lora_down_ws_size(rows: int, K: int, rank: int, adapters: int) -> int:
     """Bytes of the workspace that sfc_lora_down takes (0: none)."""
-    return int(lib.sfc_lora_down_ws_size(rows, K, rank, adapters))
+    return int(lib.sfc_lora_down_ws_size(*_lora_sizes("sfc_lora_down_ws_size", rows, K, rank, adapters)))
 
 
 def sfc_lora_down(X, A, ids, V, scales=None, layout: int = SFC_B_NK, stream=None, workspace=None) -> None:
@@ -539,7 +547,7 @@ def sfc_lora_up(V, B, ids, Y, base=None, layout: int = SFC_B_NK, stream=None) ->
 
 def sfc_lora_wgrad_ws_size(rows: int, columns: int, rank: int, adapters: int) -> int:
     """Bytes of the workspace that sfc_lora_wgrad takes (0: none)."""
-    return int(lib.sfc_lora_wgrad_ws_size(rows, columns, rank, adapters))
+    return int(lib.sfc_lora_wgrad_ws_size(*_lora_sizes("sfc_lora_wgrad_ws_size", rows, columns, rank, adapters)))
 
 
 def sfc_lora_wgrad(Z, V, ids, G, layout: int = SFC_B_NK, stream=None, workspace=None) -> None:
