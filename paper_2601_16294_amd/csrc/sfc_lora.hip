@@ -373,12 +373,6 @@ __device__ __forceinline__ void store_words(char* to, const row_u32x4& v, int n)
   }
 }
 
-// Ranks in NC chunks of 32; columns of a workgroup.  Wide blocks read V least often, narrow ones take fewer
-// registers (us at 64 / 128 / 256 columns: bf16 4096x14336 rank 64 74 / 65 / 61, 8192x4096 rank 16 28 / 25 / 27, fp32
-// 1003x5003 rank 12 17 / 14 / 26).
-template <int NC, bool OB>
-constexpr int up_columns() { return NC == 2 && OB ? 256 : NC <= 4 ? 128 : 64; }
-
 // Column of 64 that lane n of fragment j computes, so that a lane, which ends with 4 columns of every
 // fragment, has 16 bytes of a row at a time, and 4 lanes 64: bf16 8 columns of two fragments, fp32 4 of one.
 template <bool OB>
@@ -392,7 +386,7 @@ __device__ __forceinline__ int up_column(int j, int n) {
 // workgroups: those in flight cover whole rows.
 template <int Q, int NC, bool NK, bool OB>
 __global__ __launch_bounds__(256, (NC == 1 ? 3 : 2)) void lora_up_kernel(LoraParams p) {
-  constexpr int TERMS = OB ? 2 : 3, ES = OB ? 2 : 4, CB = up_columns<NC, OB>(), UNITS = CB / 64;
+  constexpr int TERMS = OB ? 2 : 3, ES = OB ? 2 : 4, CB = lora_up_columns(NC, OB), UNITS = CB / 64;
   constexpr int PITCH = NK ? NC * 64 + 16 : CB * 2 + 16;     // NK: [column][rank], else [rank][column]
   constexpr int PIECES = OB ? 2 : 4;           // 16-byte pieces of 64 columns of a row that a lane has
   __shared__ __attribute__((aligned(16))) unsigned char smem[NK ? CB * PITCH : 32 * NC * PITCH];
@@ -1010,22 +1004,14 @@ __global__ __launch_bounds__(256) void lora_grad_sum(LoraParams p, int64_t lines
   else reinterpret_cast<float*>(p.Y)[to] = v;
 }
 
-int lanes_for(int rank, int most) {
-  int lanes = 1;
-  while (lanes < most && 8 * lanes < rank) lanes *= 2;
-  return lanes;
-}
-
 hipError_t launch_row_down(const LoraParams& p, bool nk, hipStream_t stream) {
   if (nk) {
-    // a rank to a wave while that takes few waves, else 4, which read X once (us, K = 4096, 1 / 4: 16 rows, rank 16 3.7 / 4.9, 128
-    // rows 4.3 / 5.0, 256 rows 5.2 / 5.3, 128 rows, rank 64 7.2 / 6.5)
-    const bool one = p.rows * p.rank <= 2048;
+    const bool one = lora_row_ranks(p.rows, p.rank) == 1;
     const int64_t jobs = p.rows * (one ? p.rank : (p.rank + 3) / 4);
     return launch_kernel(one ? lora_row_down_nk<1> : lora_row_down_nk<4>, dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, stream, p);
   }
   const dim3 grid((unsigned)p.rows), block(kRowWaves * 64);
-  switch (lanes_for(p.rank, 32)) {
+  switch (lora_row_lanes(p.rank, 32)) {
     case 1: return launch_kernel(lora_row_down_kn<1>, grid, block, 0, stream, p);
     case 2: return launch_kernel(lora_row_down_kn<2>, grid, block, 0, stream, p);
     case 4: return launch_kernel(lora_row_down_kn<4>, grid, block, 0, stream, p);
@@ -1039,7 +1025,7 @@ template <bool OB>
 hipError_t launch_row_up(const LoraParams& p, bool nk, hipStream_t stream) {
   const dim3 block(256);
   if (!nk) return launch_kernel(lora_row_up_kn<OB>, dim3((unsigned)((p.cols + 2047) / 2048), (unsigned)p.rows), block, 0, stream, p);
-  const int lanes = lanes_for(p.rank, 8);
+  const int lanes = lora_row_lanes(p.rank, 8);
   const dim3 grid((unsigned)((p.cols + 1024 / lanes - 1) / (1024 / lanes)), (unsigned)p.rows);
   switch (lanes) {
     case 1: return launch_kernel(lora_row_up_nk<1, OB>, grid, block, 0, stream, p);
@@ -1057,20 +1043,20 @@ hipError_t launch_lora_down(const LoraParams& p, bool nk, hipStream_t stream) {
 
 template <int NC, bool NK, bool OB>
 static hipError_t up_launch(const LoraParams& p, int num_cus, hipStream_t stream) {
-  // 256 rows to a workgroup read the weights least often; 64 where there would be few workgroups (us, bf16, 8 runs, 64 / 256:
-  // 1024 rows x 4096, rank 64 7.7 / 16.5, 2048 11.9 / 17.4, 4096 21.9 / 21.7; 4096 x 14336 57 / 50; 8192 x 4096, rank 16 27 / 25)
-  const int64_t across = (p.cols + up_columns<NC, OB>() - 1) / up_columns<NC, OB>();
-  if (across * ((p.rows + 255) / 256) >= 2 * num_cus)
-    return launch_kernel(lora_up_kernel<4, NC, NK, OB>, dim3((unsigned)across, (unsigned)((p.rows + 255) / 256)), dim3(256), 0, stream, p);
-  return launch_kernel(lora_up_kernel<1, NC, NK, OB>, dim3((unsigned)across, (unsigned)((p.rows + 63) / 64)), dim3(256), 0, stream, p);
+  const unsigned across = (unsigned)((p.cols + lora_up_columns(NC, OB) - 1) / lora_up_columns(NC, OB));
+  if (lora_up_tiles(p.rows, p.cols, p.rank, OB, num_cus) == 4)
+    return launch_kernel(lora_up_kernel<4, NC, NK, OB>, dim3(across, (unsigned)((p.rows + 255) / 256)), dim3(256), 0, stream, p);
+  return launch_kernel(lora_up_kernel<1, NC, NK, OB>, dim3(across, (unsigned)((p.rows + 63) / 64)), dim3(256), 0, stream, p);
 }
 
 template <bool NK, bool OB>
 static hipError_t up_rank(const LoraParams& p, int num_cus, hipStream_t stream) {
-  if (p.rank <= 32) return up_launch<1, NK, OB>(p, num_cus, stream);
-  if (p.rank <= 64) return up_launch<2, NK, OB>(p, num_cus, stream);
-  if (p.rank <= 128) return up_launch<4, NK, OB>(p, num_cus, stream);
-  return up_launch<8, NK, OB>(p, num_cus, stream);
+  switch (lora_up_chunks(p.rank)) {
+    case 1: return up_launch<1, NK, OB>(p, num_cus, stream);
+    case 2: return up_launch<2, NK, OB>(p, num_cus, stream);
+    case 4: return up_launch<4, NK, OB>(p, num_cus, stream);
+    default: return up_launch<8, NK, OB>(p, num_cus, stream);
+  }
 }
 
 hipError_t launch_lora_up(const LoraParams& p, bool nk, bool bf16, int num_cus, hipStream_t stream) {
@@ -1081,8 +1067,8 @@ hipError_t launch_lora_up(const LoraParams& p, bool nk, bool bf16, int num_cus, 
 
 template <bool NK, bool OB>
 static hipError_t wgrad_launch(const LoraParams& all, hipStream_t stream) {
-  const bool narrow = all.cols < 8 || all.rank < 8;
-  const int fr = narrow ? 1 : all.rank <= 64 ? (all.rank + 15) / 16 : 4;
+  const bool narrow = lora_grad_narrow(all.cols, all.rank);
+  const int fr = lora_grad_ranks(all.cols, all.rank);
   const auto kernel = narrow    ? lora_wgrad_kernel<1, true, NK, OB>
                       : fr == 1 ? lora_wgrad_kernel<1, false, NK, OB>
                       : fr == 2 ? lora_wgrad_kernel<2, false, NK, OB>

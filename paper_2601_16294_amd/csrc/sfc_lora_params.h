@@ -49,6 +49,34 @@ inline bool lora_by_rows(int64_t rows, int64_t cols, int rank) {
   return rows <= 4096 && rows * rank * cols <= (int64_t)(rows <= 64 ? 256 : rows <= 256 ? 128 : 32) << 20;
 }
 
+// Row by row, weights N x K: ranks of a wave in down.  One while that takes few waves, else 4, which read X once (us, K = 4096, 1 / 4:
+// 16 rows, rank 16 3.7 / 4.9, 128 rows 4.3 / 5.0, 256 rows 5.2 / 5.3, 128 rows, rank 64 7.2 / 6.5).
+inline int lora_row_ranks(int64_t rows, int rank) { return rows * rank <= 2048 ? 1 : 4; }
+// Lanes of 8 ranks each that share a row of the weights, up to `most`.
+inline int lora_row_lanes(int rank, int most) {
+  int lanes = 1;
+  while (lanes < most && 8 * lanes < rank) lanes *= 2;
+  return lanes;
+}
+
+// Up in tiles: chunks of 32 ranks that a kernel holds.
+constexpr int lora_up_chunks(int rank) { return rank <= 32 ? 1 : rank <= 64 ? 2 : rank <= 128 ? 4 : 8; }
+// Columns of a workgroup.  Wide blocks read V least often, narrow ones take fewer
+// registers (us at 64 / 128 / 256 columns: bf16 4096x14336 rank 64 74 / 65 / 61, 8192x4096 rank 16 28 / 25 / 27, fp32
+// 1003x5003 rank 12 17 / 14 / 26).
+constexpr int lora_up_columns(int chunks, bool bf16) { return chunks == 2 && bf16 ? 256 : chunks <= 4 ? 128 : 64; }
+// Tiles of 16 rows of each of a workgroup's 4 waves.  256 rows to a workgroup read the weights least often; 64 where there would
+// be few workgroups (us, bf16, 8 runs, 64 / 256: 1024 rows x 4096, rank 64 7.7 / 16.5, 2048 11.9 / 17.4, 4096 21.9 / 21.7; 4096 x
+// 14336 57 / 50; 8192 x 4096, rank 16 27 / 25).
+inline int lora_up_tiles(int64_t rows, int64_t cols, int rank, bool bf16, int num_cus) {
+  const int columns = lora_up_columns(lora_up_chunks(rank), bf16);
+  return (cols + columns - 1) / columns * ((rows + 255) / 256) >= 2 * num_cus ? 4 : 1;
+}
+
+// Weight gradient: rows of Z or V of fewer than 8 elements, which are loaded one by one; ranks of a workgroup, in 16.
+inline bool lora_grad_narrow(int64_t cols, int rank) { return cols < 8 || rank < 8; }
+inline int lora_grad_ranks(int64_t cols, int rank) { return lora_grad_narrow(cols, rank) ? 1 : rank <= 64 ? (rank + 15) / 16 : 4; }
+
 // Ranges of K in the tiles of down.
 inline int lora_down_splits(int64_t rows, int64_t cols, int rank, int num_cus) {
   if (lora_by_rows(rows, cols, rank)) return 1;
@@ -68,7 +96,7 @@ inline int lora_wgrad_splits(int64_t rows, int64_t cols, int rank, int adapters,
   // parts of the rows, so that all workgroups, two to a CU, are in flight at once; each of 4 chunks at least (8
   // where there are few: a sum takes longer than 8 chunks).  Their sums are written and read back: 16 MB at
   // most.  (2^22: one launch.)
-  const int fr = cols < 8 ? 1 : rank <= 64 ? (rank + 15) / 16 : 4;
+  const int fr = lora_grad_ranks(cols, rank);
   const int64_t groups = (cols + kGradColumns - 1) / kGradColumns * ((rank + 16 * fr - 1) / (16 * fr));
   const int64_t chunks = (rows + 31) / 32, each = cols * rank;
   if (each < 1 || groups * (adapters + 32) > (int64_t)1 << 22) return 1;

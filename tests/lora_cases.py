@@ -4,7 +4,8 @@ import torch
 
 # (rows, columns, rank, adapters): down and up in tiles, every chunk count of up; the weight gradient in parts and whole, rows
 # of Z or V of fewer than 8 elements too
-SPECIAL = [(4100, 70, 12, 5), (2100, 1100, 40, 2), (1500, 515, 100, 2), (600, 520, 256, 4), (4500, 5, 3, 3), (4101, 64, 8, 1)]
+SPECIAL = [(4100, 70, 12, 5), (2100, 1100, 40, 2), (1500, 515, 100, 2), (600, 520, 256, 4), (4500, 5, 3, 3), (4101, 64, 8, 1),
+           (600, 8200, 256, 2)]
 
 
 def product(v, w):
@@ -33,3 +34,6 @@ def agrees(got, want, bound):
     g = got.double()
     fine = torch.where(torch.isfinite(want), (g - want).abs() <= bound, (g == want) | (torch.isnan(g) & torch.isnan(want)))
     return bool(fine.all())
+
+# (rows, columns, rank, adapters) that up takes with 256 rows to a workgroup, for every chunk count
+TALL = [(8300, 4003, 24, 3), (8200, 4100, 40, 4), (8300, 2050, 100, 3), (8300, 1030, 256, 2), (8200, 1040, 129, 3)]
