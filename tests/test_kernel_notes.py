@@ -3,6 +3,7 @@ needed."""
 import pytest
 
 import kernel_notes
+from rows_cases import EXPERTS
 from test_rows_routes import exe, launches, one  # noqa: F401
 
 
@@ -31,3 +32,15 @@ def test_few_rows_of_experts_have_no_kernel_that_no_call_takes(kernels, exe):
                         asked.add((e["fm"], e["fn"]))
     compiled = {tuple(int(i) for i in n[n.index("<") + 1:].split(", ")[:2]) for n in kernels if n.startswith("moe_rows_kernel<")}
     assert compiled == asked
+
+
+def test_gathered_bf16_products_of_the_gpu_tests_reach_every_block(kernels, exe):
+    """What test_gpu_moe_bf16_order.py runs (two rows behind the last segment), past the caches or not aside."""
+    reached = set()
+    for c, N, K in EXPERTS:
+        if sum(c):
+            for layout in (0, 1):
+                for pad in (0, 5):
+                    (name, e), = launches(one(exe, "experts", sum(c) + 2, N, K, len(c), layout, 1, pad=pad))
+                    reached.add((e["b"], layout) if name == "tile" else ("rows", layout))
+    assert reached >= {(b, layout) for b in (64, 128, 256) for layout in (0, 1)} | {("rows", 0)}
