@@ -73,6 +73,24 @@ __global__ void sfc_order_kernel(int gm, int gn, int order, int32_t* out) {
   }
 }
 
+// Words are dealt out from pages of pinned memory that every device reaches, and never given back.
+volatile int32_t* host_word() {
+  constexpr int kWords = 1024;
+  static int32_t* words = nullptr;
+  static int used = kWords;
+  if (used == kWords) {
+    void* p = nullptr;
+    if (hipHostMalloc(&p, kWords * sizeof(int32_t), hipHostMallocPortable | hipHostMallocMapped | hipHostMallocCoherent) != hipSuccess) {
+      (void)hipGetLastError();               // (the event alone marks the table)
+      return nullptr;
+    }
+    words = static_cast<int32_t*>(p);
+    for (int i = 0; i < kWords; ++i) words[i] = 0;
+    used = 0;
+  }
+  return words + used++;
+}
+
 hipError_t launch_sfc_order(int gm, int gn, int order, int32_t* dev_out, hipStream_t stream) {
   const int64_t total = (int64_t)gm * gn;
   int blocks = (int)((total + 255) / 256);

@@ -37,6 +37,9 @@ struct GemmParams {
 
 // Curve table of a gm x gn grid into dev_out (gm*gn int32), order = SFC_ORDER_*.
 hipError_t launch_sfc_order(int gm, int gn, int order, int32_t* dev_out, hipStream_t stream);
+// A word of host memory that the device can write, 0 so far; nullptr if there is none.  Calls one at a time.  (Weak: the host
+// layer is also built without the kernels.)
+__attribute__((weak)) volatile int32_t* host_word();
 
 // How a kernel brings its operands into LDS.
 enum Loads {

@@ -9,6 +9,7 @@
 // hipFreeAsync).
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <map>
 #include <mutex>
 #include <string>
@@ -25,11 +26,15 @@ namespace {
 thread_local std::string g_last_error;
 
 // A curve table on the device, written by a kernel on the stream of the call
-// that first needed it; `ready` marks its completion for calls on other streams.
+// that first needed it; `ready` marks its completion for calls on other streams, and
+// `word` for the host (an event cannot be asked after while the stream that it was last
+// recorded on is captured: HIP refuses and ends that capture).
 struct Table {
   int32_t* d = nullptr;
   hipEvent_t ready = nullptr;
-  bool done = false;        // `ready` has been seen complete
+  hipStream_t stream = nullptr;
+  volatile int32_t* word = nullptr;
+  bool done = false;        // it has been seen complete
 };
 
 // Layer copies of calls that pass no workspace, and arrival counters of reductions
@@ -112,19 +117,38 @@ struct RelaxedCapture {
   }
 };
 
-// Memory for a captured call: a plain allocation (one in stream order would become a
-// node of the graph and its memory the graph's).
-hipError_t captured_malloc(void** out, size_t bytes) {
+// Memory for a captured call, or while another stream is captured: a plain allocation (one
+// in stream order would become a node of the graph and its memory the graph's).
+hipError_t plain_malloc(void** out, size_t bytes) {
   RelaxedCapture relaxed;
   return relaxed.e != hipSuccess ? relaxed.e : hipMalloc(out, bytes);
+}
+
+// Whether a table is known to be complete.
+int table_done(Table& t) {
+  if (!t.done && t.word) {
+    t.done = *t.word != 0;
+    std::atomic_thread_fence(std::memory_order_acquire);
+  } else if (!t.done) {
+    hipError_t e;
+    {
+      RelaxedCapture relaxed;
+      e = hipEventQuery(t.ready);
+    }
+    if (e == hipSuccess) t.done = true;
+    else if (e == hipErrorNotReady) (void)hipGetLastError();   // not an error: do not leave it for the next check
+    else return hip_fail(e, "hipEventQuery(curve table)");
+  }
+  return SFC_OK;
 }
 
 // Curve table of a gm x gn grid on the current device.  The first call for a
 // grid allocates it and enqueues the generator on `stream` (no wait); a later
 // call on another stream waits for that kernel on the device, until the table
-// is known to be complete.  A call that is recorded into a graph before that cannot
-// wait for it: it records the generator too, into a table that only recorded calls
-// use (each replay writes the same values).  Must be called with g_mu held.
+// is known to be complete, or makes a table of its own where the generator's stream is
+// being captured (its event would join the capture).  A call that is recorded into a graph
+// before that cannot wait for it: it records the generator too, into a table that only
+// recorded calls use (each replay writes the same values).  Must be called with g_mu held.
 int get_table(DeviceState& st, int gm, int gn, int order, hipStream_t stream, const int32_t** out) {
   auto key = std::make_tuple(gm, gn, order);
   auto it = st.tables.find(key);
@@ -136,21 +160,15 @@ int get_table(DeviceState& st, int gm, int gn, int order, hipStream_t stream, co
   const bool cap = is_captured(stream);
   if (known) {
     Table& t = it->second;
-    hipError_t e;
-    {
-      RelaxedCapture relaxed;
-      e = hipEventQuery(t.ready);
+    const int rc = table_done(t);
+    if (rc != SFC_OK) return rc;
+    bool use = t.done;
+    if (!use && !cap && !(t.stream && is_captured(t.stream))) {
+      const hipError_t e = hipStreamWaitEvent(stream, t.ready, 0);
+      if (e != hipSuccess) return hip_fail(e, "hipStreamWaitEvent(curve table)");
+      use = true;
     }
-    if (e == hipSuccess) {
-      t.done = true;
-    } else if (e == hipErrorNotReady) {
-      (void)hipGetLastError();   // not an error: do not leave it for the next check
-      if (!cap) e = hipStreamWaitEvent(stream, t.ready, 0);
-      if (!cap && e != hipSuccess) return hip_fail(e, "hipStreamWaitEvent(curve table)");
-    } else {
-      return hip_fail(e, "hipEventQuery(curve table)");
-    }
-    if (t.done || !cap) {
+    if (use) {
       *out = t.d;
       return SFC_OK;
     }
@@ -159,7 +177,7 @@ int get_table(DeviceState& st, int gm, int gn, int order, hipStream_t stream, co
     int32_t*& d = st.captured_tables[key];
     if (!d) {
       void* p = nullptr;
-      hipError_t e = captured_malloc(&p, sizeof(int32_t) * (size_t)gm * (size_t)gn);
+      hipError_t e = plain_malloc(&p, sizeof(int32_t) * (size_t)gm * (size_t)gn);
       if (e != hipSuccess) return hip_fail(e, "hipMalloc(curve table of captured calls)");
       d = static_cast<int32_t*>(p);
     }
@@ -169,16 +187,24 @@ int get_table(DeviceState& st, int gm, int gn, int order, hipStream_t stream, co
     return SFC_OK;
   }
   Table t;
-  hipError_t e = hipMalloc(&t.d, sizeof(int32_t) * (size_t)gm * (size_t)gn);
+  t.stream = stream;
+  if (sfc::host_word) {
+    RelaxedCapture relaxed;
+    t.word = sfc::host_word();
+  }
+  void* d = nullptr;
+  hipError_t e = plain_malloc(&d, sizeof(int32_t) * (size_t)gm * (size_t)gn);
   if (e != hipSuccess) return hip_fail(e, "hipMalloc(curve table)");
+  t.d = static_cast<int32_t*>(d);
   e = sfc::launch_sfc_order(gm, gn, order, t.d, stream);
+  if (e == hipSuccess && t.word) e = sfc::launch_fill_i32(const_cast<int32_t*>(t.word), 1, 1, stream);
   if (e == hipSuccess) e = hipEventCreateWithFlags(&t.ready, hipEventDisableTiming);
   if (e == hipSuccess) e = hipEventRecord(t.ready, stream);
   if (e != hipSuccess) {
     // the generator may be queued: the table is kept (never used) rather than freed under it
     return hip_fail(e, "curve table");
   }
-  st.tables[key] = t;
+  st.tables[key] = t;       // (one that it replaces is kept: calls use it)
   *out = t.d;
   return SFC_OK;
 }
@@ -194,7 +220,7 @@ int stream_workspace(DeviceState& st, hipStream_t stream, size_t bytes, void** o
     void* d = nullptr;
     if (cap) {
       if (bytes < 2 * m.ws_bytes) bytes = 2 * m.ws_bytes;
-      hipError_t e = captured_malloc(&d, bytes);
+      hipError_t e = plain_malloc(&d, bytes);
       if (e != hipSuccess) return hip_fail(e, "hipMalloc(workspace of captured calls)");
     } else {
       if (m.ws) {
@@ -225,7 +251,7 @@ int stream_counters(DeviceState& st, hipStream_t stream, int64_t n, int32_t** ou
     int64_t count = n < 4096 ? 4096 : n;
     if (cap) {
       if (count < 2 * m.n_counters) count = 2 * m.n_counters;
-      hipError_t e = captured_malloc(&d, (size_t)count * 4u);
+      hipError_t e = plain_malloc(&d, (size_t)count * 4u);
       if (e != hipSuccess) return hip_fail(e, "hipMalloc(counters of captured calls)");
     } else {
       if (m.counters) {
