@@ -550,8 +550,9 @@ int sfc_moe_wgrad_mx4_ex(int64_t M, int64_t N, int64_t rows, int experts,
  *   offsets    experts + 1 segment bounds, on the device; bounds outside 0 .. rows count as the
  *              nearest of them.
  *   C          rows x N, out_type.
- * The gradient of A is the same call with the other layout.  The kernel and its block shape are chosen from
- * rows, N, K and experts, so equal calls give equal bits.
+ * The gradient of A is the same call with the other layout.  The kernel and its block shape, and with them the order of
+ * the sums, are chosen from rows, N, K, experts, b_layout, out_type, whether A, B, lda, ldb and stride_b make 16-byte
+ * aligned rows, and the device's number of CUs: calls that are equal in these repeat their bits.
  */
 int sfc_moe_gemm_ex(int64_t rows, int64_t N, int64_t K, int experts,
                     const void *A, int64_t lda, const int32_t *order, int64_t a_rows, int topk,
