@@ -10,7 +10,7 @@
 // leave, the last one rounded: two are off by at most 2^-16 of it (bf16 results, which are rounded to 2^-8),
 // three hold every bit of it (fp32 results), down to 2^-134.
 //
-// Measured: up of 4096 rows x 14336, rank 64 58 us = 4.2 TB/s, of 8192 x 4096, rank 16 27 us = 5 TB/s; 32 rows x 4096 of 16
+// Measured: up of 4096 rows x 14336, rank 64 57 us = 4.2 TB/s, of 8192 x 4096, rank 16 26 us = 5.2 TB/s; 32 rows x 4096 of 16
 // adapters, rank 16, 3.7 us down and 3.7 up, a launch and a chain of loads each.
 //
 // Two forms of down and up.  Where rows x rank x columns is small, as in decode steps, every row is taken by
@@ -655,7 +655,8 @@ __device__ __forceinline__ void store4(float* to, const f32x4& v, int64_t inside
 // slots of LDS, the next one written while one is computed with, three more on their way.  In a
 // chunk, rows of other adapters are zeros in both operands.  Bound: one read of Z for every 64 ranks, 13 us for 8192
 // rows x 4096, rank 16; with 4 adapters it takes 26 and the sum 4: the pass over the ids, the list and the first loads come before
-// a workgroup's 8 chunks (2001 rows x 4097, rank 40, 4 chunks each: 19).
+// a workgroup's 8 chunks (2001 rows x 4097, rank 40, 4 chunks each: 19).  That is for rows in runs: a chunk is loaded once for every
+// adapter that has a row in it (both launches, 8192 rows x 4096, rank 16, runs / at random: 4 adapters 27 / 62, 32 adapters 27 / 198).
 // NARROW: rows of Z or V of fewer than 8 elements, which are loaded one by one.
 template <int FR, bool NARROW, bool NK, bool OB>
 __global__ __launch_bounds__(kGradWaves * 64) void lora_wgrad_kernel(LoraParams p) {

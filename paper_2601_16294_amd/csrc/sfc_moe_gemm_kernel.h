@@ -27,7 +27,8 @@
 // TFLOP/s for kMoeNK and kMoeKN, 1330 for kMoeTN, with the MFMAs busy in 63, 60 and 58 % of the cycles at 2.16 GHz, no
 // bank conflicts, waves waiting in a fifth of the cycles (other places of the barrier and of the loads: within 1.5 %).
 // Stores take 5 to 6 % of a product, up to a fifth of a weight gradient in fp32.  4096 tokens, 2 of 8 experts
-// 14336x4096: 852 us = 1129 TFLOP/s, 12 % more with the empty rows of last blocks.  256x256 blocks read each
+// 14336x4096: 845 us = 1139 TFLOP/s, 12 % more with the empty rows of last blocks.  256x256 blocks of kMoeNK and kMoeKN spill 2
+// to 9 registers, outside of the stages' loop, where one reload waits for the loads in flight, once a block.  256x256 blocks read each
 // operand least often; 128x128 and 64x64, two and four workgroups to a CU, fill the chip where there are few rows or
 // columns: moe_tile_us() of the host layer estimates which takes least.
 #pragma once

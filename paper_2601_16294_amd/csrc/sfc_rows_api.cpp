@@ -25,9 +25,11 @@ int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 
 // Whether a C of so many elements goes past the caches: from 32 MB on, as for the 4-bit products.  Not the largest whose
 // rows are stored in parts of lines where the depth of `stages` is soon computed, so that stores bound the call (us past
-// the caches / through them, results in rotation: weight gradients in fp32 of 60 experts 1407x2047, 17 rows each, 691 MB 284 / 203,
-// of 64 experts 1999x999, 64 rows, 511 MB 195 / 181, 1001x1503, 250 rows, 385 MB 163 / 156, but of 16 experts, 96 MB 48 / 53,
-// and of 8 experts 4095x4095, 2048 rows, 537 MB 602 / 633).
+// the caches / through them, weight gradients with inputs and results in rotation over four sets: fp32, 60 experts 1407x2047, 17
+// rows each, 691 MB 286 / 200; 64 of 2001x1503, 128 rows, 770 MB 278 / 254; 64 of 1001x1503, 250 rows, 385 MB 172 / 153; 32 of
+// 2001x1503, 128 rows, 385 MB 130 / 130; bf16, 60 of 1407x2047, 17 rows, 346 MB 210 / 132; 64 of 2047x2047, 250 rows, 536 MB 429 /
+// 412.  Whole lines, fp32, 60 of 1408x2048, 17 rows, 692 MB 124 / 128; deep, 8 of 4095x4095, 2048 rows, 537 MB 624 / 631).
+// Below 256 MB it goes either way: 16 of 1001x1503, 96 MB, 250 rows 46 / 47, but 64 rows 38 / 30.
 bool past_caches(int64_t elements, int out_type, const void* C, int64_t ldc, int64_t stages) {
   const int64_t size = sfc::type_size(out_type), bytes = elements * size;
   const bool whole = ((uintptr_t)C | (uintptr_t)(ldc * size)) % 16 == 0;
