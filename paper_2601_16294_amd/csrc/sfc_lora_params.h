@@ -62,12 +62,14 @@ inline int lora_row_lanes(int rank, int most) {
 // Up in tiles: chunks of 32 ranks that a kernel holds.
 constexpr int lora_up_chunks(int rank) { return rank <= 32 ? 1 : rank <= 64 ? 2 : rank <= 128 ? 4 : 8; }
 // Columns of a workgroup.  Wide blocks read V least often, narrow ones take fewer
-// registers (us at 64 / 128 / 256 columns: bf16 4096x14336 rank 64 74 / 65 / 61, 8192x4096 rank 16 28 / 25 / 27, fp32
-// 1003x5003 rank 12 17 / 14 / 26).
+// registers (us at 64 / 128 / 256 columns: bf16 4096x14336 rank 64 70 / 55 / 53, 8192x4096 rank 16 27 / 25 / 26, fp32
+// 1003x5003 rank 12 14 / 14 / 22, bf16 4096x4096 rank 128 35 / 25 / 27).  Ranks over 128: 64 hold all of their ranks in
+// registers; 128 spill up to 46 with fp32 results and leave small batches few workgroups, but large ones would gain (rank 256, 64 /
+// 128: 600x520 15 / 19, fp32 1000x14336 69 / 81, bf16 4096x4096 54 / 38).
 constexpr int lora_up_columns(int chunks, bool bf16) { return chunks == 2 && bf16 ? 256 : chunks <= 4 ? 128 : 64; }
 // Tiles of 16 rows of each of a workgroup's 4 waves.  256 rows to a workgroup read the weights least often; 64 where there would
-// be few workgroups (us, bf16, 8 runs, 64 / 256: 1024 rows x 4096, rank 64 7.7 / 16.5, 2048 11.9 / 17.4, 4096 21.9 / 21.7; 4096 x
-// 14336 57 / 50; 8192 x 4096, rank 16 27 / 25).
+// be few workgroups (us, bf16, 8 runs, 64 / 256: 1024 rows x 4096, rank 64 7.4 / 16.4, 2048 11.5 / 17.2, 4096 21.1 / 20.7; 4096 x
+// 14336 57 / 50; 8192 x 4096, rank 16 27 / 25; 4096 x 4096, rank 256 70 / 55).
 inline int lora_up_tiles(int64_t rows, int64_t cols, int rank, bool bf16, int num_cus) {
   const int columns = lora_up_columns(lora_up_chunks(rank), bf16);
   return (cols + columns - 1) / columns * ((rows + 255) / 256) >= 2 * num_cus ? 4 : 1;
