@@ -41,10 +41,10 @@ constexpr int kGradWaves = 4, kGradColumns = 64 * kGradWaves;
 constexpr int kGradAdapters = 1024;                      // most adapters whose rows are dealt out in parts
 
 // Whether rows are taken one by one, each reading its adapter's weights (from the L2 for the most part).  That takes
-// the same time in any order of the rows; the tiles are faster where rows come in runs and slower where they do not,
+// about the same time in any order of the rows; the tiles are faster where rows come in runs and slower where they do not,
 // which the host does not know (us of up, bf16, one by one / tiles of 8 runs / tiles of 32 adapters at random: 64 rows x
-// 14336, rank 64 15 / 23 / 77; 256 x 14336, rank 16 15 / 7 / 46; 512 x 4096, rank 16 9 / 5 / 43; 2048 x 4096, rank 64 108 /
-// 11 / 94).  Up to 256 rows may be a decode step, a request each; more are taken for prompts.
+// 14336, rank 64 15 / 23 / 85; 256 x 14336, rank 16 14 / 7 / 41; 512 x 4096, rank 16 9 / 5 / 39; 2048 x 4096, rank 64 107 /
+// 11 / 102).  Up to 256 rows may be a decode step, a request each; more are taken for prompts.
 inline bool lora_by_rows(int64_t rows, int64_t cols, int rank) {
   return rows <= 4096 && rows * rank * cols <= (int64_t)(rows <= 64 ? 256 : rows <= 256 ? 128 : 32) << 20;
 }
