@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 import torch
 
-from lora_cases import SPECIAL, agrees, product, special
+from lora_cases import SPECIAL, TALL, agrees, product, special
 from rows_cases import BF16, F32, framed, small_ints, untouched_outside
 
 pytestmark = pytest.mark.gpu
@@ -89,6 +89,13 @@ def test_up(so, rows, cols, rank, n, nk, dtype, which):
     assert torch.equal(y[none], base[none]) and untouched_outside(y)
 
 
+@pytest.mark.parametrize("rows,cols,rank,n", TALL)
+@pytest.mark.parametrize("nk", [True, False])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_up_of_256_rows_to_a_workgroup(so, rows, cols, rank, n, nk, dtype):
+    test_up(so, rows, cols, rank, n, nk, dtype, "both")
+
+
 @pytest.mark.parametrize("rows,cols,rank,n", SPECIAL)
 @pytest.mark.parametrize("nk", [True, False])
 @pytest.mark.parametrize("which", ["rows", "V", "both"])
@@ -110,6 +117,23 @@ def test_weight_gradient(so, rows, cols, rank, n, nk, which):
         bound = 3 * len(t) * 2.0 ** -23 * size + 2.0 ** -134 * torch.where(torch.isfinite(z[t]), z[t].abs(), 0.0).sum(0).double()[:, None]
         assert agrees(g[i] if nk else g[i].t(), want, bound)
     assert untouched_outside(g)
+
+
+@pytest.mark.parametrize("rows,cols,rank,n", [(70_001, 40, 9, 2), (140_000, 300, 20, 1), (66_000, 6, 5, 3), (131_100, 70, 8, 1030)])
+@pytest.mark.parametrize("nk", [True, False])
+def test_weight_gradient_of_more_rows_than_are_listed_at_a_time(so, rows, cols, rank, n, nk):
+    """Infinite Z in the first rows and the last, times V of which later terms are 0."""
+    ids = (torch.arange(rows, device="cuda") // 50 % n).to(torch.int32)
+    z, v = small_ints((rows, cols), 1, most=1), torch.ones((rows, rank), device="cuda")
+    v[::2] = -2.0
+    z[70, cols // 2], z[rows - 3, 1] = INF, -INF
+    g = torch.full((n, cols, rank) if nk else (n, rank, cols), 5.0, device="cuda")
+    so.sfc_lora_wgrad(z, v, ids, g, layout=so.SFC_B_NK if nk else so.SFC_B_KN)
+    for i in {0, n - 1, int(ids[70]), int(ids[rows - 3])}:
+        t = torch.nonzero(ids == i)[:, 0]
+        want, _ = product(z[t].t(), v[t].t())
+        assert agrees(g[i] if nk else g[i].t(), want, 0.0)
+    assert torch.isinf(g).sum() == 2 * rank and not torch.isnan(g).any()
 
 
 @pytest.mark.parametrize("nk", [True, False])
